@@ -459,6 +459,179 @@ int smallkv_match_workspace_size(const smallkv_match_t *match, size_t *bytes);
 /* Enqueues the matching on `stream` (two or three kernel launches). */
 int smallkv_match(const smallkv_match_t *match, void *ws, size_t ws_bytes, void *stream);
 
+/* ---------------------------------------------------------------------------
+ * The caches themselves: what fills them and what keeps them small.  A chunk
+ * of new tokens (a prompt, a piece of one, or a decode step's single tokens)
+ * is turned by its rotary positions and appended (smallkv_append), attends to
+ * the cache (smallkv_chunk_attn) and leaves its attention weights with the
+ * cached rows (smallkv_chunk_scores), by which smallkv_evict chooses the rows
+ * that a compressed cache keeps.  All four take one layer's operands, or, where
+ * no queries are involved (smallkv_evict), several layers as n_heads = layers *
+ * kv heads.  A dense cache [B][layers][Hkv][n_cap][d] is described in place
+ * (page_table NULL), so these calls fill exactly what smallkv_step reads, and
+ * smallkv_evict's outputs are the small model's k, v, held and row_pos. */
+
+/* The keys and values of every sequence: row r of sequence b and kv head h is
+ * at k + page * page_stride + h * head_stride + (r % page_rows) * row_stride
+ * elements (v alike), with page = page_table[b][r / page_rows], or, without a
+ * table, page = b (and r < page_rows).  Rows hold head_dim elements; k, v and
+ * every stride are multiples of 16 bytes.  A row whose page number is outside
+ * [0, n_pages) is absent: not attended, not written, not copied. */
+typedef struct {
+  void *k, *v;
+  int32_t dtype, head_dim;  /* smallkv_dtype_t; 64 or 128 */
+  int32_t n_heads;          /* kv heads */
+  int32_t page_rows;        /* rows per page: a power of two with a table; without
+                               one any number >= 1, the rows a sequence can have */
+  int32_t n_pages;          /* pages of the pool; >= the batch without a table */
+  int32_t table_width;      /* pages per sequence in the table */
+  int64_t page_stride, head_stride, row_stride; /* in elements, >= 0 */
+  const int32_t *page_table; /* [B][table_width] or NULL */
+} smallkv_cache_t;
+
+/* The new tokens of a batch, packed without gaps between sequences: tokens
+ * start[b] .. start[b+1]-1 belong to sequence b and are the last of its len[b]
+ * cached rows (token i of n: row len[b] - n + i).  A sequence may have none.
+ * Device values are clamped (start into [0, n_tokens], the new tokens to
+ * max_new, len to max_len and the cache's rows); tokens in no sequence are
+ * neither read nor written, and neither are those past max_new. */
+typedef struct {
+  int32_t batch;     /* B >= 1 */
+  int32_t n_tokens;  /* packed tokens, >= 0 */
+  int32_t max_new;   /* host: no sequence has more new tokens, >= 1 */
+  int32_t max_len;   /* host: no sequence has more cached rows, >= 1 */
+  const int32_t *start; /* [B+1], ascending */
+  const int32_t *len;   /* [B], the new tokens included */
+} smallkv_chunk_t;
+
+/* Queries of the packed tokens: token t, head h at q + t * token_stride +
+ * h * head_stride elements (multiples of 16 bytes, like q), in the cache's
+ * dtype and head_dim; head h reads kv head h / (n_heads / cache n_heads). */
+typedef struct {
+  int32_t n_heads;
+  float scale;       /* softmax scale, > 0 */
+  const void *q;
+  int64_t token_stride, head_stride;
+  void *out;         /* smallkv_chunk_attn: the output, laid out by its own strides */
+  int64_t out_token_stride, out_head_stride;
+  float *lse;        /* [n_tokens][n_heads] ln of the sum of exp(logit): written by
+                        smallkv_chunk_attn (NULL: not), read by smallkv_chunk_scores */
+} smallkv_queries_t;
+
+/* Rotary positions.  Pair j < rot_dim / 2 of a head turns by the angle
+ * position * freq[j] and is multiplied by `amplitude`:
+ *   x' = amplitude * (x cos - y sin),  y' = amplitude * (x sin + y cos)
+ * with (x, y) = elements (j, j + rot_dim/2) or (2j, 2j + 1); elements from
+ * rot_dim on are copied.  The angle is reduced in 64 bits, so that far positions
+ * keep their accuracy; the rest is fp32, rounded once to the dtype. */
+typedef enum { SMALLKV_ROPE_HALF = 0, SMALLKV_ROPE_INTERLEAVED = 1 } smallkv_rope_layout_t;
+
+/* Frequencies for positions past those a model was trained on, f_j =
+ * base^(-2j/rot_dim) changed by `factor`: */
+typedef enum {
+  SMALLKV_ROPE_PLAIN = 0,  /* f_j */
+  SMALLKV_ROPE_LINEAR = 1, /* f_j / factor: positions interpolated */
+  SMALLKV_ROPE_BASE = 2,   /* base * factor^(rot_dim / (rot_dim - 2)) in place of base
+                              (rot_dim 2: unchanged) */
+  SMALLKV_ROPE_RAMP = 3,   /* f_j / factor for slow pairs, f_j for fast ones, a linear
+                              ramp in j between the pairs that turn `high` and `low`
+                              times over `orig_len` positions (YaRN, arXiv 2309.00071,
+                              its bounds rounded outwards to whole pairs);
+                              amplitude 0.1 ln(factor) + 1 */
+  SMALLKV_ROPE_BANDS = 4   /* the same with a ramp in the turns themselves,
+                              (turns - low) / (high - low) */
+} smallkv_rope_scaling_t;
+
+/* freq[0 .. rot_dim/2 - 1] (HOST memory) and the amplitude (NULL: not wanted).
+ * low, high and orig_len are read by RAMP and BANDS only (0 < low < high,
+ * orig_len >= 1).  SMALLKV_EINVAL for an odd rot_dim or one below 2, base <= 1,
+ * factor < 1 or an unknown scaling.  Host only. */
+int smallkv_rope_freqs(int32_t rot_dim, double base, int32_t scaling, double factor, double low,
+                       double high, int32_t orig_len, double *freq, float *amplitude);
+
+typedef struct {
+  const void *q, *k, *v;  /* the new tokens' projections, in the cache's dtype */
+  int64_t q_token_stride, q_head_stride, k_token_stride, k_head_stride, v_token_stride,
+      v_head_stride;      /* in elements, multiples of 16 bytes like the pointers */
+  int32_t n_q_heads;
+  void *q_out;            /* turned queries; may be q itself with the same strides */
+  int64_t q_out_token_stride, q_out_head_stride;
+  const int32_t *positions; /* [n_tokens] or NULL: the token's cached row */
+  const double *freq;       /* [rot_dim / 2], device memory */
+  int32_t rot_dim;          /* even, 0 .. head_dim (0: nothing turns) */
+  int32_t layout;           /* smallkv_rope_layout_t */
+  float amplitude;
+  int32_t *row_pos;         /* optional [B][cache n_heads][pos_rows]: the position of
+                               each appended row, written where row < pos_rows */
+  int32_t pos_rows;
+} smallkv_append_t;
+
+/* q_out = turned q; the cache rows of the new tokens = turned k, and v.  Nothing
+ * else of the cache is written.  One launch. */
+int smallkv_append(const smallkv_chunk_t *chunk, const smallkv_cache_t *cache,
+                   const smallkv_append_t *append, void *stream);
+
+/* For every new token and query head: the softmax attention over the cached
+ * rows up to and including the token's own (logits scale * <q, K_r>):
+ *   out = sum softmax_r V_r,  lse = ln sum_r exp(logit_r)
+ * A token that sees no row (its row number is negative, or every page absent)
+ * gets out = 0 and lse = -inf.  Infinities and NaN in rows a token does not see
+ * do not reach it.  bf16 models: the probabilities are rounded to bf16 for the
+ * product with V (2^-8 relative); sums, logits and statistics are fp32.
+ * ws: smallkv_chunk_attn_workspace_size (may be 0); calls that share one must
+ * not overlap.  Deterministic. */
+int smallkv_chunk_attn(const smallkv_chunk_t *chunk, const smallkv_cache_t *cache,
+                       const smallkv_queries_t *queries, void *ws, size_t ws_bytes, void *stream);
+int smallkv_chunk_attn_workspace_size(const smallkv_chunk_t *chunk, const smallkv_cache_t *cache,
+                                      const smallkv_queries_t *queries, size_t *bytes);
+
+/* The attention weight each cached row receives from the new tokens, added to
+ * its running score (Eq. 1's column sums; H2O's accumulated attention):
+ *   out[b][h][r] = (r < len_b - n_b ? before[b][h][r] : 0) +
+ *                  sum over the new tokens that see row r of exp(logit - lse)
+ * for r < len_b: the new tokens' own rows start from 0, entries r >= len_b are
+ * not written, and absent rows receive nothing.  n_score_heads = the query heads
+ * (one sum each), or the cache's kv heads (the sum over the query heads of each
+ * as well).  before, out: [B][n_score_heads][score_rows] fp32, score_rows >=
+ * max_len; out may be before; before NULL: 0.  queries->lse is read, out of it
+ * is not used.  Sums are fp32 in a fixed order: deterministic. */
+int smallkv_chunk_scores(const smallkv_chunk_t *chunk, const smallkv_cache_t *cache,
+                         const smallkv_queries_t *queries, int32_t n_score_heads,
+                         const float *before, float *out, int64_t score_rows, void *stream);
+
+/* Eviction by accumulated attention weight.  Per sequence b and kv head, of the
+ * n = len[b] rows of `from`:
+ *   kept  = min(max(keep[b], 0), n, the rows of `to`, out_rows)
+ *   last  = min(max(recent[b], 0), kept)   rows from the end stay
+ *   first = min(sinks, kept - last)        rows from the start stay
+ * and of the rows between, the kept - last - first of largest F, equal F by
+ * lower row, F = the sum of the kv head's n_score_heads / n_heads score rows in
+ * ascending order (fp32; -0 equals 0, NaN ranks below everything).  Row i of
+ * `to` becomes the i-th kept row in ascending order, and likewise out_scores
+ * and out_pos (row_pos NULL: the row itself); entries from `kept` on are not
+ * written.  held[b] = kept.  `to` and the outputs must not overlap `from` and
+ * the inputs (the same k or v pointer gives SMALLKV_EINVAL).  Deterministic. */
+typedef struct {
+  int32_t batch, max_len;      /* max_len: host, no sequence has more rows */
+  const int32_t *len, *keep;   /* [B] */
+  const int32_t *recent;       /* [B] or NULL (0) */
+  int32_t sinks;               /* host, >= 0 */
+  smallkv_cache_t from, to;    /* same dtype, head_dim and n_heads */
+  int32_t n_score_heads;       /* a multiple of n_heads, at most 64 per kv head */
+  const float *scores;         /* [B][n_score_heads][score_rows], score_rows >= max_len */
+  int64_t score_rows;
+  const int32_t *row_pos;      /* [B][n_heads][pos_rows] or NULL, pos_rows >= max_len */
+  int64_t pos_rows;
+  int64_t out_rows;            /* >= 1 */
+  float *out_scores;           /* [B][n_score_heads][out_rows] or NULL */
+  int32_t *out_pos;            /* [B][n_heads][out_rows] */
+  int32_t *held;               /* [B] */
+} smallkv_evict_t;
+
+/* max_len up to 2^20 (SMALLKV_EUNSUPPORTED past it). */
+int smallkv_evict(const smallkv_evict_t *evict, void *ws, size_t ws_bytes, void *stream);
+int smallkv_evict_workspace_size(const smallkv_evict_t *evict, size_t *bytes);
+
 /* A static string for a status code. */
 const char *smallkv_status_string(int status);
 

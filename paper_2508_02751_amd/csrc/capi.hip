@@ -2,6 +2,8 @@
 // and launches.  Nothing here touches device memory or synchronises.
 #include <hip/hip_runtime.h>
 
+#include <math.h>
+
 #include <mutex>
 
 #include "launch.h"
@@ -180,6 +182,119 @@ int check_match(const smallkv_match_t *m) {
   const int64_t H = (int64_t)m->large.n_layers * m->large.n_q_heads +
                     (int64_t)m->small.n_layers * m->small.n_q_heads;
   if (H > 65535) return SMALLKV_EUNSUPPORTED;
+  return SMALLKV_OK;
+}
+
+// ---- cache operators ----
+
+// A stride in elements: not negative, whole 16-byte pieces.
+bool stride_ok(int64_t s, int dtype) { return s >= 0 && s % (dtype == SMALLKV_F32 ? 4 : 8) == 0; }
+
+int check_cache(const smallkv_cache_t *c, int batch) {
+  if (!c || !c->k || !c->v || c->n_heads < 1 || c->page_rows < 1 || c->n_pages < 1) return SMALLKV_EINVAL;
+  if (c->dtype != SMALLKV_F32 && c->dtype != SMALLKV_BF16) return SMALLKV_EINVAL;
+  if (!aligned16(c->k) || !aligned16(c->v)) return SMALLKV_EINVAL;
+  const int64_t strides[] = {c->page_stride, c->head_stride, c->row_stride};
+  for (const int64_t s : strides)
+    if (!stride_ok(s, c->dtype)) return SMALLKV_EINVAL;
+  if (c->page_table) {
+    if (c->table_width < 1 || (c->page_rows & (c->page_rows - 1))) return SMALLKV_EINVAL;
+    if ((int64_t)c->page_rows * c->table_width > (1 << 30)) return SMALLKV_EUNSUPPORTED;
+  } else {
+    if (c->n_pages < batch) return SMALLKV_EINVAL;
+    if (c->page_rows > (1 << 30)) return SMALLKV_EUNSUPPORTED;
+  }
+  if (c->head_dim != 64 && c->head_dim != 128) return SMALLKV_EUNSUPPORTED;
+  for (const int64_t s : strides)
+    if (s / (c->dtype == SMALLKV_F32 ? 4 : 8) > UINT32_MAX) return SMALLKV_EUNSUPPORTED;
+  if ((int64_t)batch * c->n_heads > (1 << 24)) return SMALLKV_EUNSUPPORTED;
+  return SMALLKV_OK;
+}
+
+// Rows that are written: no broadcast strides.
+bool writable(const smallkv_cache_t &c) {
+  return (c.page_rows == 1 || c.row_stride >= c.head_dim) && (c.n_heads == 1 || c.head_stride >= c.head_dim) &&
+         (c.n_pages == 1 || c.page_stride >= c.head_dim);
+}
+
+int check_chunk(const smallkv_chunk_t *c, const smallkv_cache_t *kv) {
+  if (!c || c->batch < 1 || c->n_tokens < 0 || c->max_new < 1 || c->max_len < 1) return SMALLKV_EINVAL;
+  if (!c->start || !c->len) return SMALLKV_EINVAL;
+  const int rc = check_cache(kv, c->batch);
+  if (rc) return rc;
+  if (c->max_len > (1 << 30) || c->max_new > (1 << 30) || c->n_tokens > (1 << 30))
+    return SMALLKV_EUNSUPPORTED;
+  return SMALLKV_OK;
+}
+
+int check_queries(const smallkv_chunk_t *c, const smallkv_cache_t *kv, const smallkv_queries_t *q) {
+  const int rc = check_chunk(c, kv);
+  if (rc) return rc;
+  if (!q || !q->q || q->n_heads < 1 || q->n_heads % kv->n_heads) return SMALLKV_EINVAL;
+  if (!(q->scale > 0.0f) || !(q->scale <= 3.402823e38f)) return SMALLKV_EINVAL;
+  if (!aligned16(q->q) || !stride_ok(q->token_stride, kv->dtype) || !stride_ok(q->head_stride, kv->dtype))
+    return SMALLKV_EINVAL;
+  // rows (token, query head of a group) and tiles of 32 of them are counted in 32 bits
+  const int64_t rows = (int64_t)c->max_new * (q->n_heads / kv->n_heads);
+  if (rows > (1 << 30) || (rows + 31) / 32 * c->batch * kv->n_heads > (1 << 30)) return SMALLKV_EUNSUPPORTED;
+  return SMALLKV_OK;
+}
+
+int check_attn(const smallkv_chunk_t *c, const smallkv_cache_t *kv, const smallkv_queries_t *q) {
+  const int rc = check_queries(c, kv, q);
+  if (rc) return rc;
+  if (!q->out || !aligned16(q->out) || !stride_ok(q->out_token_stride, kv->dtype) ||
+      !stride_ok(q->out_head_stride, kv->dtype))
+    return SMALLKV_EINVAL;
+  if ((c->n_tokens > 1 && q->out_token_stride < kv->head_dim) ||
+      (q->n_heads > 1 && q->out_head_stride < kv->head_dim))
+    return SMALLKV_EINVAL;
+  return SMALLKV_OK;
+}
+
+int check_append(const smallkv_chunk_t *c, const smallkv_cache_t *kv, const smallkv_append_t *a) {
+  const int rc = check_chunk(c, kv);
+  if (rc) return rc;
+  if (!a || !a->q || !a->k || !a->v || !a->q_out || a->n_q_heads < 1) return SMALLKV_EINVAL;
+  if (a->n_q_heads % kv->n_heads) return SMALLKV_EINVAL;
+  if (!writable(*kv)) return SMALLKV_EINVAL;
+  if ((c->n_tokens > 1 && a->q_out_token_stride < kv->head_dim) ||
+      (a->n_q_heads > 1 && a->q_out_head_stride < kv->head_dim))
+    return SMALLKV_EINVAL;
+  const void *ptrs[] = {a->q, a->k, a->v, a->q_out};
+  for (const void *p : ptrs)
+    if (!aligned16(p)) return SMALLKV_EINVAL;
+  const int64_t strides[] = {a->q_token_stride, a->q_head_stride, a->k_token_stride, a->k_head_stride,
+                             a->v_token_stride, a->v_head_stride, a->q_out_token_stride,
+                             a->q_out_head_stride};
+  for (const int64_t s : strides)
+    if (!stride_ok(s, kv->dtype)) return SMALLKV_EINVAL;
+  if (a->q_out == a->q && (a->q_out_token_stride != a->q_token_stride ||
+                           a->q_out_head_stride != a->q_head_stride))
+    return SMALLKV_EINVAL;
+  if (a->rot_dim < 0 || a->rot_dim > kv->head_dim || a->rot_dim % 2) return SMALLKV_EINVAL;
+  if (a->rot_dim > 0 && !a->freq) return SMALLKV_EINVAL;
+  if (a->layout != SMALLKV_ROPE_HALF && a->layout != SMALLKV_ROPE_INTERLEAVED) return SMALLKV_EINVAL;
+  if (!(a->amplitude == a->amplitude)) return SMALLKV_EINVAL;
+  if (a->row_pos && a->pos_rows < 1) return SMALLKV_EINVAL;
+  if (a->n_q_heads > (1 << 16)) return SMALLKV_EUNSUPPORTED;
+  return SMALLKV_OK;
+}
+
+int check_evict(const smallkv_evict_t *e) {
+  if (!e || e->batch < 1 || e->max_len < 1 || e->sinks < 0 || e->out_rows < 1) return SMALLKV_EINVAL;
+  if (!e->len || !e->keep || !e->scores || !e->out_pos || !e->held) return SMALLKV_EINVAL;
+  int rc = check_cache(&e->from, e->batch);
+  if (rc) return rc;
+  if ((rc = check_cache(&e->to, e->batch))) return rc;
+  if (e->from.dtype != e->to.dtype || e->from.head_dim != e->to.head_dim || e->from.n_heads != e->to.n_heads)
+    return SMALLKV_EINVAL;
+  if (!writable(e->to)) return SMALLKV_EINVAL;
+  if (e->from.k == e->to.k || e->from.v == e->to.v) return SMALLKV_EINVAL;
+  if (e->out_pos == e->row_pos || e->out_scores == e->scores) return SMALLKV_EINVAL;
+  if (e->n_score_heads < 1 || e->n_score_heads % e->from.n_heads) return SMALLKV_EINVAL;
+  if (e->score_rows < e->max_len || (e->row_pos && e->pos_rows < e->max_len)) return SMALLKV_EINVAL;
+  if (e->n_score_heads / e->from.n_heads > 64 || e->max_len > (1 << 20)) return SMALLKV_EUNSUPPORTED;
   return SMALLKV_OK;
 }
 
@@ -448,6 +563,88 @@ int smallkv_match(const smallkv_match_t *m, void *ws, size_t ws_bytes, void *str
   if (rc) return rc;
   if (!ws || ws_bytes < match_layout(*m).total) return SMALLKV_EWORKSPACE;
   return status_of(launch_match(*m, ws, static_cast<hipStream_t>(stream)));
+}
+
+int smallkv_rope_freqs(int32_t rot_dim, double base, int32_t scaling, double factor, double low, double high,
+                       int32_t orig_len, double *freq, float *amplitude) {
+  if (!freq || rot_dim < 2 || rot_dim % 2 || !(base > 1.0) || !(factor >= 1.0) || !isfinite(base) ||
+      !isfinite(factor))
+    return SMALLKV_EINVAL;
+  if (scaling < SMALLKV_ROPE_PLAIN || scaling > SMALLKV_ROPE_BANDS) return SMALLKV_EINVAL;
+  const bool ramp = scaling == SMALLKV_ROPE_RAMP, bands = scaling == SMALLKV_ROPE_BANDS;
+  if ((ramp || bands) && (!(low > 0.0) || !(high > low) || !isfinite(high) || orig_len < 1)) return SMALLKV_EINVAL;
+  constexpr double kTwoPi = 6.283185307179586476925;
+  if (scaling == SMALLKV_ROPE_BASE && rot_dim > 2) base *= pow(factor, rot_dim / (rot_dim - 2.0));
+  // the pair that turns `turns` times over orig_len positions
+  auto pair = [&](double turns) { return rot_dim * log(orig_len / (turns * kTwoPi)) / (2.0 * log(base)); };
+  const double from = ramp ? fmax(floor(pair(high)), 0.0) : 0.0;
+  const double to = ramp ? fmin(ceil(pair(low)), rot_dim - 1.0) : 0.0;
+  for (int j = 0; j < rot_dim / 2; ++j) {
+    const double f = pow(base, -2.0 * j / rot_dim);
+    double slow = 0.0;  // the share of f / factor
+    if (scaling == SMALLKV_ROPE_LINEAR) slow = 1.0;
+    if (ramp) slow = fmin(fmax((j - from) / fmax(to - from, 1e-3), 0.0), 1.0);
+    if (bands) slow = 1.0 - fmin(fmax((orig_len * f / kTwoPi - low) / (high - low), 0.0), 1.0);
+    freq[j] = f / factor * slow + f * (1.0 - slow);
+  }
+  if (amplitude) *amplitude = ramp ? (float)(0.1 * log(factor) + 1.0) : 1.0f;
+  return SMALLKV_OK;
+}
+
+int smallkv_append(const smallkv_chunk_t *chunk, const smallkv_cache_t *cache, const smallkv_append_t *append,
+                   void *stream) {
+  const int rc = check_append(chunk, cache, append);
+  if (rc) return rc;
+  return status_of(launch_append(*chunk, *cache, *append, static_cast<hipStream_t>(stream)));
+}
+
+int smallkv_chunk_attn_workspace_size(const smallkv_chunk_t *chunk, const smallkv_cache_t *cache,
+                                      const smallkv_queries_t *queries, size_t *bytes) {
+  if (!bytes) return SMALLKV_EINVAL;
+  const int rc = check_attn(chunk, cache, queries);
+  if (rc) return rc;
+  *bytes = plan_chunk_attn(*chunk, *cache, *queries).ws_bytes;
+  return SMALLKV_OK;
+}
+
+int smallkv_chunk_attn(const smallkv_chunk_t *chunk, const smallkv_cache_t *cache,
+                       const smallkv_queries_t *queries, void *ws, size_t ws_bytes, void *stream) {
+  const int rc = check_attn(chunk, cache, queries);
+  if (rc) return rc;
+  const AttnPlan p = plan_chunk_attn(*chunk, *cache, *queries);
+  if (p.ws_bytes && (!ws || ws_bytes < p.ws_bytes)) return SMALLKV_EWORKSPACE;
+  if (p.ws_bytes && !aligned16(ws)) return SMALLKV_EINVAL;
+  return status_of(launch_chunk_attn(*chunk, *cache, *queries, p, ws, static_cast<hipStream_t>(stream)));
+}
+
+int smallkv_chunk_scores(const smallkv_chunk_t *chunk, const smallkv_cache_t *cache,
+                         const smallkv_queries_t *queries, int32_t n_score_heads, const float *before,
+                         float *out, int64_t score_rows, void *stream) {
+  const int rc = check_queries(chunk, cache, queries);
+  if (rc) return rc;
+  if (!queries->lse || !out || score_rows < chunk->max_len) return SMALLKV_EINVAL;
+  if (n_score_heads != queries->n_heads && n_score_heads != cache->n_heads) return SMALLKV_EINVAL;
+  if (((int64_t)chunk->max_len + 127) / 128 * chunk->batch * cache->n_heads > (1 << 30) ||
+      queries->n_heads / cache->n_heads > 65535)
+    return SMALLKV_EUNSUPPORTED;
+  return status_of(launch_chunk_scores(*chunk, *cache, *queries, n_score_heads, before, out, score_rows,
+                                       static_cast<hipStream_t>(stream)));
+}
+
+int smallkv_evict_workspace_size(const smallkv_evict_t *evict, size_t *bytes) {
+  if (!bytes) return SMALLKV_EINVAL;
+  const int rc = check_evict(evict);
+  if (rc) return rc;
+  *bytes = evict_workspace(*evict);
+  return SMALLKV_OK;
+}
+
+int smallkv_evict(const smallkv_evict_t *evict, void *ws, size_t ws_bytes, void *stream) {
+  const int rc = check_evict(evict);
+  if (rc) return rc;
+  if (!ws || ws_bytes < evict_workspace(*evict)) return SMALLKV_EWORKSPACE;
+  if (!aligned16(ws)) return SMALLKV_EINVAL;
+  return status_of(launch_evict(*evict, ws, static_cast<hipStream_t>(stream)));
 }
 
 int smallkv_step(const smallkv_step_t *s, void *ws, size_t ws_bytes, void *stream) {

@@ -129,4 +129,27 @@ hipError_t launch_hybrid(const smallkv_batch_t &b, const smallkv_model_t &m,
                          const int32_t *marg, const float *marg_prob, const float *mass,
                          int mode, bool group_sel, int layer0, int nl, hipStream_t st);
 
+// Cache operators.  Waves (of 32 rows) of the attention's many-rows form.
+constexpr int kAttnWaves = 4;
+
+// Plan of smallkv_chunk_attn: which forms run, their tiles of rows (bounds over
+// the batch), the spans the cached rows are cut into, and the records' bytes.
+struct AttnPlan {
+  int use_few;
+  int few_tiles, few_span, few_split;
+  int many_tiles, many_span, many_split;
+  size_t many_bytes, ws_bytes;
+};
+AttnPlan plan_chunk_attn(const smallkv_chunk_t &c, const smallkv_cache_t &kv,
+                         const smallkv_queries_t &q);
+hipError_t launch_chunk_attn(const smallkv_chunk_t &c, const smallkv_cache_t &kv,
+                             const smallkv_queries_t &q, const AttnPlan &p, void *ws, hipStream_t st);
+hipError_t launch_chunk_scores(const smallkv_chunk_t &c, const smallkv_cache_t &kv,
+                               const smallkv_queries_t &q, int n_score_heads, const float *before,
+                               float *out, int64_t score_rows, hipStream_t st);
+hipError_t launch_append(const smallkv_chunk_t &c, const smallkv_cache_t &kv,
+                         const smallkv_append_t &a, hipStream_t st);
+size_t evict_workspace(const smallkv_evict_t &e);
+hipError_t launch_evict(const smallkv_evict_t &e, void *ws, hipStream_t st);
+
 }  // namespace smallkv

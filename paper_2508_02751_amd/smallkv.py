@@ -7,8 +7,9 @@ is no fallback: if the library is not built, or a call fails, this module
 raises.
 
 Entry points mirror the C names: smallkv_small_attn, smallkv_partition,
-smallkv_hybrid_attn, smallkv_step, smallkv_workspace_size, and the prefill
-matching smallkv_match, smallkv_match_workspace_size.
+smallkv_hybrid_attn, smallkv_step, smallkv_workspace_size, the prefill
+matching smallkv_match, smallkv_match_workspace_size, and the cache operators
+(prepare_append, prepare_chunk_attn, prepare_chunk_scores, prepare_evict).
 """
 from __future__ import annotations
 
@@ -74,13 +75,55 @@ class Store(C.Structure):
                 ("v_slot", C.c_void_p), ("counts", C.c_void_p)]
 
 
+class Cache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("dtype", C.c_int32),
+                ("head_dim", C.c_int32), ("n_heads", C.c_int32), ("page_rows", C.c_int32),
+                ("n_pages", C.c_int32), ("table_width", C.c_int32), ("page_stride", C.c_int64),
+                ("head_stride", C.c_int64), ("row_stride", C.c_int64), ("page_table", C.c_void_p)]
+
+
+class Chunk(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("n_tokens", C.c_int32), ("max_new", C.c_int32),
+                ("max_len", C.c_int32), ("start", C.c_void_p), ("len", C.c_void_p)]
+
+
+class Queries(C.Structure):
+    _fields_ = [("n_heads", C.c_int32), ("scale", C.c_float), ("q", C.c_void_p),
+                ("token_stride", C.c_int64), ("head_stride", C.c_int64), ("out", C.c_void_p),
+                ("out_token_stride", C.c_int64), ("out_head_stride", C.c_int64),
+                ("lse", C.c_void_p)]
+
+
+class Append(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p),
+                ("q_token_stride", C.c_int64), ("q_head_stride", C.c_int64),
+                ("k_token_stride", C.c_int64), ("k_head_stride", C.c_int64),
+                ("v_token_stride", C.c_int64), ("v_head_stride", C.c_int64),
+                ("n_q_heads", C.c_int32), ("q_out", C.c_void_p),
+                ("q_out_token_stride", C.c_int64), ("q_out_head_stride", C.c_int64),
+                ("positions", C.c_void_p), ("freq", C.c_void_p), ("rot_dim", C.c_int32),
+                ("layout", C.c_int32), ("amplitude", C.c_float), ("row_pos", C.c_void_p),
+                ("pos_rows", C.c_int32)]
+
+
+class Evict(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("max_len", C.c_int32), ("len", C.c_void_p),
+                ("keep", C.c_void_p), ("recent", C.c_void_p), ("sinks", C.c_int32),
+                ("from_", Cache), ("to", Cache), ("n_score_heads", C.c_int32),
+                ("scores", C.c_void_p), ("score_rows", C.c_int64), ("row_pos", C.c_void_p),
+                ("pos_rows", C.c_int64), ("out_rows", C.c_int64), ("out_scores", C.c_void_p),
+                ("out_pos", C.c_void_p), ("held", C.c_void_p)]
+
+
 EXPORTS = ("smallkv_small_attn", "smallkv_partition", "smallkv_hybrid_attn", "smallkv_step",
            "smallkv_step_noalloc", "smallkv_step_events", "smallkv_hybrid_attn_layers",
            "smallkv_hybrid_attn_workspace_size", "smallkv_workspace_size", "smallkv_match", "smallkv_match_workspace_size",
            "smallkv_group_select", "smallkv_group_select_workspace_size",
            "smallkv_accum_select", "smallkv_accum_select_workspace_size",
            "smallkv_store_update", "smallkv_store_workspace_size",
-           "smallkv_status_string", "smallkv_abi_version")
+           "smallkv_append", "smallkv_rope_freqs", "smallkv_chunk_attn",
+           "smallkv_chunk_attn_workspace_size", "smallkv_chunk_scores", "smallkv_evict",
+           "smallkv_evict_workspace_size", "smallkv_status_string", "smallkv_abi_version")
 
 _lib = None
 
@@ -127,6 +170,17 @@ def lib():
         L.smallkv_workspace_size.argtypes = [P(Step), P(C.c_size_t)]
         L.smallkv_match.argtypes = [P(Match), C.c_void_p, C.c_size_t, C.c_void_p]
         L.smallkv_match_workspace_size.argtypes = [P(Match), P(C.c_size_t)]
+        L.smallkv_append.argtypes = [P(Chunk), P(Cache), P(Append), C.c_void_p]
+        L.smallkv_rope_freqs.argtypes = [C.c_int32, C.c_double, C.c_int32, C.c_double, C.c_double,
+                                         C.c_double, C.c_int32, P(C.c_double), P(C.c_float)]
+        L.smallkv_chunk_attn.argtypes = [P(Chunk), P(Cache), P(Queries), C.c_void_p, C.c_size_t,
+                                         C.c_void_p]
+        L.smallkv_chunk_attn_workspace_size.argtypes = [P(Chunk), P(Cache), P(Queries),
+                                                        P(C.c_size_t)]
+        L.smallkv_chunk_scores.argtypes = [P(Chunk), P(Cache), P(Queries), C.c_int32, C.c_void_p,
+                                           C.c_void_p, C.c_int64, C.c_void_p]
+        L.smallkv_evict.argtypes = [P(Evict), C.c_void_p, C.c_size_t, C.c_void_p]
+        L.smallkv_evict_workspace_size.argtypes = [P(Evict), P(C.c_size_t)]
         L.smallkv_status_string.argtypes = [C.c_int]
         L.smallkv_status_string.restype = C.c_char_p
         L.smallkv_abi_version.argtypes = []
@@ -137,7 +191,9 @@ def lib():
                   "smallkv_match", "smallkv_match_workspace_size", "smallkv_group_select",
                   "smallkv_group_select_workspace_size", "smallkv_accum_select",
                   "smallkv_accum_select_workspace_size", "smallkv_store_update",
-                  "smallkv_store_workspace_size"):
+                  "smallkv_store_workspace_size", "smallkv_append", "smallkv_rope_freqs",
+                  "smallkv_chunk_attn", "smallkv_chunk_attn_workspace_size",
+                  "smallkv_chunk_scores", "smallkv_evict", "smallkv_evict_workspace_size"):
             getattr(L, f).restype = C.c_int
         _lib = L
     return _lib
@@ -500,3 +556,307 @@ def smallkv_store_update(desc: Store, ws, stream=None):
     w, wb = _ws(ws)
     _check("smallkv_store_update", lib().smallkv_store_update(C.byref(desc), w, wb,
                                                               _stream(stream)))
+
+
+# -------------------------------------------------------- cache operators --
+
+ROPE_HALF, ROPE_INTERLEAVED = 0, 1
+ROPE_PLAIN, ROPE_LINEAR, ROPE_BASE, ROPE_RAMP, ROPE_BANDS = range(5)
+
+
+def rope_freqs(rot_dim: int, base: float, scaling: int = ROPE_PLAIN, factor: float = 1.0,
+               low: float = 1.0, high: float = 32.0, orig_len: int = 0, device="cuda"):
+    """(frequencies [rot_dim / 2] float64 on `device`, amplitude) for a RopeSpec."""
+    buf = (C.c_double * max(rot_dim // 2, 1))()
+    amp = C.c_float()
+    _check("smallkv_rope_freqs", lib().smallkv_rope_freqs(
+        int(rot_dim), float(base), int(scaling), float(factor), float(low), float(high),
+        int(orig_len), buf, C.byref(amp)))
+    return torch.tensor(list(buf), dtype=torch.float64, device=device), amp.value
+
+
+def _on_gpu(*tensors) -> torch.device:
+    """The one GPU that all the tensors (None entries aside) are on."""
+    dev = None
+    for t in tensors:
+        if t is None:
+            continue
+        if dev is not None and t.device != dev:
+            raise ValueError(f"tensors on different devices: {dev} and {t.device}")
+        dev = t.device
+    if dev is None or dev.type != "cuda":
+        raise ValueError("tensors passed to libsmallkv must be on a GPU")
+    return dev
+
+
+def _need(t: Optional[torch.Tensor], dtype, shape, what: str, optional=False):
+    if t is None and optional:
+        return
+    if t is None or t.dtype != dtype or tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{what} must be {dtype} {tuple(shape)}")
+    if not t.is_contiguous():
+        raise ValueError(f"{what} must be contiguous")
+
+
+def _strides(t: torch.Tensor, what: str):
+    """Strides of the leading dimensions (0 where the extent is 1); rows contiguous."""
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{what}: the last dimension must be contiguous")
+    return tuple(0 if n <= 1 else s for n, s in zip(t.shape[:-1], t.stride()[:-1]))
+
+
+@dataclasses.dataclass
+class CacheSpec:
+    """One layer's keys and values, 4-d views [pages][Hkv][rows per page][d] of any
+    strides with contiguous rows (k and v alike): page_table int32 [B][width], or
+    None for a dense cache (sequence b is page b), such as k[:, layer] of a
+    [B][L][Hkv][n_cap][d] tensor."""
+    k: torch.Tensor
+    v: torch.Tensor
+    page_table: Optional[torch.Tensor] = None
+
+    def c(self, batch: Optional[int] = None) -> Cache:
+        k, v, t = self.k, self.v, self.page_table
+        if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype:
+            raise ValueError("cache k and v must be 4-d tensors of one shape and dtype")
+        st = _strides(k, "cache k")
+        if st != _strides(v, "cache v"):
+            raise ValueError("cache k and v must have the same strides")
+        if t is not None:
+            if t.dim() != 2 or (batch is not None and t.shape[0] != batch):
+                raise ValueError("page_table must be [B][pages per sequence]")
+            _need(t, torch.int32, t.shape, "page_table")
+        elif batch is not None and k.shape[0] < batch:
+            raise ValueError("a dense cache has a page per sequence")
+        return Cache(k.data_ptr(), v.data_ptr(), _dtype_code(k), k.shape[3], k.shape[1],
+                     k.shape[2], k.shape[0], t.shape[1] if t is not None else 0, *st,
+                     t.data_ptr() if t is not None else None)
+
+    @property
+    def capacity(self) -> int:
+        """Rows a sequence can have."""
+        return self.k.shape[2] * (self.page_table.shape[1] if self.page_table is not None else 1)
+
+
+@dataclasses.dataclass
+class ChunkSpec:
+    """The new tokens of a batch: start int32 [B+1] (packed token ranges), length
+    int32 [B] (cached rows, the new ones included); n_tokens packed tokens, no
+    sequence with more than max_new new tokens or max_len rows."""
+    start: torch.Tensor
+    length: torch.Tensor
+    n_tokens: int
+    max_new: int
+    max_len: int
+
+    def c(self) -> Chunk:
+        if self.length.dim() != 1:
+            raise ValueError("length must be int32 [B]")
+        B = self.length.numel()
+        _need(self.length, torch.int32, (B,), "length")
+        _need(self.start, torch.int32, (B + 1,), "start")
+        return Chunk(B, int(self.n_tokens), int(self.max_new), int(self.max_len),
+                     self.start.data_ptr(), self.length.data_ptr())
+
+
+@dataclasses.dataclass
+class RopeSpec:
+    """Rotary positions: freq float64 [rot_dim / 2] (see rope_freqs), the pairs'
+    layout, and the factor on the turned elements."""
+    freq: torch.Tensor
+    layout: int = ROPE_HALF
+    amplitude: float = 1.0
+
+
+def _rows(t: torch.Tensor, n_tokens: int, heads: Optional[int], like: torch.Tensor, what: str):
+    """(token stride, head stride) of packed rows [T][heads][d]."""
+    if t.dim() != 3 or t.shape[0] != n_tokens or t.shape[2] != like.shape[3] or \
+            t.dtype != like.dtype or (heads is not None and t.shape[1] != heads):
+        raise ValueError(f"{what} must be [n_tokens][heads][head_dim] in the cache's dtype")
+    return _strides(t, what)
+
+
+class _Call:
+    """A prepared call: the descriptors hold raw pointers, `keep` the tensors."""
+
+    def _start(self, dev, keep):
+        self._dev, self._keep = dev, keep
+
+    def _run(self, fn, stream, *args):
+        # on the tensors' device, on its current stream unless one is given
+        if torch.cuda.current_device() == self._dev.index:
+            _check(fn, getattr(lib(), fn)(*args, _stream(stream)))
+        else:
+            with torch.cuda.device(self._dev):
+                _check(fn, getattr(lib(), fn)(*args, _stream(stream)))
+
+
+class AppendCall(_Call):
+    """smallkv_append: q_out = turned q, the cache's new rows = turned k, and v."""
+
+    def __init__(self, chunk, cache, rope, q, k, v, positions, q_out, row_pos):
+        ch, ca = chunk.c(), cache.c(chunk.length.numel())
+        T, like = chunk.n_tokens, cache.k
+        if q_out is None:
+            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        qs, os = _rows(q, T, None, like, "q"), _rows(q_out, T, q.shape[1], like, "q_out")
+        ks, vs = _rows(k, T, ca.n_heads, like, "k"), _rows(v, T, ca.n_heads, like, "v")
+        _need(rope.freq, torch.float64, (rope.freq.numel(),), "freq")
+        _need(positions, torch.int32, (T,), "positions", optional=True)
+        if row_pos is not None:
+            if row_pos.dim() != 3:
+                raise ValueError("row_pos must be [B][Hkv][rows]")
+            _need(row_pos, torch.int32, (ch.batch, ca.n_heads, row_pos.shape[2]), "row_pos")
+        dev = _on_gpu(q, k, v, q_out, positions, row_pos, rope.freq, cache.k, cache.v,
+                      cache.page_table, chunk.start, chunk.length)
+        self.q_out = q_out
+        self.desc = Append(q.data_ptr(), k.data_ptr(), v.data_ptr(), *qs, *ks, *vs, q.shape[1],
+                           q_out.data_ptr(), *os, _ptr(positions), _ptr(rope.freq),
+                           2 * rope.freq.numel(), int(rope.layout), float(rope.amplitude),
+                           _ptr(row_pos), row_pos.shape[2] if row_pos is not None else 0)
+        self._c = (ch, ca)
+        self._start(dev, (chunk, cache, rope, q, k, v, positions, row_pos))
+
+    def run(self, stream=None):
+        self._run("smallkv_append", stream, C.byref(self._c[0]), C.byref(self._c[1]),
+                  C.byref(self.desc))
+
+
+def prepare_append(chunk: ChunkSpec, cache: CacheSpec, rope: RopeSpec, q, k, v, positions=None,
+                   q_out=None, row_pos=None) -> AppendCall:
+    """The new tokens' q [T][Hq][d], k and v [T][Hkv][d] (views of a fused projection
+    will do): q turned into q_out (allocated if None, q itself will do), k turned
+    and v written to the cache.  positions int32 [T] (None: the tokens' cached
+    rows); row_pos int32 [B][Hkv][rows]: receives the appended rows' positions."""
+    return AppendCall(chunk, cache, rope, q, k, v, positions, q_out, row_pos)
+
+
+class ChunkAttnCall(_Call):
+    """smallkv_chunk_attn: out [T][Hq][d] and lse [T][Hq]."""
+
+    def __init__(self, chunk, cache, q, scale, out, lse, ws):
+        ch, ca = chunk.c(), cache.c(chunk.length.numel())
+        T = chunk.n_tokens
+        qs = _rows(q, T, None, cache.k, "q")
+        hq = q.shape[1]
+        if out is None:
+            out = torch.empty((T, hq, q.shape[2]), dtype=q.dtype, device=q.device)
+        os = _rows(out, T, hq, cache.k, "out")
+        if lse is True:
+            lse = torch.empty((T, hq), dtype=torch.float32, device=q.device)
+        lse = lse if lse is not False else None
+        _need(lse, torch.float32, (T, hq), "lse", optional=True)
+        dev = _on_gpu(q, out, lse, ws, cache.k, cache.v, cache.page_table, chunk.start,
+                      chunk.length)
+        self.out, self.lse = out, lse
+        self.desc = Queries(hq, float(scale), q.data_ptr(), *qs, out.data_ptr(), *os, _ptr(lse))
+        n = C.c_size_t()
+        _check("smallkv_chunk_attn_workspace_size", lib().smallkv_chunk_attn_workspace_size(
+            C.byref(ch), C.byref(ca), C.byref(self.desc), C.byref(n)))
+        self.ws = ws if ws is not None else torch.empty(n.value, dtype=torch.uint8, device=dev)
+        self._c = (ch, ca)
+        self._start(dev, (chunk, cache, q))
+
+    def run(self, stream=None):
+        w, wb = _ws(self.ws)
+        self._run("smallkv_chunk_attn", stream, C.byref(self._c[0]), C.byref(self._c[1]),
+                  C.byref(self.desc), w, wb)
+
+
+def prepare_chunk_attn(chunk: ChunkSpec, cache: CacheSpec, q, scale: float, out=None, lse=True,
+                       ws=None) -> ChunkAttnCall:
+    """Attention of the new tokens' q [T][Hq][d] over the cache.  out: allocated if
+    None; lse: True (allocated), a float32 [T][Hq] tensor, or False."""
+    return ChunkAttnCall(chunk, cache, q, scale, out, lse, ws)
+
+
+class ChunkScoresCall(_Call):
+    """smallkv_chunk_scores: out [B][Hq or Hkv][rows]."""
+
+    def __init__(self, chunk, cache, q, lse, scale, out, before):
+        ch, ca = chunk.c(), cache.c(chunk.length.numel())
+        T = chunk.n_tokens
+        qs = _rows(q, T, None, cache.k, "q")
+        _need(lse, torch.float32, (T, q.shape[1]), "lse")
+        if out.dim() != 3:
+            raise ValueError("scores must be [B][Hq or Hkv][rows]")
+        _need(out, torch.float32, (ch.batch, out.shape[1], out.shape[2]), "out")
+        _need(before, torch.float32, out.shape, "before", optional=True)
+        dev = _on_gpu(q, lse, out, before, cache.k, cache.v, cache.page_table, chunk.start,
+                      chunk.length)
+        self.out = out
+        self.desc = Queries(q.shape[1], float(scale), q.data_ptr(), *qs, None, 0, 0, _ptr(lse))
+        self._c = (ch, ca)
+        self._args = (out.shape[1], _ptr(before), _ptr(out), out.shape[2])
+        self._start(dev, (chunk, cache, q, lse, out, before))
+
+    def run(self, stream=None):
+        self._run("smallkv_chunk_scores", stream, C.byref(self._c[0]), C.byref(self._c[1]),
+                  C.byref(self.desc), *self._args)
+
+
+def prepare_chunk_scores(chunk: ChunkSpec, cache: CacheSpec, q, lse, scale: float, out,
+                         before=None) -> ChunkScoresCall:
+    """The attention weight of the new tokens per cached row (lse: of
+    prepare_chunk_attn), added to `before` (None: 0; `out` itself will do) into
+    out float32 [B][Hq or Hkv][rows]."""
+    return ChunkScoresCall(chunk, cache, q, lse, scale, out, before)
+
+
+class EvictCall(_Call):
+    """smallkv_evict: the cache `to`, out_pos, out_scores and held."""
+
+    def __init__(self, cache, to, length, keep, scores, recent, sinks, row_pos, out_pos,
+                 out_scores, held, max_len):
+        if length.dim() != 1:
+            raise ValueError("length must be int32 [B]")
+        B = length.numel()
+        ca, ct = cache.c(B), to.c(B)
+        H = ca.n_heads
+        for t, what in ((length, "length"), (keep, "keep"), (recent, "recent"), (held, "held")):
+            _need(t, torch.int32, (B,), what, optional=what in ("recent", "held"))
+        if scores.dim() != 3 or scores.shape[1] % H:
+            raise ValueError("scores must be [B][a multiple of the kv heads][rows]")
+        _need(scores, torch.float32, (B, *scores.shape[1:]), "scores")
+        if row_pos is not None:
+            if row_pos.dim() != 3:
+                raise ValueError("row_pos must be [B][Hkv][rows]")
+            _need(row_pos, torch.int32, (B, H, row_pos.shape[2]), "row_pos")
+        rows = to.capacity if out_pos is None else out_pos.shape[-1]
+        dev = _on_gpu(length, keep, recent, scores, row_pos, out_pos, out_scores, held, cache.k,
+                      cache.v, cache.page_table, to.k, to.v, to.page_table)
+        if out_pos is None:
+            out_pos = torch.zeros((B, H, rows), dtype=torch.int32, device=dev)
+        _need(out_pos, torch.int32, (B, H, rows), "out_pos")
+        _need(out_scores, torch.float32, (B, scores.shape[1], rows), "out_scores", optional=True)
+        if held is None:
+            held = torch.zeros(B, dtype=torch.int32, device=dev)
+        if max_len is None:
+            max_len = min(cache.capacity, scores.shape[2],
+                          row_pos.shape[2] if row_pos is not None else 1 << 30)
+        self.out_pos, self.out_scores, self.held = out_pos, out_scores, held
+        self.desc = Evict(B, int(max_len), _ptr(length), _ptr(keep), _ptr(recent), int(sinks), ca,
+                          ct, scores.shape[1], _ptr(scores), scores.shape[2], _ptr(row_pos),
+                          row_pos.shape[2] if row_pos is not None else 0, rows, _ptr(out_scores),
+                          _ptr(out_pos), _ptr(held))
+        n = C.c_size_t()
+        _check("smallkv_evict_workspace_size", lib().smallkv_evict_workspace_size(
+            C.byref(self.desc), C.byref(n)))
+        self.ws = torch.empty(n.value, dtype=torch.uint8, device=dev)
+        self._start(dev, (cache, to, length, keep, recent, scores, row_pos))
+
+    def run(self, stream=None):
+        w, wb = _ws(self.ws)
+        self._run("smallkv_evict", stream, C.byref(self.desc), w, wb)
+
+
+def prepare_evict(cache: CacheSpec, to: CacheSpec, length, keep, scores, recent=None,
+                  sinks: int = 0, row_pos=None, out_pos=None, out_scores=None, held=None,
+                  max_len: Optional[int] = None) -> EvictCall:
+    """Keep the keep[b] rows of largest score (scores float32 [B][m * Hkv][rows], the
+    sum over a kv head's m) of each sequence's length[b], the first `sinks` and the
+    last recent[b] among them, moved to the cache `to`.  row_pos int32
+    [B][Hkv][rows]: the rows' positions (None: the rows).  out_pos, held: allocated
+    if None; out_scores float32 [B][m * Hkv][rows of out_pos] or None."""
+    return EvictCall(cache, to, length, keep, scores, recent, sinks, row_pos, out_pos, out_scores,
+                     held, max_len)
