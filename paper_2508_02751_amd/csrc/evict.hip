@@ -1,11 +1,13 @@
 // Eviction from a cache by accumulated attention weight.
 //
 //   evict_select -- one workgroup per (sequence, kv head): the rows' summed
-//                   scores as order-preserving 32-bit keys, the exact threshold
-//                   of the top ones by a radix descent of 8 bits a pass
-//                   (histograms in LDS), then the kept rows in ascending order,
-//                   ties to the lowest rows, with their positions and scores;
-//   evict_copy   -- the kept rows as a flat array of 16-byte pieces, K and V.
+//                   scores as order-preserving 32-bit keys, read once and kept in
+//                   registers (up to 32768 rows; longer rows are read again by
+//                   every pass), the exact threshold of the top ones by counting
+//                   passes, then the kept rows' numbers in ascending order, ties to
+//                   the lowest rows;
+//   evict_copy   -- the kept rows as a flat array of 16-byte pieces, K and V, and
+//                   their positions and scores.
 #include <algorithm>
 
 #include "cache.h"
@@ -52,141 +54,204 @@ __device__ __forceinline__ uint32_t score_key(const float *p, int64_t stride, in
   return f != f ? 0u : logit_key(f);
 }
 
-__global__ __launch_bounds__(kST) void evict_select(EvictArgs a) {
-  __shared__ uint32_t hist[kSW][256];
-  __shared__ uint32_t total[256];
-  __shared__ uint32_t pick[2];  // the digit, and how many are still wanted within it
-  __shared__ int cnt[2][kSW];
+// Threads of evict_select hold KPT keys each, wave by wave in runs of rows: key j
+// of a lane is row (wave * KPT + j) * 64 + lane.  KPT 0: the rows are read anew.
+template <int KPT> struct Keys {
+  uint32_t k[KPT];
+  __device__ __forceinline__ void load(const EvictArgs &a, const float *f, int r0, int lo, int hi) {
+    const int lane = threadIdx.x & (kWave - 1);
+    float s[KPT];
+#pragma unroll
+    for (int j = 0; j < KPT; ++j) {
+      const int row = min(r0 + j * kWave + lane, max(hi - 1, 0));
+      s[j] = f[row];
+    }
+    for (int i = 1; i < a.gs; ++i)
+#pragma unroll
+      for (int j = 0; j < KPT; ++j) s[j] += f[i * a.score_rows + min(r0 + j * kWave + lane, max(hi - 1, 0))];
+#pragma unroll
+    for (int j = 0; j < KPT; ++j) k[j] = s[j] != s[j] ? 0u : logit_key(s[j]);
+  }
+  template <typename F> __device__ __forceinline__ void each(const EvictArgs &, const float *, int r0, int, F &&use) const {
+#pragma unroll
+    for (int j = 0; j < KPT; ++j) use(r0 + j * kWave + (int)(threadIdx.x & (kWave - 1)), k[j]);
+  }
+};
+template <> struct Keys<0> {
+  __device__ __forceinline__ void load(const EvictArgs &, const float *, int, int, int) {}
+  template <typename F>
+  __device__ __forceinline__ void each(const EvictArgs &a, const float *f, int r0, int r1, F &&use) const {
+    for (int r = r0; r < r1; r += kWave) {
+      const int row = r + (int)(threadIdx.x & (kWave - 1));
+      use(row, score_key(f + min(row, r1 - 1), a.score_rows, a.gs));
+    }
+  }
+};
+
+// The threshold of the `top` largest keys of rows lo..hi-1, by counting: the
+// range between the smallest and the largest key is cut into kBins equal bins
+// (keys of floats are spread about evenly in it, where the bits of one digit are
+// not: scores share their leading bits, and the counters of a few bins would be
+// hit by all lanes at once), the bin that holds the threshold becomes the next
+// range, and the descent ends when its keys are equal or all wanted: two or three
+// passes instead of four by 8-bit digits.
+constexpr int kBins = 2 * kST;
+
+template <int KPT>
+__global__ __launch_bounds__(kST, KPT <= 8 ? 8 : 4) void evict_select(EvictArgs a) {
+  __shared__ uint32_t hist[kBins];
+  __shared__ uint32_t part[2][kSW];
+  __shared__ uint32_t pick[3];  // the bin, how many of it are wanted, and its count
   const int lane = threadIdx.x & (kWave - 1);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  const int unit = blockIdx.x, b = unit / a.heads, h = unit % a.heads;
+  const int unit = blockIdx.x, b = unit / a.heads;
   const Budget x = budget(a, b);
-  if (h == 0 && threadIdx.x == 0) a.held[b] = x.kept;
-  const float *f = a.scores + ((int64_t)b * a.heads + h) * a.gs * a.score_rows;
+  if (unit % a.heads == 0 && threadIdx.x == 0) a.held[b] = x.kept;
+  if (x.kept == 0) return;
+  const float *f = a.scores + (int64_t)unit * a.gs * a.score_rows;
   const int lo = x.first, hi = x.n - x.last;  // ranked rows
-  const uint32_t top = x.kept - x.last - x.first;
-  uint32_t prefix = 0, want = top;
-  if (top > 0 && top < (uint32_t)(hi - lo)) {
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      for (int i = threadIdx.x; i < kSW * 256; i += kST) hist[i / 256][i % 256] = 0;
-      __syncthreads();
-      for (int r = lo + threadIdx.x; r < hi; r += kST) {
-        const uint32_t k = score_key(f + r, a.score_rows, a.gs);
-        if (shift == 24 || (k >> (shift + 8)) == prefix) atomicAdd(&hist[wave][k >> shift & 255u], 1u);
-      }
-      __syncthreads();
-      if (threadIdx.x < 256) {
-        uint32_t t = 0;
-        for (int w = 0; w < kSW; ++w) t += hist[w][threadIdx.x];
-        total[threadIdx.x] = t;
-      }
-      __syncthreads();
-      if (wave == 0) {
-        // bins from the top: lane l holds bins 255-4l .. 252-4l
-        uint32_t v[4], sum = 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) sum += v[i] = total[255 - 4 * lane - i];
-        uint32_t s = sum;
-#pragma unroll
-        for (int o = 1; o < kWave; o <<= 1) {
-          const uint32_t y = __shfl_up(s, o, kWave);
-          if (lane >= o) s += y;
-        }
-        uint32_t above = s - sum;
-        if (above < want && s >= want) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            if (above < want && above + v[i] >= want) {
-              pick[0] = 255 - 4 * lane - i;
-              pick[1] = want - above;
-            }
-            above += v[i];
-          }
-        }
-      }
-      __syncthreads();
-      prefix = prefix << 8 | pick[0];
-      want = pick[1];
-      __syncthreads();
-    }
-  } else {
-    prefix = top ? 0u : 0xffffffffu;  // every ranked row, or none (no key is all ones)
-    want = top;
-  }
-  // each wave walks its own run of rows; how many the runs before it keep
-  const int per = ((x.n + kSW - 1) / kSW + kWave - 1) / kWave * kWave;
+  const int per = KPT ? KPT * kWave : ((x.n + kSW - 1) / kSW + kWave - 1) / kWave * kWave;
   const int r0 = min(wave * per, x.n), r1 = min(r0 + per, x.n);
-  int sure = 0, ties = 0;
-  for (int r = r0; r < r1; r += kWave) {
-    const int row = r + lane;
-    bool yes = false, tie = false;
-    if (row < r1) {
-      yes = row < lo || row >= hi;
-      if (!yes) {
-        const uint32_t k = score_key(f + row, a.score_rows, a.gs);
-        yes = k > prefix;
-        tie = k == prefix;
+  Keys<KPT> keys;
+  keys.load(a, f, r0, lo, x.n);
+  const uint32_t top = x.kept - x.last - x.first;
+  uint32_t want = top, low = 0u, high = 0xffffffffu;  // the threshold is in [low, high]
+  if (top > 0 && top < (uint32_t)(hi - lo)) {
+    uint32_t mn = 0xffffffffu, mx = 0u;
+    keys.each(a, f, r0, r1, [&](int row, uint32_t k) {
+      if (row >= lo && row < hi) {
+        mn = min(mn, k);
+        mx = max(mx, k);
+      }
+    });
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+      mn = min(mn, (uint32_t)__shfl_xor((int)mn, o, kWave));
+      mx = max(mx, (uint32_t)__shfl_xor((int)mx, o, kWave));
+    }
+    if (lane == 0) {
+      part[0][wave] = mn;
+      part[1][wave] = mx;
+    }
+    hist[threadIdx.x] = 0u;
+    hist[threadIdx.x + kST] = 0u;
+    __syncthreads();
+    for (int w = 0; w < kSW; ++w) {
+      mn = min(mn, part[0][w]);
+      mx = max(mx, part[1][w]);
+    }
+    low = mn;
+    high = mx;
+    while (low < high) {
+      // bins of 2^shift keys, bin 0 the highest keys
+      const int bits = 32 - __clz(high - low), shift = max(bits - 11, 0);  // (kBins = 2^11)
+      keys.each(a, f, r0, r1, [&](int row, uint32_t k) {
+        if (row >= lo && row < hi && k >= low && k <= high) atomicAdd(&hist[(high - k) >> shift], 1u);
+      });
+      __syncthreads();
+      const uint32_t c0 = hist[2 * threadIdx.x], c1 = hist[2 * threadIdx.x + 1];
+      uint32_t s = c0 + c1;
+#pragma unroll
+      for (int o = 1; o < kWave; o <<= 1) {
+        const uint32_t y = __shfl_up((int)s, o, kWave);
+        if (lane >= o) s += y;
+      }
+      if (lane == kWave - 1) part[0][wave] = s;
+      __syncthreads();
+      uint32_t above = s - c0 - c1;
+      for (int w = 0; w < wave; ++w) above += part[0][w];
+      if (above < want && above + c0 >= want) {
+        pick[0] = 2 * threadIdx.x;
+        pick[1] = want - above;
+        pick[2] = c0;
+      } else if (above + c0 < want && above + c0 + c1 >= want) {
+        pick[0] = 2 * threadIdx.x + 1;
+        pick[1] = want - above - c0;
+        pick[2] = c1;
+      }
+      hist[2 * threadIdx.x] = 0u;
+      hist[2 * threadIdx.x + 1] = 0u;
+      __syncthreads();
+      const uint32_t from = pick[0] << shift;
+      want = pick[1];
+      const uint32_t floor = high - from < (1u << shift) - 1 ? low : high - from - ((1u << shift) - 1);
+      high -= from;
+      low = max(low, floor);
+      if (want == pick[2]) {  // the whole bin is kept: its lowest key is a threshold
+        high = low;
+        want = 0xffffffffu;
       }
     }
-    sure += __popcll(__ballot(yes));
-    ties += __popcll(__ballot(tie));
+  } else if (top == 0) {
+    low = 0xffffffffu;  // none (no key is all ones)
   }
+  // the ranked rows above `low`, and the first `want` of those equal to it (with a
+  // whole bin or all rows kept: all of them)
+  if (top > 0 && top == (uint32_t)(hi - lo)) want = 0xffffffffu;
+  uint32_t sure = 0, ties = 0;
+  keys.each(a, f, r0, r1, [&](int row, uint32_t k) {
+    const bool in = row < r1, fixed = row < lo || row >= hi;
+    sure += __popcll(__ballot(in && (fixed || k > low)));
+    ties += __popcll(__ballot(in && !fixed && k == low));
+  });
+  __syncthreads();  // (the smallest and largest keys have been read)
   if (lane == 0) {
-    cnt[0][wave] = sure;
-    cnt[1][wave] = ties;
+    part[0][wave] = sure;
+    part[1][wave] = ties;
   }
   __syncthreads();
-  int at = 0, before = 0;  // kept rows and ties of the runs before
+  uint32_t at = 0, before = 0;  // kept rows and ties of the runs before
   for (int w = 0; w < wave; ++w) {
-    at += cnt[0][w];
-    before += cnt[1][w];
+    at += part[0][w];
+    before += part[1][w];
   }
-  at += min(before, (int)want);
+  at += min(before, want);
   const uint64_t below = (1ull << lane) - 1;
-  for (int r = r0; r < r1; r += kWave) {
-    const int row = r + lane;
-    bool yes = false, tie = false;
-    if (row < r1) {
-      yes = row < lo || row >= hi;
-      if (!yes) {
-        const uint32_t k = score_key(f + row, a.score_rows, a.gs);
-        yes = k > prefix;
-        tie = k == prefix;
-      }
-    }
+  int32_t *src = a.src + unit * a.cap;
+  keys.each(a, f, r0, r1, [&](int row, uint32_t k) {
+    const bool in = row < r1, fixed = row < lo || row >= hi, tie = in && !fixed && k == low;
     const uint64_t mt = __ballot(tie);
-    yes |= tie && before + __popcll(mt & below) < (int)want;
+    const bool yes = in && (fixed || k > low || (tie && before + __popcll(mt & below) < want));
     const uint64_t m = __ballot(yes);
-    if (yes) {
-      const int64_t to = at + __popcll(m & below);
-      a.src[unit * a.cap + to] = row;
-      a.out_pos[unit * a.out_rows + to] = a.row_pos ? a.row_pos[unit * a.pos_rows + row] : row;
-      if (a.out_scores)
-        for (int i = 0; i < a.gs; ++i)
-          a.out_scores[((int64_t)unit * a.gs + i) * a.out_rows + to] = f[i * a.score_rows + row];
-    }
+    if (yes) src[at + __popcll(m & below)] = row;
     at += __popcll(m);
     before += __popcll(mt);
-  }
+  });
 }
 
 // blockIdx.x: (sequence, kv head); blockIdx.y: interleaved shares of the pieces;
-// blockIdx.z: K (0) or V (1).
+// blockIdx.z: K (0), V (1), or positions and scores (2).
 constexpr int kShares = 32;
 
 __global__ __launch_bounds__(kCT) void evict_copy(EvictArgs a) {
   const int unit = blockIdx.x, b = unit / a.heads, h = unit % a.heads;
   const Budget x = budget(a, b);
+  const int32_t *src = a.src + unit * a.cap;
+  if (blockIdx.z == 2) {
+    for (int r = blockIdx.y * kCT + threadIdx.x; r < x.kept; r += kShares * kCT) {
+      const int row = src[r];
+      a.out_pos[unit * a.out_rows + r] = a.row_pos ? a.row_pos[unit * a.pos_rows + row] : row;
+      if (a.out_scores)
+        for (int i = 0; i < a.gs; ++i)
+          a.out_scores[((int64_t)unit * a.gs + i) * a.out_rows + r] =
+              a.scores[((int64_t)unit * a.gs + i) * a.score_rows + row];
+    }
+    return;
+  }
   const int psh = 31 - __clz(a.row_bytes / 16);
   const int64_t items = (int64_t)x.kept << psh;
   const unsigned char *from = (blockIdx.z ? a.from.v : a.from.k) + (((uint64_t)h * a.from.head_stride) << 4);
   unsigned char *to = (blockIdx.z ? a.to_v : a.to_k) + (((uint64_t)h * a.to.head_stride) << 4);
   for (int64_t q = blockIdx.y * kCT + threadIdx.x; q < items; q += kShares * kCT) {
     const int r = (int)(q >> psh), p = (int)(q & ((1 << psh) - 1));
-    const int64_t s = row_offset(a.from, b, a.src[unit * a.cap + r]), d = row_offset(a.to, b, r);
+    const int64_t s = row_offset(a.from, b, src[r]), d = row_offset(a.to, b, r);
     if (s < 0 || d < 0) continue;
     reinterpret_cast<uint4 *>(to + d)[p] = reinterpret_cast<const uint4 *>(from + s)[p];
   }
+}
+
+template <int KPT> void launch_select(const EvictArgs &a, unsigned units, hipStream_t st) {
+  hipLaunchKernelGGL((evict_select<KPT>), dim3(units), dim3(kST), 0, st, a);
 }
 
 int64_t kept_cap(const smallkv_evict_t &e) {
@@ -226,10 +291,13 @@ hipError_t launch_evict(const smallkv_evict_t &e, void *ws, hipStream_t st) {
   a.src = static_cast<int32_t *>(ws);
   a.cap = kept_cap(e);
   const unsigned units = (unsigned)(e.batch * e.from.n_heads);
-  hipLaunchKernelGGL(evict_select, dim3(units), dim3(kST), 0, st, a);
+  // the smallest number of keys per thread that covers the longest sequence
+  const int kpt = (std::min(a.max_len, a.from.cap) + kST - 1) / kST;
+  (kpt <= 2 ? launch_select<2> : kpt <= 8 ? launch_select<8> : kpt <= 16 ? launch_select<16>
+   : kpt <= 32 ? launch_select<32> : launch_select<0>)(a, units, st);
   const hipError_t err = hipGetLastError();
   if (err != hipSuccess) return err;
-  hipLaunchKernelGGL(evict_copy, dim3(units, kShares, 2), dim3(kCT), 0, st, a);
+  hipLaunchKernelGGL(evict_copy, dim3(units, kShares, 3), dim3(kCT), 0, st, a);
   return hipGetLastError();
 }
 
