@@ -18,11 +18,13 @@
 // Two forms:
 //   many rows -- NW waves of 32 rows each share every tile of rows in LDS;
 //                tiles are double-buffered, copied from memory to LDS directly;
-//   few rows  -- sequences of at most 32 rows (a decode step's single tokens):
-//                one column of 32 rows, each wave reads its own tiles of keys
-//                and the waves' results are joined at the end.
-// Where the (tile, kv head) pairs are too few to fill the GPU the rows are cut
-// into spans, and chunk_merge joins their records.
+//   few rows  -- where no sequence has more than 32 rows (a decode step): one
+//                column of 32 rows, each wave walks its own tiles of 32 keys,
+//                without a barrier, and the waves' results are joined at the end.
+// Where the (tile, kv head) pairs are too few to fill the GPU the cached rows are
+// cut into spans, and attn_merge joins their records.  The span is found on the
+// device from the sequences' own lengths, as the shortest with which the spans of
+// all sequences still run at once: spans of equal length whatever the mixture.
 #include <algorithm>
 
 #include "cache.h"
@@ -42,97 +44,189 @@ struct AttnArgs {
   int64_t q_token, q_head, o_token, o_head;  // in elements
   float *lse;     // [n_tokens][hq] or null
   float scale2, scale2_lo;  // scale * log2(e), and what its rounding left
-  int few;        // sequences of at most 32 rows go to the few-rows form
-  int span;       // cached rows per record; one record: the output is written directly
-  int n_split;
-  float *rec;     // [split][tile * hkv][rows][D] fp32, then [split][tile * hkv][rows][2]
+  int splits;     // (tile, span) units that may run at once, per kv head; 0: no spans
+  float *rec;     // [unit * hkv][rows][D] fp32, then [unit * hkv][rows][2]
   int64_t rec_ml; // where the second array starts, in floats
+  int *span;      // the span, for attn_merge
 };
 
 constexpr double kLog2e = 1.4426950408889634074;
 constexpr float kLn2 = 0.693147180559945309417f;
 
-// The 32-row tile of a sequence or tile number `flat` over all sequences.
+// Steps of the many-rows form's spans.
+constexpr int kManyRound = 256;
+constexpr int kWhole = 1 << 30;  // a span no sequence is longer than
+
+// A tile of rows: its sequence, first row and the sequence's rows; the span's
+// number, the spans of its rows and the tile's first unit.
 struct Tile {
-  int b, row0, rows;  // sequence, first row, the sequence's rows
+  int b, row0, rows, split, n_split, unit0;
   Seq s;
 };
 
-__device__ __forceinline__ bool few_rows(const AttnArgs &a, const Seq &s) {
-  return a.few && s.n_new * a.g <= 32;
+// Inclusive sums over the wave (row_shr 1, 2, 4, 8, then across rows of 16 lanes).
+__device__ __forceinline__ int wave_scan(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
+  return x;
+}
+__device__ __forceinline__ int last_lane(int x) { return __builtin_amdgcn_readlane(x, kWave - 1); }
+
+// Spans of a sequence's rows: at least one, so that rows that see no key are written.
+__device__ __forceinline__ int spans_of(int len, int span) {
+  return span == kWhole ? 1 : max((len + span - 1) / span, 1);
 }
 
-// Tiles of BM rows are numbered sequence by sequence; within one, the last
-// rows (which see the most keys) first.
-template <int BM> __device__ __forceinline__ bool locate(const AttnArgs &a, int flat, Tile &t) {
+// The shortest span, in steps of `round` rows, with which all units fit `splits`;
+// kWhole where the tiles alone do not.  The first 64 sequences are in `n` (tiles)
+// and `len` of each lane, the others are read again.
+template <int BM> __device__ __forceinline__ int find_span(const AttnArgs &a, int round) {
+  if (!a.splits) return kWhole;
   const int lane = threadIdx.x & (kWave - 1);
+  int tiles0 = 0, len0 = 0;
+  auto each = [&](auto &&use) {
+    for (int b0 = 0; b0 < a.c.batch; b0 += kWave) {
+      int n = tiles0, len = len0;
+      if (b0 > 0) {
+        n = len = 0;
+        if (b0 + lane < a.c.batch) {
+          const Seq s = sequence(a.c, b0 + lane, a.kv.cap);
+          n = (s.n_new * a.g + BM - 1) / BM;
+          len = s.len;
+        }
+      }
+      use(n, len);
+    }
+  };
+  if (lane < a.c.batch) {
+    const Seq s = sequence(a.c, lane, a.kv.cap);
+    tiles0 = (s.n_new * a.g + BM - 1) / BM;
+    len0 = s.len;
+  }
+  int tiles = 0;
+  float work = 0.0f;  // cached rows over all tiles, in steps of `round`
+  int longest = 0;
+  each([&](int n, int len) {
+    tiles += last_lane(wave_scan(n));
+    const int steps = (len + round - 1) / round;
+    longest = max(longest, (int)wave_max(n ? (float)steps : 0.0f));
+    work += wave_sum((float)n * (float)steps);
+  });
+  if (tiles >= a.splits) return kWhole;
+  // between work / splits, and work / (splits - tiles): there they fit for sure
+  int lo = max((int)(work / (float)a.splits), 1), hi = max(min((int)(work / (float)(a.splits - tiles)) + 2, longest), lo);
+  while (lo < hi) {
+    const int mid = (lo + hi) >> 1;
+    int units = 0;
+    each([&](int n, int len) { units += last_lane(wave_scan(n * spans_of(len, mid * round))); });
+    if (units <= a.splits)
+      hi = mid;
+    else
+      lo = mid + 1;
+  }
+  return __builtin_amdgcn_readfirstlane(lo) * round;
+}
+
+// Units (or tiles) are numbered sequence by sequence, tile by tile and span by span;
+// the last rows of a sequence, which see the most keys, come first.
+template <int BM, bool UNITS> __device__ __forceinline__ bool locate(const AttnArgs &a, int span, int flat, Tile &t) {
+  const int lane = threadIdx.x & (kWave - 1);
+  int unit = 0;  // of the sequences before
   for (int b0 = 0; b0 < a.c.batch; b0 += kWave) {
-    int n = 0;
+    int n = 0, ns = 0;
     if (b0 + lane < a.c.batch) {
       const Seq s = sequence(a.c, b0 + lane, a.kv.cap);
-      if (!few_rows(a, s)) n = (s.n_new * a.g + BM - 1) / BM;
+      n = (s.n_new * a.g + BM - 1) / BM;
+      ns = spans_of(s.len, span);
     }
-    int x = n;
-#pragma unroll
-    for (int o = 1; o < kWave; o <<= 1) {
-      const int y = __shfl_up(x, o, kWave);
-      if (lane >= o) x += y;
-    }
+    const int units = wave_scan(n * ns), x = UNITS ? units : wave_scan(n);
     const uint64_t m = __ballot(x > flat);
     if (m) {
       const int l = __builtin_amdgcn_readfirstlane(__ffsll((long long)m) - 1);
+      const int tiles = __builtin_amdgcn_readlane(n, l);
       t.b = b0 + l;
-      const int tiles = __shfl(n, l, kWave), before = __shfl(x, l, kWave) - tiles;
-      t.row0 = __builtin_amdgcn_readfirstlane((tiles - 1 - (flat - before)) * BM);
+      t.n_split = __builtin_amdgcn_readlane(ns, l);
+      const int per = UNITS ? t.n_split : 1, in = flat - (__builtin_amdgcn_readlane(x, l) - tiles * per);
+      const int tile = in / per;
+      t.split = in - tile * per;
+      t.unit0 = unit + __builtin_amdgcn_readlane(units, l) - (tiles - tile) * t.n_split;
+      t.row0 = (tiles - 1 - tile) * BM;
       t.s = sequence(a.c, t.b, a.kv.cap);
       t.rows = t.s.n_new * a.g;
       return true;
     }
-    flat -= __builtin_amdgcn_readfirstlane(__shfl(x, kWave - 1, kWave));
+    flat -= last_lane(x);
+    unit += last_lane(units);
   }
   return false;
 }
 
-template <bool PRIV, int BM> __device__ __forceinline__ bool find_tile(const AttnArgs &a, int flat, Tile &t) {
-  if (!PRIV) return locate<BM>(a, flat, t);
-  t.b = flat;
-  t.row0 = 0;
-  t.s = sequence(a.c, t.b, a.kv.cap);
-  t.rows = t.s.n_new * a.g;
-  return t.rows > 0 && t.rows <= 32;
-}
-
 // A wave's share of the copies of one tile of rows.  The page of the lane's row is
-// looked up a tile ahead; the rows' offsets are then passed between lanes.
+// looked up a tile ahead (without a branch: the value must not be needed before
+// then); the rows' offsets are then passed between lanes.
 template <typename T, int D, int BN, int SHARE> struct Loader {
   using L = TileLayout<T, D>;
   static constexpr int kRpi = 64 / L::C;        // rows per instruction
   static constexpr int kInstr = SHARE / kRpi;   // instructions per wave, K or V
   static_assert(SHARE % kRpi == 0 && kInstr >= 1, "a wave copies whole instructions");
-  int row, page;  // the lane's row of the looked-up tile, and its page (-1: none)
+  const int32_t *pages;  // of the sequence (dense: any readable word)
+  int len, page;         // rows from `len` on do not exist; the looked-up page
 
-  __device__ __forceinline__ void lookup(const CacheView &kv, int b, int row0, int len) {
-    row = row0 + (int)(threadIdx.x & (BN - 1));
-    page = -1;
-    if (row < len) page = row_page(kv, b, row);
+  __device__ __forceinline__ void init(const AttnArgs &a, int b, int end) {
+    pages = a.kv.table ? a.kv.table + (int64_t)b * a.kv.width : a.c.len;
+    len = end;
+  }
+  __device__ __forceinline__ void lookup(const CacheView &kv, int row0) {
+    const int row = row0 + (int)(threadIdx.x & (BN - 1));
+    page = pages[max(min(row, len - 1), 0) >> kv.shift];  // (dense: shift 31)
+  }
+  // Offset of the lane's row of the looked-up tile, or -1.
+  __device__ __forceinline__ int64_t offset(const CacheView &kv, int b, int row0) const {
+    const int row = row0 + (int)(threadIdx.x & (BN - 1));
+    const int64_t off = page_offset(kv, kv.table ? page : b, row);
+    return row < len ? off : -1;
+  }
+  __device__ __forceinline__ static int64_t pass(int64_t off, int from) {
+    const int lo = __shfl((int)off, from, kWave), hi = __shfl((int)(off >> 32), from, kWave);
+    return ((int64_t)hi << 32) | (uint32_t)lo;
+  }
+  // The lane's row of an instruction and piece of a row; ANEW: computed each time
+  // (kept, the addresses of the few-rows form's 16 instructions would take 32 registers).
+  template <bool ANEW> __device__ __forceinline__ static void place(int &rr, int &p) {
+    int lane = threadIdx.x & (kWave - 1);
+    if (ANEW) asm volatile("" : "+v"(lane));
+    rr = lane / L::C;
+    p = lane & (L::C - 1);
   }
   // Rows first..first+SHARE-1 of the tile; sk, sv: the tile's start in LDS.
-  // Returns which rows exist.
-  __device__ __forceinline__ uint64_t issue(const CacheView &kv, const unsigned char *k, const unsigned char *v,
-                                            int first, unsigned char *sk, unsigned char *sv) const {
-    const int lane = threadIdx.x & (kWave - 1), rr = lane / L::C, p = lane & (L::C - 1);
-    const int64_t off = page_offset(kv, page, row);
+  __device__ __forceinline__ static void issue(int64_t off, const unsigned char *k, const unsigned char *v, int first,
+                                               unsigned char *sk, unsigned char *sv) {
+    int rr, p;
+    place<false>(rr, p);
 #pragma unroll
     for (int j = 0; j < kInstr; ++j) {
       const int r = first + j * kRpi + rr;
-      const int lo = __shfl((int)off, r, kWave), hi = __shfl((int)(off >> 32), r, kWave);
-      const int64_t o = ((int64_t)hi << 32) | (uint32_t)lo;
-      const unsigned char *pk = hi < 0 ? zero_row : k + o;
-      const unsigned char *pv = hi < 0 ? zero_row : v + o;
-      load_to_lds16(pk + ((p ^ L::swz_k(r)) << 4), sk + (first + j * kRpi) * L::bytes);
-      load_to_lds16(pv + ((p ^ L::swz_v(r)) << 4), sv + (first + j * kRpi) * L::bytes);
+      const int64_t o = pass(off, r);
+      load_to_lds16((o < 0 ? zero_row : k + o) + ((p ^ L::swz_k(r)) << 4), sk + (first + j * kRpi) * L::bytes);
+      load_to_lds16((o < 0 ? zero_row : v + o) + ((p ^ L::swz_v(r)) << 4), sv + (first + j * kRpi) * L::bytes);
     }
-    return __ballot(off >= 0);
+  }
+  // The same for all rows, keys or values only.
+  template <bool VALUES>
+  __device__ __forceinline__ static void issue_one(int64_t off, const unsigned char *base, unsigned char *lds) {
+    int rr, p;
+    place<true>(rr, p);
+#pragma unroll
+    for (int j = 0; j < kInstr; ++j) {
+      const int r = j * kRpi + rr;
+      const int64_t o = pass(off, r);
+      load_to_lds16((o < 0 ? zero_row : base + o) + ((p ^ (VALUES ? L::swz_v(r) : L::swz_k(r))) << 4),
+                    lds + j * kRpi * L::bytes);
+    }
   }
 };
 
@@ -209,8 +303,10 @@ __device__ __forceinline__ void values32(const unsigned char *sv, int key0, cons
         for (int x = 0; x < 2; ++x) {
           const int r = key0 + 16 * s + 8 * x + 4 * half + ((lane & 15) >> 2);
           const int c = d * 4 + ((lane & 31) >> 4) * 2 + ((lane & 3) >> 1);
-          const unsigned char *at = sv + r * L::bytes + ((c ^ L::swz_v(r)) << 4) + (lane & 1) * 8;
-          vf.h[x] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((SMALLKV_LDS s16x4_t *)at);
+          // (one addition: the compiler follows an LDS array through few of them, and
+          // does not hold these reads up for copies into other arrays while it does)
+          const int at = r * L::bytes + ((c ^ L::swz_v(r)) << 4) + (lane & 1) * 8;
+          vf.h[x] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((SMALLKV_LDS s16x4_t *)(sv + at));
         }
         o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf.v, pf, o[d], 0, 0, 0);
       }
@@ -245,6 +341,12 @@ template <typename T> __device__ __forceinline__ bool drop_not_finite(uint4 &w) 
 template <typename T, int D> struct State {
   float m, l;  // running maximum (log2 units), this half-wave's part of the sum
   f32x16_t o[D / 32];
+  __device__ __forceinline__ void clear() {
+    m = -INFINITY;
+    l = 0.0f;
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d) o[d] = f32x16_t{};
+  }
 };
 
 // The running maximum, sum and output of a tile's logits s.
@@ -334,144 +436,51 @@ __device__ __forceinline__ void give_back(const AttnArgs &a, int b, const unsign
   }
 }
 
-// PRIV: the few-rows form (waves take turns at the tiles of BN keys).
-template <typename T, int D, int NW, bool PRIV, int BN>
-__global__ __launch_bounds__(NW * kWave, !PRIV && sizeof(T) == 2 ? 2 : 1) void chunk_attn(AttnArgs a) {
-  using L = TileLayout<T, D>;
-  constexpr int BM = PRIV ? 32 : NW * 32, kBuf = BN * L::bytes * (PRIV ? NW : 1);
-  constexpr int kShare = PRIV ? BN : BN / NW;
-  // four arrays: what is copied into one does not hold up the reads of another
-  __shared__ __align__(16) unsigned char k0[kBuf], v0[kBuf], k1[kBuf], v1[kBuf];
-  __shared__ float ml[2][2][kWave];
-  const int lane = threadIdx.x & (kWave - 1);
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  const int kvh = blockIdx.x % a.hkv, flat = blockIdx.x / a.hkv;
+// A workgroup's share of the work, and the lane's row of it.
+template <int BM> struct Share {
   Tile t;
-  if (!find_tile<PRIV, BM>(a, flat, t)) return;
-  const int pos0 = t.s.len - t.s.n_new;  // cached row of the first new token
-  const int last = min(t.row0 + BM, t.rows) - 1;
-  const int limit = max(pos0 + last / a.g + 1, 0);  // keys the tile's rows see (<= len)
-  const int split = blockIdx.y, begin = split * a.span, end = min(limit, begin + a.span);
-  if (begin >= limit && split > 0) return;
-  // the lane's row
-  const int r = t.row0 + (PRIV ? 0 : wave * 32) + (lane & 31);
-  const bool live = r < t.rows;
-  const int rc = live ? r : t.rows - 1, token = t.s.first + rc / a.g, head = kvh * a.g + rc % a.g;
-  const int own = live ? pos0 + rc / a.g : -1;
-  const int first_own = pos0 + t.row0 / a.g;  // of the workgroup's first row
-  const int highest = pos0 + min(t.row0 + (PRIV ? 0 : wave * 32) + 31, t.rows - 1) / a.g;  // of the wave's last
-  const bool idle = !PRIV && t.row0 + wave * 32 >= t.rows;
-  QFrag<T, D> q;
-  q.load(a.q + (token * a.q_token + head * a.q_head) * (int64_t)sizeof(T), lane >> 5);
-  const unsigned char *k = a.kv.k + (((uint64_t)kvh * a.kv.head_stride) << 4);
-  const unsigned char *v = a.kv.v + (((uint64_t)kvh * a.kv.head_stride) << 4);
+  int kvh, unit, begin, end;  // kv head; unit and kv head; the span's cached rows
+  int r, token, head, own;    // the lane's row, its cached row (-1: past the last)
+  int first_own;              // cached row of the workgroup's first row
+  bool live;
+  const unsigned char *k, *v; // of the kv head
 
-  State<T, D> st;
-  st.m = -INFINITY;
-  st.l = 0.0f;
-#pragma unroll
-  for (int d = 0; d < D / 32; ++d) st.o[d] = f32x16_t{};
+  __device__ __forceinline__ bool find(const AttnArgs &a, int block, int round, int wave_row) {
+    kvh = block % a.hkv;
+    const int span = find_span<BM>(a, round);
+    if (a.splits && block == 0 && threadIdx.x == 0) *a.span = span;
+    if (!locate<BM, true>(a, span, block / a.hkv, t)) return false;
+    unit = block;
+    const int pos0 = t.s.len - t.s.n_new;  // cached row of the first new token
+    const int last = min(t.row0 + BM, t.rows) - 1;
+    const int limit = max(pos0 + last / a.g + 1, 0);  // keys the tile's rows see (<= len)
+    begin = t.split * span;  // (one span: 0)
+    end = min(limit, begin + span);
+    if (begin >= limit && t.split > 0) return false;  // (attn_merge reads no record of it)
+    r = t.row0 + wave_row + (int)(threadIdx.x & 31);
+    live = r < t.rows;
+    const int rc = live ? r : t.rows - 1;
+    token = t.s.first + rc / a.g;
+    head = kvh * a.g + rc % a.g;
+    own = live ? pos0 + rc / a.g : -1;
+    first_own = pos0 + t.row0 / a.g;
+    k = a.kv.k + (((uint64_t)kvh * a.kv.head_stride) << 4);
+    v = a.kv.v + (((uint64_t)kvh * a.kv.head_stride) << 4);
+    return true;
+  }
+};
 
-  constexpr uint64_t kAll = BN == 64 ? ~0ull : (1ull << (BN & 63)) - 1;
-  const int step = PRIV ? NW * BN : BN, at = PRIV ? wave * BN * L::bytes : 0;
-  const int mine = PRIV ? 0 : wave * kShare;
-  int row = begin + (PRIV ? wave * BN : 0);
-  Loader<T, D, BN, kShare> ld;
-  ld.lookup(a.kv, t.b, row, end);
-  uint64_t valid = 0;
-  if (row < end) {
-    valid = ld.issue(a.kv, k, v, mine, k0 + at, v0 + at);
-    ld.lookup(a.kv, t.b, row + step, end);
-  }
-  // the tile at `row` is in place; the next one goes to (nk, nv)
-  auto advance = [&](unsigned char *nk, unsigned char *nv) {
-    wait_memory();  // this wave's copies of the tile, and its reads of the other buffer
-    if (!PRIV) __syncthreads();
-    const uint64_t now = valid;
-    if (row + step < end) {
-      valid = ld.issue(a.kv, k, v, mine, nk + at, nv + at);
-      ld.lookup(a.kv, t.b, row + 2 * step, end);
-    }
-    return now;
-  };
-  // tiles that every row sees whole, then the others
-  bool odd = false, taken = false;
-  uint64_t now = 0;
-  bool full = true;
-  while (row < end) {
-    now = advance(k1, v1);
-    if (!(full = row + BN - 1 <= first_own && (now & kAll) == kAll)) break;
-    if (!idle) full_tile<T, D, BN>(st, q, k0 + at, v0 + at, a.scale2, a.scale2_lo);
-    row += step;
-    if (row >= end) break;
-    odd = true;
-    now = advance(k0, v0);
-    if (!(full = row + BN - 1 <= first_own && (now & kAll) == kAll)) break;
-    if (!idle) full_tile<T, D, BN>(st, q, k1 + at, v1 + at, a.scale2, a.scale2_lo);
-    row += step;
-    odd = false;
-  }
-  while (row < end) {
-    unsigned char *sk = (odd ? k1 : k0) + at, *sv = (odd ? v1 : v0) + at;
-    if (full) now = advance(odd ? k0 : k1, odd ? v0 : v1);
-    full = true;
-    if (min(row + BN, end) - 1 > first_own) {
-      // some row does not see some key, and 0 * inf or 0 * NaN would reach it
-      // through the matrix product: such values are taken out here and given to
-      // the rows that see them at the end
-      bool found = false;
-      for (int i = PRIV ? lane : threadIdx.x; i < BN * L::C; i += PRIV ? kWave : NW * kWave) {
-        uint4 w = reinterpret_cast<uint4 *>(sv)[i];
-        if (drop_not_finite<T>(w)) {
-          reinterpret_cast<uint4 *>(sv)[i] = w;
-          found = true;
-        }
-      }
-      taken |= PRIV ? __any(found) : __syncthreads_or(found);
-    }
-    if (!idle && row <= highest)
-      masked_tile<T, D, BN>(st, q, sk, sv, row, own, now, a.scale2, a.scale2_lo);
-    row += step;
-    odd = !odd;
-  }
-  if (PRIV) {
-    taken = __syncthreads_or(taken);
-    // join the waves' results: the upper half hands over to the lower one
-    float *x = reinterpret_cast<float *>(k0);
-#pragma unroll
-    for (int h = NW / 2; h >= 1; h >>= 1) {
-      __syncthreads();
-      if (wave >= h && wave < 2 * h) {
-        float *y = x + (wave - h) * (D / 2) * kWave;
-        ml[0][wave - h][lane] = st.m;
-        ml[1][wave - h][lane] = st.l;
-#pragma unroll
-        for (int d = 0; d < D / 32; ++d)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) y[(d * 16 + i) * kWave + lane] = st.o[d][i];
-      }
-      __syncthreads();
-      if (wave < h) {
-        const float *y = x + wave * (D / 2) * kWave;
-        const float om = ml[0][wave][lane], ol = ml[1][wave][lane];
-        const float m = fmaxf(st.m, om), base = m == -INFINITY ? 0.0f : m;
-        const float f = __builtin_amdgcn_exp2f(st.m - base), fo = __builtin_amdgcn_exp2f(om - base);
-        st.m = m;
-        st.l = st.l * f + ol * fo;
-#pragma unroll
-        for (int d = 0; d < D / 32; ++d)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) st.o[d][i] = st.o[d][i] * f + y[(d * 16 + i) * kWave + lane] * fo;
-      }
-    }
-    if (wave > 0) return;
-  }
-  if (!live) return;
+// The lane's row of the output, or of the span's record.  taken: values were taken
+// out of a tile of BN keys.
+template <typename T, int D, int BM, int BN>
+__device__ __forceinline__ void write_row(const AttnArgs &a, const Share<BM> &w, const State<T, D> &st, bool taken) {
+  if (!w.live) return;
   const float l = swap_halves_sum(st.l);
-  const int half = lane >> 5;
-  if (a.n_split > 1) {
-    const int64_t at_row = ((int64_t)split * gridDim.x + blockIdx.x) * BM + (r - t.row0);
-    float *o = a.rec + at_row * D;
+  const int half = (threadIdx.x & (kWave - 1)) >> 5;
+  const int from = max(w.begin, w.first_own + 2 - BN), to = min(w.end - 1, w.own);
+  if (w.t.n_split > 1) {
+    const int64_t row = (int64_t)w.unit * BM + (w.r - w.t.row0);
+    float *o = a.rec + row * D;
 #pragma unroll
     for (int d = 0; d < D / 32; ++d)
 #pragma unroll
@@ -479,14 +488,14 @@ __global__ __launch_bounds__(NW * kWave, !PRIV && sizeof(T) == 2 ? 2 : 1) void c
         *reinterpret_cast<f32x4_t *>(o + d * 32 + 2 * i + 4 * half) =
             f32x4_t{st.o[d][i], st.o[d][i + 1], st.o[d][i + 2], st.o[d][i + 3]};
     if (half == 0) {
-      a.rec[a.rec_ml + 2 * at_row] = st.m;
-      a.rec[a.rec_ml + 2 * at_row + 1] = l;
+      a.rec[a.rec_ml + 2 * row] = st.m;
+      a.rec[a.rec_ml + 2 * row + 1] = l;
     }
-    if (taken) give_back<float, T, D>(a, t.b, v, o, max(begin, first_own + 2 - BN), min(end - 1, own));
+    if (taken) give_back<float, T, D>(a, w.t.b, w.v, o, from, to);
     return;
   }
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;  // (0: the row sees no key)
-  unsigned char *o = a.out + (token * a.o_token + head * a.o_head) * (int64_t)sizeof(T);
+  unsigned char *o = a.out + (w.token * a.o_token + w.head * a.o_head) * (int64_t)sizeof(T);
 #pragma unroll
   for (int d = 0; d < D / 32; ++d)
 #pragma unroll
@@ -498,71 +507,261 @@ __global__ __launch_bounds__(NW * kWave, !PRIV && sizeof(T) == 2 ? 2 : 1) void c
       else
         *reinterpret_cast<bf16x4_t *>(o + e * 2) = __builtin_convertvector(x, bf16x4_t);
     }
-  if (taken) give_back<T, T, D>(a, t.b, v, o, max(begin, first_own + 2 - BN), min(end - 1, own));
+  if (taken) give_back<T, T, D>(a, w.t.b, w.v, o, from, to);
   if (a.lse && half == 0)
-    a.lse[(int64_t)token * a.hq + head] = l == 0.0f ? -INFINITY : (st.m + __log2f(l)) * kLn2;
+    a.lse[(int64_t)w.token * a.hq + w.head] = l == 0.0f ? -INFINITY : (st.m + __log2f(l)) * kLn2;
 }
 
-// Joins the records of a row's spans: a wave per row, D / 64 elements a lane.
-template <typename T, int D, bool PRIV, int BM>
-__global__ __launch_bounds__(4 * kWave) void chunk_merge(AttnArgs a) {
-  constexpr int E = D / kWave;
+// Infinite and NaN values of a tile are taken out of it where some row does not see
+// some key, since 0 * inf or 0 * NaN would reach that row through the matrix
+// product; write_row gives them to the rows that see them.
+template <typename T, int N> __device__ __forceinline__ bool take_out(unsigned char *sv, int first, int step) {
+  bool found = false;
+  for (int i = first; i < N; i += step) {
+    uint4 w = reinterpret_cast<uint4 *>(sv)[i];
+    if (drop_not_finite<T>(w)) {
+      reinterpret_cast<uint4 *>(sv)[i] = w;
+      found = true;
+    }
+  }
+  return found;
+}
+
+template <typename T, int D, int NW, int BN>
+__global__ __launch_bounds__(NW * kWave, sizeof(T) == 2 ? 2 : 1) void attn_many(AttnArgs a) {
+  using L = TileLayout<T, D>;
+  constexpr int BM = NW * 32, kBuf = BN * L::bytes, kRows = BN / NW;
+  // four arrays: what is copied into one does not hold up the reads of another
+  __shared__ __align__(16) unsigned char k0[kBuf], v0[kBuf], k1[kBuf], v1[kBuf];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  Share<BM> w;
+  if (!w.find(a, blockIdx.x, kManyRound, wave * 32)) return;
+  const int w0 = w.t.row0 + wave * 32;
+  const bool idle = w0 >= w.t.rows;
+  const int highest = w.t.s.len - w.t.s.n_new + min(w0 + 31, w.t.rows - 1) / a.g;  // of the wave's rows
+  QFrag<T, D> q;
+  q.load(a.q + (w.token * a.q_token + w.head * a.q_head) * (int64_t)sizeof(T), (threadIdx.x & (kWave - 1)) >> 5);
+  State<T, D> st;
+  st.clear();
+  constexpr uint64_t kAll = BN == 64 ? ~0ull : (1ull << (BN & 63)) - 1;
+  int row = w.begin;
+  Loader<T, D, BN, kRows> ld;
+  ld.init(a, w.t.b, w.end);
+  ld.lookup(a.kv, row);
+  uint64_t valid = 0;
+  if (row < w.end) {
+    const int64_t off = ld.offset(a.kv, w.t.b, row);
+    valid = __ballot(off >= 0);
+    ld.issue(off, w.k, w.v, wave * kRows, k0, v0);
+    ld.lookup(a.kv, row + BN);
+  }
+  // the tile at `row` is in place; the next one goes to (nk, nv)
+  auto advance = [&](unsigned char *nk, unsigned char *nv) {
+    wait_memory();  // this wave's copies of the tile, and its reads of the other buffer
+    __syncthreads();
+    const uint64_t now = valid;
+    if (row + BN < w.end) {
+      const int64_t off = ld.offset(a.kv, w.t.b, row + BN);
+      valid = __ballot(off >= 0);
+      ld.issue(off, w.k, w.v, wave * kRows, nk, nv);
+      ld.lookup(a.kv, row + 2 * BN);
+    }
+    return now;
+  };
+  // tiles that every row sees whole, then the others
+  bool odd = false, taken = false, full = true;
+  uint64_t now = 0;
+  while (row < w.end) {
+    now = advance(k1, v1);
+    if (!(full = row + BN - 1 <= w.first_own && (now & kAll) == kAll)) break;
+    if (!idle) full_tile<T, D, BN>(st, q, k0, v0, a.scale2, a.scale2_lo);
+    row += BN;
+    if (row >= w.end) break;
+    odd = true;
+    now = advance(k0, v0);
+    if (!(full = row + BN - 1 <= w.first_own && (now & kAll) == kAll)) break;
+    if (!idle) full_tile<T, D, BN>(st, q, k1, v1, a.scale2, a.scale2_lo);
+    row += BN;
+    odd = false;
+  }
+  while (row < w.end) {
+    unsigned char *sk = odd ? k1 : k0, *sv = odd ? v1 : v0;
+    if (full) now = advance(odd ? k0 : k1, odd ? v0 : v1);
+    full = true;
+    if (min(row + BN, w.end) - 1 > w.first_own)
+      taken |= __syncthreads_or(take_out<T, BN * L::C>(sv, threadIdx.x, NW * kWave));
+    if (!idle && row <= highest) masked_tile<T, D, BN>(st, q, sk, sv, row, w.own, now, a.scale2, a.scale2_lo);
+    row += BN;
+    odd = !odd;
+  }
+  write_row<T, D, BM, BN>(a, w, st, taken);
+}
+
+// Waits until at most N of this wave's copies and loads are outstanding.
+template <int N> __device__ __forceinline__ void wait_copies() {
+  __builtin_amdgcn_s_waitcnt((N & 15) | (N >> 4) << 14 | 7 << 4 | 15 << 8);
+  asm volatile("" ::: "memory");
+}
+// Waits for this wave's LDS reads.
+__device__ __forceinline__ void wait_lds() {
+  __builtin_amdgcn_s_waitcnt(15 | 3 << 14 | 7 << 4);
+  asm volatile("" ::: "memory");
+}
+
+template <typename T, int D, int NW>
+__global__ __launch_bounds__(NW * kWave, sizeof(T) == 2 || D == 64 ? 2 : 1) void attn_few(AttnArgs a) {
+  using L = TileLayout<T, D>;
+  constexpr int BN = 32, kTile = BN * L::bytes;
+  // one tile of keys and one of values per wave: the next keys are requested when
+  // this tile's are multiplied, the next values after this tile's
+  __shared__ __align__(16) unsigned char k0[NW * kTile], v0[NW * kTile];
+  __shared__ float ml[2][(NW + 1) / 2][kWave];
   const int lane = threadIdx.x & (kWave - 1);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  const int kvh = blockIdx.x % a.hkv, flat = blockIdx.x / a.hkv;
+  Share<32> w;
+  if (!w.find(a, blockIdx.x, NW * 32, 0)) return;
+  unsigned char *sk = k0 + wave * kTile, *sv = v0 + wave * kTile;
+  constexpr int step = NW * BN;
+  int row = w.begin + wave * BN;
+  using Ld = Loader<T, D, BN, BN>;
+  Ld ld;
+  ld.init(a, w.t.b, w.end);
+  ld.lookup(a.kv, row);
+  QFrag<T, D> q;
+  q.load(a.q + (w.token * a.q_token + w.head * a.q_head) * (int64_t)sizeof(T), lane >> 5);
+  State<T, D> st;
+  st.clear();
+  wait_copies<0>();  // the queries and the first page number, requested together
+  int64_t off = ld.offset(a.kv, w.t.b, row);
+  bool taken = false;
+  auto masked = [&]() {
+    wait_memory();
+    if (min(row + BN, w.end) - 1 > w.first_own) {
+      taken |= __any(take_out<T, BN * L::C>(sv, lane, kWave));
+      wait_lds();
+    }
+    masked_tile<T, D, BN>(st, q, sk, sv, row, w.own, (uint32_t)__ballot(off >= 0), a.scale2, a.scale2_lo);
+  };
+  if (row < w.end) {
+    Ld::template issue_one<false>(off, w.k, sk);
+    ld.lookup(a.kv, row + step);
+    Ld::template issue_one<true>(off, w.v, sv);
+    // Copies are requested in the order keys, page number, values, and none of them
+    // on a condition: a wait for all but the last kInstr leaves the values, or the
+    // next keys, on their way.
+    for (; row + step < w.end; row += step) {
+      if (row + BN - 1 <= w.first_own && __ballot(off >= 0) == ~0ull) {
+        wait_copies<Ld::kInstr>();
+        f32x16_t s[1] = {logits32<T, D>(sk, 0, q)};
+        wait_lds();
+        off = ld.offset(a.kv, w.t.b, row + step);
+        Ld::template issue_one<false>(off, w.k, sk);
+        softmax_step<T, D>(st, s, a.scale2, a.scale2_lo);
+        wait_copies<Ld::kInstr>();
+        values32<T, D>(sv, 0, s[0], st.o);
+      } else {
+        masked();
+        wait_lds();
+        off = ld.offset(a.kv, w.t.b, row + step);
+        Ld::template issue_one<false>(off, w.k, sk);
+      }
+      wait_lds();
+      ld.lookup(a.kv, row + 2 * step);
+      Ld::template issue_one<true>(off, w.v, sv);
+    }
+    masked();
+  }
+  taken = __syncthreads_or(taken);
+  // join the waves' results: the upper half hands over to the lower one
+  float *x = reinterpret_cast<float *>(k0);
+#pragma unroll
+  for (int h = NW / 2; h >= 1; h >>= 1) {
+    __syncthreads();
+    if (wave >= h && wave < 2 * h) {
+      float *y = x + (wave - h) * (D / 2) * kWave;
+      ml[0][wave - h][lane] = st.m;
+      ml[1][wave - h][lane] = st.l;
+#pragma unroll
+      for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) y[(d * 16 + i) * kWave + lane] = st.o[d][i];
+    }
+    __syncthreads();
+    if (wave < h) {
+      const float *y = x + wave * (D / 2) * kWave;
+      const float om = ml[0][wave][lane], ol = ml[1][wave][lane];
+      const float m = fmaxf(st.m, om), base = m == -INFINITY ? 0.0f : m;
+      const float f = __builtin_amdgcn_exp2f(st.m - base), fo = __builtin_amdgcn_exp2f(om - base);
+      st.m = m;
+      st.l = st.l * f + ol * fo;
+#pragma unroll
+      for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) st.o[d][i] = st.o[d][i] * f + y[(d * 16 + i) * kWave + lane] * fo;
+    }
+  }
+  if (wave == 0) write_row<T, D, 32, BN>(a, w, st, taken);
+}
+
+// Joins the records of a tile's spans: four elements of a row per lane, all spans in
+// one pass with the running maximum, so that their loads are in flight together.
+template <int D> constexpr int merge_rows() { return 256 / (D / 4); }  // per workgroup
+
+template <typename T, int D, int BM>
+__global__ __launch_bounds__(256) void attn_merge(AttnArgs a) {
+  const int kvh = blockIdx.x % a.hkv, span = *a.span;
   Tile t;
-  if (!find_tile<PRIV, BM>(a, flat, t)) return;
-  const int in = blockIdx.y * 4 + wave, r = t.row0 + in;
+  if (span == kWhole || !locate<BM, false>(a, span, blockIdx.x / a.hkv, t) || t.n_split == 1) return;
+  const int in = blockIdx.y * merge_rows<D>() + threadIdx.x / (D / 4), e = threadIdx.x % (D / 4) * 4;
+  const int r = t.row0 + in;
   if (r >= t.rows) return;
   const int own = t.s.len - t.s.n_new + r / a.g;
   const int token = t.s.first + r / a.g, head = kvh * a.g + r % a.g;
   // spans that hold a row this one sees; the others wrote nothing it needs
-  const int n = min(max((own + a.span) / a.span, 0), a.n_split);
-  const int64_t stride = (int64_t)gridDim.x * BM, at = (int64_t)blockIdx.x * BM + in;
-  float m = -INFINITY;
-  for (int s = lane; s < n; s += kWave) m = fmaxf(m, a.rec[a.rec_ml + 2 * (s * stride + at)]);
-  m = wave_max(m);
-  const float base = m == -INFINITY ? 0.0f : m;
-  float l = 0.0f, o[E] = {};
+  const int n = own < 0 ? 0 : min(own / span + 1, t.n_split);
+  const int64_t stride = (int64_t)a.hkv * BM, at = ((int64_t)t.unit0 * a.hkv + kvh) * BM + in;
+  const float *ml = a.rec + a.rec_ml + 2 * at, *rec = a.rec + at * D + e;
+  float m = -INFINITY, l = 0.0f;
+  f32x4_t o = {};
+#pragma unroll 8
   for (int s = 0; s < n; ++s) {
-    const int64_t i = s * stride + at;
-    const float w = __builtin_amdgcn_exp2f(a.rec[a.rec_ml + 2 * i] - base);
-    l += w * a.rec[a.rec_ml + 2 * i + 1];
-#pragma unroll
-    for (int e = 0; e < E; ++e) o[e] += w * a.rec[i * D + lane * E + e];
+    const float2 x = *reinterpret_cast<const float2 *>(ml + 2 * s * stride);
+    const f32x4_t v = *reinterpret_cast<const f32x4_t *>(rec + s * stride * D);
+    const float top = fmaxf(m, x.x), base = top == -INFINITY ? 0.0f : top;
+    const float f = __builtin_amdgcn_exp2f(m - base), w = __builtin_amdgcn_exp2f(x.x - base);
+    m = top;
+    l = l * f + x.y * w;
+    o = o * f + v * w;
   }
-  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+  const f32x4_t x = o * (l == 0.0f ? 0.0f : 1.0f / l);
   unsigned char *out = a.out + (token * a.o_token + head * a.o_head) * (int64_t)sizeof(T);
-#pragma unroll
-  for (int e = 0; e < E; ++e) elem<T>::store1(out, lane * E + e, o[e] * inv);
-  if (a.lse && lane == 0)
+  if constexpr (sizeof(T) == 4)
+    *reinterpret_cast<f32x4_t *>(out + e * 4) = x;
+  else
+    *reinterpret_cast<bf16x4_t *>(out + e * 2) = __builtin_convertvector(x, bf16x4_t);
+  if (a.lse && e == 0)
     a.lse[(int64_t)token * a.hq + head] = l == 0.0f ? -INFINITY : (m + __log2f(l)) * kLn2;
 }
 
-template <typename T, int D, int NW, bool PRIV, int BN>
-hipError_t launch_form(AttnArgs a, int tiles, int span, int n_split, float *rec, hipStream_t st) {
-  constexpr int BM = PRIV ? 32 : NW * 32;
-  a.span = span;
-  a.n_split = n_split;
-  a.rec = rec;
-  a.rec_ml = (int64_t)n_split * tiles * a.hkv * BM * D;
-  hipLaunchKernelGGL((chunk_attn<T, D, NW, PRIV, BN>), dim3(tiles * a.hkv, n_split), dim3(NW * kWave), 0, st, a);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess || n_split == 1) return e;
-  hipLaunchKernelGGL((chunk_merge<T, D, PRIV, BM>), dim3(tiles * a.hkv, BM / 4), dim3(4 * kWave), 0, st, a);
+template <typename T, int D> hipError_t launch_typed(AttnArgs a, const AttnPlan &p, hipStream_t st) {
+  constexpr bool h = sizeof(T) == 2;
+  constexpr int NF = h ? 4 : 2, BM = kAttnWaves * 32;
+  const dim3 grid(p.units * a.hkv), merge(p.tiles * a.hkv, p.rows / merge_rows<D>());
+  a.rec_ml = (int64_t)p.units * a.hkv * p.rows * D;
+  if (p.few)
+    hipLaunchKernelGGL((attn_few<T, D, NF>), grid, dim3(NF * kWave), 0, st, a);
+  else
+    hipLaunchKernelGGL((attn_many<T, D, kAttnWaves, h ? 64 : 32>), grid, dim3(kAttnWaves * kWave), 0, st, a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || !p.splits) return e;
+  if (p.few)
+    hipLaunchKernelGGL((attn_merge<T, D, 32>), merge, dim3(256), 0, st, a);
+  else
+    hipLaunchKernelGGL((attn_merge<T, D, BM>), merge, dim3(256), 0, st, a);
   return hipGetLastError();
 }
 
-template <typename T, int D> hipError_t launch_typed(AttnArgs a, const AttnPlan &p, float *ws, hipStream_t st) {
-  constexpr bool h = sizeof(T) == 2;
-  if (p.many_tiles) {
-    const hipError_t e = launch_form<T, D, kAttnWaves, false, h ? 64 : 32>(a, p.many_tiles, p.many_span, p.many_split, ws, st);
-    if (e != hipSuccess) return e;
-  }
-  if (!p.few_tiles) return hipSuccess;
-  return launch_form<T, D, h ? 4 : 2, true, 32>(a, p.few_tiles, p.few_span, p.few_split,
-                                                ws + p.many_bytes / sizeof(float), st);
-}
+constexpr size_t kSpanBytes = 256;  // before the records
 
 int ceil_div(int64_t x, int64_t y) { return (int)((x + y - 1) / y); }
 
@@ -572,29 +771,19 @@ AttnPlan plan_chunk_attn(const smallkv_chunk_t &c, const smallkv_cache_t &kv, co
   AttnPlan p{};
   const int g = q.n_heads / kv.n_heads;
   const int64_t rows = (int64_t)c.max_new * g;
-  constexpr int kBm = kAttnWaves * 32;
-  p.use_few = rows <= 32 || c.batch > 1;
-  if (p.use_few) {
-    // a workgroup per CU; spans of whole rounds of the waves' tiles
-    const int round = kv.dtype == SMALLKV_F32 ? 64 : 128;
-    p.few_tiles = c.batch;
-    const int64_t units = (int64_t)c.batch * kv.n_heads;
-    const int want = units >= 512 ? 1 : ceil_div(512, units);
-    p.few_span = ceil_div(ceil_div(c.max_len, want), round) * round;
-    p.few_split = ceil_div(c.max_len, p.few_span);
-  }
-  if (rows > 32) {
-    const int64_t per = ceil_div(rows, kBm);
-    p.many_tiles = (int)std::min<int64_t>(c.batch * per, (int64_t)c.n_tokens * g / kBm + c.batch);
-    const int64_t units = (int64_t)p.many_tiles * kv.n_heads;
-    const int want = units >= 384 ? 1 : ceil_div(512, units);
-    p.many_span = ceil_div(ceil_div(c.max_len, want), 256) * 256;
-    p.many_split = ceil_div(c.max_len, p.many_span);
-  }
-  const int64_t d2 = (kv.head_dim + 2) * (int64_t)sizeof(float);
-  if (p.many_split > 1) p.many_bytes = (size_t)p.many_split * p.many_tiles * kv.n_heads * kBm * d2;
-  p.ws_bytes = p.many_bytes;
-  if (p.few_split > 1) p.ws_bytes += (size_t)p.few_split * p.few_tiles * kv.n_heads * 32 * d2;
+  p.few = rows <= 32;
+  p.rows = p.few ? 32 : kAttnWaves * 32;
+  // no more tiles than this, whatever the sequences' lengths
+  p.tiles = (int)std::min<int64_t>(c.batch * ceil_div(rows, p.rows), (int64_t)c.n_tokens * g / p.rows + c.batch);
+  // the workgroups that run at once on 256 CUs: three per CU of bf16 and 64 elements
+  // (33 KB of LDS, up to 160 registers), two of 128 elements and of fp32.  (A batch
+  // of chunks and tokens of 64 elements: 49 us with 512, 46 with 768, 46 with 1024;
+  // a batch-64 decode step of 128 elements: 79 with 256, 70 with 512, 71 with 1024.)
+  const int slots = std::max((kv.head_dim == 64 && kv.dtype == SMALLKV_BF16 ? 768 : 512) / kv.n_heads, 1);
+  const int round = !p.few ? kManyRound : kv.dtype == SMALLKV_F32 ? 64 : 128;
+  if (p.tiles < slots && c.max_len > round) p.splits = slots;
+  p.units = std::max(p.tiles, p.splits);
+  if (p.splits) p.ws_bytes = kSpanBytes + (size_t)p.units * kv.n_heads * p.rows * (kv.head_dim + 2) * sizeof(float);
   return p;
 }
 
@@ -616,11 +805,12 @@ hipError_t launch_chunk_attn(const smallkv_chunk_t &c, const smallkv_cache_t &kv
   a.lse = q.lse;
   a.scale2 = (float)(q.scale * kLog2e);
   a.scale2_lo = (float)(q.scale * kLog2e - a.scale2);
-  a.few = p.use_few;
-  float *rec = static_cast<float *>(ws);
+  a.splits = p.splits;
+  a.span = static_cast<int *>(ws);
+  if (ws) a.rec = reinterpret_cast<float *>(static_cast<char *>(ws) + kSpanBytes);
   if (kv.dtype == SMALLKV_F32)
-    return kv.head_dim == 64 ? launch_typed<float, 64>(a, p, rec, st) : launch_typed<float, 128>(a, p, rec, st);
-  return kv.head_dim == 64 ? launch_typed<bf16_t, 64>(a, p, rec, st) : launch_typed<bf16_t, 128>(a, p, rec, st);
+    return kv.head_dim == 64 ? launch_typed<float, 64>(a, p, st) : launch_typed<float, 128>(a, p, st);
+  return kv.head_dim == 64 ? launch_typed<bf16_t, 64>(a, p, st) : launch_typed<bf16_t, 128>(a, p, st);
 }
 
 }  // namespace smallkv

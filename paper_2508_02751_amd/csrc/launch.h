@@ -132,13 +132,13 @@ hipError_t launch_hybrid(const smallkv_batch_t &b, const smallkv_model_t &m,
 // Cache operators.  Waves (of 32 rows) of the attention's many-rows form.
 constexpr int kAttnWaves = 4;
 
-// Plan of smallkv_chunk_attn: which forms run, their tiles of rows (bounds over
-// the batch), the spans the cached rows are cut into, and the records' bytes.
+// Plan of smallkv_chunk_attn: its form and rows per tile, a bound on the tiles over
+// the batch, the (tile, span) units that may run at once (0: no spans), the
+// launch's units per kv head, and the records' bytes.
 struct AttnPlan {
-  int use_few;
-  int few_tiles, few_span, few_split;
-  int many_tiles, many_span, many_split;
-  size_t many_bytes, ws_bytes;
+  bool few;
+  int rows, tiles, splits, units;
+  size_t ws_bytes;
 };
 AttnPlan plan_chunk_attn(const smallkv_chunk_t &c, const smallkv_cache_t &kv,
                          const smallkv_queries_t &q);
