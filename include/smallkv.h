@@ -505,7 +505,7 @@ typedef struct {
 } smallkv_chunk_t;
 
 /* Queries of the packed tokens: token t, head h at q + t * token_stride +
- * h * head_stride elements (multiples of 16 bytes, like q), in the cache's
+ * h * head_stride elements (multiples of 16 bytes below 2^32, like q), in the cache's
  * dtype and head_dim; head h reads kv head h / (n_heads / cache n_heads). */
 typedef struct {
   int32_t n_heads;

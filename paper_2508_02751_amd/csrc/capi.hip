@@ -234,6 +234,8 @@ int check_queries(const smallkv_chunk_t *c, const smallkv_cache_t *kv, const sma
   if (!(q->scale > 0.0f) || !(q->scale <= 3.402823e38f)) return SMALLKV_EINVAL;
   if (!aligned16(q->q) || !stride_ok(q->token_stride, kv->dtype) || !stride_ok(q->head_stride, kv->dtype))
     return SMALLKV_EINVAL;
+  const int64_t bytes = kv->dtype == SMALLKV_F32 ? 4 : 2;
+  if (q->token_stride * bytes > UINT32_MAX || q->head_stride * bytes > UINT32_MAX) return SMALLKV_EUNSUPPORTED;
   // rows (token, query head of a group) and tiles of 32 of them are counted in 32 bits
   const int64_t rows = (int64_t)c->max_new * (q->n_heads / kv->n_heads);
   if (rows > (1 << 30) || (rows + 31) / 32 * c->batch * kv->n_heads > (1 << 30)) return SMALLKV_EUNSUPPORTED;

@@ -1,16 +1,22 @@
 // The attention weight that the new tokens give every cached row, added to its
 // running score: out[r] = before[r] + sum over (token, head) of exp(s - lse).
 //
-// A workgroup owns 128 keys of one kv head (32 per wave, their K rows in
-// registers as the left operand of S^T = K Q^T) and walks the query rows that
-// see them, 64 at a time through LDS, so no sum leaves its workgroup: no
-// atomics, one order, and the logits are never stored.  A lane holds one query
-// row's logits of 16 keys: one fused multiply-add, one exponential and one add
-// each, which bound the pass (an exponential takes four times an add; the
-// product's matrix instructions run beside them).
-//
-// Scores per query head: the heads are dealt to workgroups (blockIdx.y), each
-// walking one head's tokens; per kv head: the rows are (token, head) pairs.
+// No sum leaves its workgroup: no atomics, one order, and the logits are never
+// stored.  Two forms:
+//   chunk   -- a workgroup owns keys of one kv head (32 per wave, their K rows in
+//              registers as the left operand of S^T = K Q^T) and walks the
+//              query rows that see them, 64 at a time through LDS.  A lane holds one
+//              query row's logits of 16 keys of a block: one fused multiply-add, one
+//              exponential and one add each, which bound the pass; the product's
+//              matrix instructions run beside them.  Scores per query head: the heads
+//              are dealt to workgroups (blockIdx.y), each walking one head's tokens;
+//              per kv head: the rows are (token, head) pairs.
+//   few     -- no sequence has more than 32 (token, head) rows (a decode step): the
+//              rows stay in registers as the left operand of S = Q K^T, a lane holds
+//              one key's logits, and each wave streams its keys' rows, bound by
+//              reading K once.
+#include <algorithm>
+
 #include "cache.h"
 #include "launch.h"
 
@@ -30,13 +36,14 @@ struct ScoreArgs {
   float *out;
   int64_t rows;   // of before and out
   float scale2;   // scale * log2(e)
+  int span;       // few: keys per workgroup, a multiple of 128
 };
 
 constexpr float kLog2e = 1.4426950408889634074f;
 constexpr int kNW = 4, kKeys = 32 * kNW, kRows = 64;
 
-template <typename T, int D>
-__global__ __launch_bounds__(kNW * kWave) void chunk_scores(ScoreArgs a) {
+template <typename T, int D, bool PER_KV>
+__global__ __launch_bounds__(kNW * kWave, 2) void chunk_scores(ScoreArgs a) {
   using L = TileLayout<T, D>;
   constexpr bool kBf16 = sizeof(T) == 2;
   constexpr int kFrag = kBf16 ? D / 16 : D / 8;  // 16-byte pieces of a row per lane
@@ -51,75 +58,79 @@ __global__ __launch_bounds__(kNW * kWave) void chunk_scores(ScoreArgs a) {
   if (block0 >= s.len) return;
   const int pos0 = s.len - s.n_new;
   // per query head: this head's tokens; per kv head: (token, head) pairs
-  const int g = a.per_kv ? a.g : 1, head0 = kvh * a.g + (a.per_kv ? 0 : (int)blockIdx.y);
+  const int g = PER_KV ? a.g : 1, head0 = kvh * a.g + (PER_KV ? 0 : (int)blockIdx.y);
   const int first = max(0, block0 - pos0);  // the first token that sees a key of the workgroup
-  const int n_rows = (s.n_new - first) * g;
+  const int n_tokens = s.n_new - first, n_rows = n_tokens * g;
 
   uint4 kf[kFrag];
-  bool valid;
+  uint32_t exists;
   {
     const int key = key0 + (lane & 31);
     const int64_t off = key < s.len ? row_offset(a.kv, b, key) : -1;
-    valid = off >= 0;
-    const unsigned char *row = valid ? a.kv.k + off + (((uint64_t)kvh * a.kv.head_stride) << 4) : zero_row;
+    const unsigned char *row = off >= 0 ? a.kv.k + off + (((uint64_t)kvh * a.kv.head_stride) << 4) : zero_row;
 #pragma unroll
     for (int i = 0; i < kFrag; ++i)
       kf[i] = reinterpret_cast<const uint4 *>(row)[kBf16 ? 2 * i + half : half * kFrag + i];
+    exists = (uint32_t)__ballot(off >= 0);
   }
-  const uint32_t exists = (uint32_t)__ballot(valid);
 
   float acc[16];
 #pragma unroll
   for (int i = 0; i < 16; ++i) acc[i] = 0.0f;
 
-  // the lane's row of the looked-up tile: its queries, own cached row (-1: none)
-  // and the lse in log2 units (its rows beyond the last give no weight)
-  int64_t off;
-  int own;
-  float lse2;
-  auto lookup = [&](int r0) {
-    const int r = r0 + lane;
-    off = -1;
-    own = -1;
-    lse2 = 0.0f;
-    if (r < n_rows) {
-      const int i = first + (g == 1 ? r : r / g), h = head0 + (g == 1 ? 0 : r % g);
-      const int64_t t = s.first + i;
-      off = t * a.q_token + h * a.q_head;
-      lse2 = a.lse[t * a.hq + h] * kLog2e;
-      own = lse2 == -INFINITY ? -1 : pos0 + i;
+  // The lane's row of a tile: its token, head and lse, requested a tile ahead and
+  // not used before then.  Rows past the last repeat one that exists.
+  int row_token = PER_KV ? lane / g : lane, row_head = PER_KV ? lane % g : 0;
+  const int step_token = PER_KV ? kRows / g : kRows, step_head = PER_KV ? kRows % g : 0;
+  int token = 0, head = 0;
+  float lse = 0.0f;
+  const float *lse0 = a.lse + (int64_t)(s.first + first) * a.hq + head0;
+  auto lookup = [&]() {
+    token = row_token;
+    head = row_head;
+    lse = lse0[(int64_t)min(token, n_tokens - 1) * a.hq + head];
+    row_token += step_token;
+    row_head += step_head;
+    if (PER_KV && row_head >= g) {
+      row_head -= g;
+      ++row_token;
     }
   };
-  auto issue = [&](unsigned char *dst) {
+  // own: its cached row; -1, which gives no weight: past the last, or sees no key
+  int own = 0, own_now, r0 = 0;
+  float lse2 = 0.0f, lse_now;
+  const unsigned char *q = a.q + (s.first + first) * a.q_token + head0 * a.q_head;
+  auto issue = [&](unsigned char *dst, int row0) {
+    const bool dead = token >= n_tokens || lse == -INFINITY;
+    own = dead ? -1 : pos0 + first + token;
+    lse2 = dead ? 0.0f : lse * kLog2e;
     const int rr = lane / L::C, p = lane & (L::C - 1);
 #pragma unroll
     for (int j = 0; j < kInstr; ++j) {
       const int r = wave * kShare + j * kRpi + rr;
-      const int lo = __shfl((int)off, r, kWave), hi = __shfl((int)(off >> 32), r, kWave);
-      const int64_t o = ((int64_t)hi << 32) | (uint32_t)lo;
-      const unsigned char *src = hi < 0 ? zero_row : a.q + o;
-      load_to_lds16(src + ((p ^ L::swz_k(r)) << 4), dst + (wave * kShare + j * kRpi) * L::bytes);
+      uint64_t o;
+      if constexpr (PER_KV) {
+        const int from = __shfl(min(token, n_tokens - 1), r, kWave), h = __shfl(head, r, kWave);
+        o = (uint64_t)(uint32_t)from * (uint32_t)a.q_token + (uint64_t)(uint32_t)h * (uint32_t)a.q_head;
+      } else {
+        o = (uint64_t)(uint32_t)min(row0 + r, n_tokens - 1) * (uint32_t)a.q_token;
+      }
+      load_to_lds16(q + o + ((p ^ L::swz_k(r)) << 4), dst + (wave * kShare + j * kRpi) * L::bytes);
     }
   };
-  int r0 = 0, own_now, own_next = 0;
-  float lse_now, lse_next = 0.0f;
-  lookup(0);
   if (n_rows > 0) {
-    issue(q0);
-    own_next = own;
-    lse_next = lse2;
-    lookup(kRows);
+    lookup();
+    issue(q0, 0);
+    lookup();
   }
   auto turn = [&](unsigned char *sq, unsigned char *nq) {
     wait_memory();
     __syncthreads();
-    own_now = own_next;
-    lse_now = lse_next;
+    own_now = own;
+    lse_now = lse2;
     if (r0 + kRows < n_rows) {
-      issue(nq);
-      own_next = own;
-      lse_next = lse2;
-      lookup(r0 + 2 * kRows);
+      issue(nq, r0 + kRows);
+      lookup();
     }
 #pragma unroll
     for (int blk = 0; blk < kRows / 32; ++blk) {
@@ -130,7 +141,7 @@ __global__ __launch_bounds__(kNW * kWave) void chunk_scores(ScoreArgs a) {
 #pragma unroll
       for (int i = 0; i < kFrag; ++i) {
         const int c = kBf16 ? 2 * i + half : half * kFrag + i;
-        const uint4 w = *reinterpret_cast<const uint4 *>(sq + row * L::bytes + ((c ^ z) << 4));
+        const uint4 w = *reinterpret_cast<const uint4 *>(sq + (row * L::bytes + ((c ^ z) << 4)));
         if constexpr (kBf16) {
           x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, kf[i]),
                                                       __builtin_bit_cast(bf16x8_t, w), x, 0, 0, 0);
@@ -174,10 +185,144 @@ __global__ __launch_bounds__(kNW * kWave) void chunk_scores(ScoreArgs a) {
   // bits 4..1 of the lane are the register's bits 3..0
   const int i = (lane & 31) >> 1, in = 8 * (i / 4) + i % 4 + 4 * half, key = key0 + in;
   if (!(lane & 1) && key < s.len) {
-    const int64_t at = ((int64_t)b * (a.per_kv ? a.hkv : a.hq) + (a.per_kv ? kvh : head0)) * a.rows + key;
+    const int64_t at = ((int64_t)b * (PER_KV ? a.hkv : a.hq) + (PER_KV ? kvh : head0)) * a.rows + key;
     const float old = a.before && key < pos0 ? a.before[at] : 0.0f;
     a.out[at] = old + (exists >> in & 1u ? sum : 0.0f);
   }
+}
+
+template <typename T, int D>
+__global__ __launch_bounds__(kNW * kWave, 2) void few_scores(ScoreArgs a) {
+  constexpr bool kBf16 = sizeof(T) == 2;
+  constexpr int kFrag = kBf16 ? D / 16 : D / 8;  // 16-byte pieces of a row per lane
+  const int lane = threadIdx.x & (kWave - 1), half = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int units = a.c.batch * a.hkv, unit = blockIdx.x % units;
+  const int b = unit / a.hkv, kvh = unit % a.hkv;
+  const Seq s = sequence(a.c, b, a.kv.cap);
+  const int begin = (int)(blockIdx.x / units) * a.span, end = min(begin + a.span, s.len);
+  if (begin >= s.len) return;
+  const int pos0 = s.len - s.n_new, rows = s.n_new * a.g;
+  const unsigned char *k = a.kv.k + (((uint64_t)kvh * a.kv.head_stride) << 4);
+  // keys are looked up two blocks ahead and their rows requested one ahead
+  const int32_t *pages = a.kv.table ? a.kv.table + (int64_t)b * a.kv.width : a.c.len;
+  auto page_of = [&](int key) { return pages[min(key, s.len - 1) >> a.kv.shift]; };  // (dense: any word)
+  auto offset_of = [&](int key, int page) {
+    const int64_t off = page_offset(a.kv, a.kv.table ? page : b, key);
+    return key < end ? off : -1;
+  };
+  constexpr int step = 32 * kNW;
+  int key = begin + wave * 32 + (lane & 31);
+  int page = page_of(key), page_next = page_of(key + step);
+
+  // the lane's query row, and the lse (log2 units) and own cached row of the 16 rows
+  // whose logits it will hold
+  uint4 qf[kFrag];
+  {
+    const int r = lane & 31;
+    const int64_t t = s.first + r / a.g, h = kvh * a.g + r % a.g;
+    const unsigned char *row = r < rows ? a.q + t * a.q_token + h * a.q_head : zero_row;
+#pragma unroll
+    for (int i = 0; i < kFrag; ++i)
+      qf[i] = reinterpret_cast<const uint4 *>(row)[kBf16 ? 2 * i + half : half * kFrag + i];
+  }
+  float lse2[16];
+  int own[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const int r = 8 * (i / 4) + i % 4 + 4 * half;
+    lse2[i] = INFINITY;  // rows past the last, and rows that see no key, give no weight
+    own[i] = -1;
+    if (r < rows) {
+      const float x = a.lse[(int64_t)(s.first + r / a.g) * a.hq + kvh * a.g + r % a.g];
+      if (x != -INFINITY) {
+        lse2[i] = x * kLog2e;
+        own[i] = pos0 + r / a.g;
+      }
+    }
+  }
+  int64_t off = offset_of(key, page);
+  uint4 kf[kFrag];
+  auto load = [&]() {
+    const unsigned char *row = off >= 0 ? k + off : zero_row;
+#pragma unroll
+    for (int i = 0; i < kFrag; ++i)
+      kf[i] = reinterpret_cast<const uint4 *>(row)[kBf16 ? 2 * i + half : half * kFrag + i];
+  };
+  load();
+  for (int base = begin + wave * 32; base < end; base += step, key += step) {
+    f32x16_t x = {};
+#pragma unroll
+    for (int i = 0; i < kFrag; ++i) {
+      if constexpr (kBf16) {
+        x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, qf[i]),
+                                                    __builtin_bit_cast(bf16x8_t, kf[i]), x, 0, 0, 0);
+      } else {
+        const f32x4_t qa = __builtin_bit_cast(f32x4_t, qf[i]), ka = __builtin_bit_cast(f32x4_t, kf[i]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x = __builtin_amdgcn_mfma_f32_32x32x2f32(qa[e], ka[e], x, 0, 0, 0);
+      }
+    }
+    const bool exists = off >= 0, inside = key < end;
+    page = page_next;
+    off = offset_of(key + step, page);
+    load();
+    page_next = page_of(key + 2 * step);
+    float p[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], a.scale2, -lse2[i]));
+    if (base + 31 > pos0 || __any(!exists)) {  // some row may not see some key
+#pragma unroll
+      for (int i = 0; i < 16; ++i) p[i] = exists && key <= own[i] ? p[i] : 0.0f;
+    }
+    if (a.per_kv) {
+      float sum = 0.0f;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sum += p[i];
+      sum = swap_halves_sum(sum);
+      if (half == 0 && inside) {
+        const int64_t at = ((int64_t)b * a.hkv + kvh) * a.rows + key;
+        a.out[at] = (a.before && key < pos0 ? a.before[at] : 0.0f) + sum;
+      }
+    } else {
+      // rows of head j: j, j + g, j + 2g, ...
+      for (int j = 0; j < a.g; ++j) {
+        float sum = 0.0f;
+        if (s.n_new == 1) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) sum = j == 8 * (i / 4) + i % 4 + 4 * half ? p[i] : sum;
+        } else {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) sum += (8 * (i / 4) + i % 4 + 4 * half) % a.g == j ? p[i] : 0.0f;
+        }
+        sum = swap_halves_sum(sum);
+        if (half == 0 && inside) {
+          const int64_t at = ((int64_t)b * a.hq + kvh * a.g + j) * a.rows + key;
+          a.out[at] = (a.before && key < pos0 ? a.before[at] : 0.0f) + sum;
+        }
+      }
+    }
+  }
+}
+
+template <typename T, int D>
+void launch_typed(ScoreArgs a, int max_new, int max_len, hipStream_t st) {
+  const int64_t units = (int64_t)a.c.batch * a.hkv;
+  const dim3 block(kNW * kWave);
+  auto blocks = [&](int keys) { return (unsigned)(((int64_t)max_len + keys - 1) / keys * units); };
+  if ((int64_t)max_new * a.g <= 32) {
+    // two workgroups per CU, of whole rounds of 128 keys (a batch-16 step over up to
+    // 8192 rows: 9.6 us with 512, 11.6 with 1024, 12.1 with 256)
+    const int64_t rounds = ((int64_t)max_len + 127) / 128;
+    a.span = 128 * (int)std::max<int64_t>(1, std::min<int64_t>(rounds, rounds * units / 512));
+    hipLaunchKernelGGL((few_scores<T, D>), dim3(blocks(a.span)), block, 0, st, a);
+    return;
+  }
+  const dim3 grid(blocks(kKeys), a.per_kv ? 1 : a.g);
+  if (a.per_kv)
+    hipLaunchKernelGGL((chunk_scores<T, D, true>), grid, block, 0, st, a);
+  else
+    hipLaunchKernelGGL((chunk_scores<T, D, false>), grid, block, 0, st, a);
 }
 
 }  // namespace
@@ -201,17 +346,10 @@ hipError_t launch_chunk_scores(const smallkv_chunk_t &c, const smallkv_cache_t &
   a.out = out;
   a.rows = score_rows;
   a.scale2 = q.scale * kLog2e;
-  const dim3 grid((unsigned)((c.max_len + kKeys - 1) / kKeys * c.batch * kv.n_heads), a.per_kv ? 1 : a.g);
-  if (kv.dtype == SMALLKV_F32) {
-    if (kv.head_dim == 64)
-      hipLaunchKernelGGL((chunk_scores<float, 64>), grid, dim3(kNW * kWave), 0, st, a);
-    else
-      hipLaunchKernelGGL((chunk_scores<float, 128>), grid, dim3(kNW * kWave), 0, st, a);
-  } else if (kv.head_dim == 64) {
-    hipLaunchKernelGGL((chunk_scores<bf16_t, 64>), grid, dim3(kNW * kWave), 0, st, a);
-  } else {
-    hipLaunchKernelGGL((chunk_scores<bf16_t, 128>), grid, dim3(kNW * kWave), 0, st, a);
-  }
+  if (kv.dtype == SMALLKV_F32)
+    (kv.head_dim == 64 ? launch_typed<float, 64> : launch_typed<float, 128>)(a, c.max_new, c.max_len, st);
+  else
+    (kv.head_dim == 64 ? launch_typed<bf16_t, 64> : launch_typed<bf16_t, 128>)(a, c.max_new, c.max_len, st);
   return hipGetLastError();
 }
 
