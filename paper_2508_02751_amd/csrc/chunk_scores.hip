@@ -10,7 +10,9 @@
 //              exponential and one add each, which bound the pass; the product's
 //              matrix instructions run beside them.  Scores per query head: the heads
 //              are dealt to workgroups (blockIdx.y), each walking one head's tokens;
-//              per kv head: the rows are (token, head) pairs.
+//              per kv head: the rows are (token, head) pairs.  Where that makes too few
+//              workgroups (SPLIT), one owns 32 keys, its waves deal the rows among
+//              themselves without a barrier, and their sums are added at the end.
 //   few     -- no sequence has more than 32 (token, head) rows (a decode step): the
 //              rows stay in registers as the left operand of S = Q K^T, a lane holds
 //              one key's logits, and each wave streams its keys' rows, bound by
@@ -40,13 +42,14 @@ struct ScoreArgs {
 };
 
 constexpr float kLog2e = 1.4426950408889634074f;
-constexpr int kNW = 4, kKeys = 32 * kNW, kRows = 64;
+constexpr int kNW = 4;
 
-template <typename T, int D, bool PER_KV>
-__global__ __launch_bounds__(kNW * kWave, 2) void chunk_scores(ScoreArgs a) {
+template <typename T, int D, bool PER_KV, bool SPLIT>
+__global__ __launch_bounds__(kNW * kWave, SPLIT && sizeof(T) * D == 512 ? 1 : 2) void chunk_scores(ScoreArgs a) {
   using L = TileLayout<T, D>;
   constexpr bool kBf16 = sizeof(T) == 2;
   constexpr int kFrag = kBf16 ? D / 16 : D / 8;  // 16-byte pieces of a row per lane
+  constexpr int kKeys = SPLIT ? 32 : 32 * kNW, kRows = SPLIT ? 32 * kNW : 64;
   constexpr int kBuf = kRows * L::bytes, kShare = kRows / kNW, kRpi = 64 / L::C, kInstr = kShare / kRpi;
   __shared__ __align__(16) unsigned char q0[kBuf], q1[kBuf];
   const int lane = threadIdx.x & (kWave - 1), half = lane >> 5;
@@ -54,7 +57,7 @@ __global__ __launch_bounds__(kNW * kWave, 2) void chunk_scores(ScoreArgs a) {
   const int units = a.c.batch * a.hkv, unit = blockIdx.x % units;
   const int b = unit / a.hkv, kvh = unit % a.hkv;
   const Seq s = sequence(a.c, b, a.kv.cap);
-  const int block0 = (blockIdx.x / units) * kKeys, key0 = block0 + wave * 32;
+  const int block0 = (blockIdx.x / units) * kKeys, key0 = block0 + (SPLIT ? 0 : wave * 32);
   if (block0 >= s.len) return;
   const int pos0 = s.len - s.n_new;
   // per query head: this head's tokens; per kv head: (token, head) pairs
@@ -80,7 +83,8 @@ __global__ __launch_bounds__(kNW * kWave, 2) void chunk_scores(ScoreArgs a) {
 
   // The lane's row of a tile: its token, head and lse, requested a tile ahead and
   // not used before then.  Rows past the last repeat one that exists.
-  int row_token = PER_KV ? lane / g : lane, row_head = PER_KV ? lane % g : 0;
+  const int mine = SPLIT ? wave * 32 + (lane & 31) : lane;
+  int row_token = PER_KV ? mine / g : mine, row_head = PER_KV ? mine % g : 0;
   const int step_token = PER_KV ? kRows / g : kRows, step_head = PER_KV ? kRows % g : 0;
   int token = 0, head = 0;
   float lse = 0.0f;
@@ -110,7 +114,8 @@ __global__ __launch_bounds__(kNW * kWave, 2) void chunk_scores(ScoreArgs a) {
       const int r = wave * kShare + j * kRpi + rr;
       uint64_t o;
       if constexpr (PER_KV) {
-        const int from = __shfl(min(token, n_tokens - 1), r, kWave), h = __shfl(head, r, kWave);
+        const int at = SPLIT ? j * kRpi + rr : r;  // the lane whose row it is
+        const int from = __shfl(min(token, n_tokens - 1), at, kWave), h = __shfl(head, at, kWave);
         o = (uint64_t)(uint32_t)from * (uint32_t)a.q_token + (uint64_t)(uint32_t)h * (uint32_t)a.q_head;
       } else {
         o = (uint64_t)(uint32_t)min(row0 + r, n_tokens - 1) * (uint32_t)a.q_token;
@@ -125,7 +130,7 @@ __global__ __launch_bounds__(kNW * kWave, 2) void chunk_scores(ScoreArgs a) {
   }
   auto turn = [&](unsigned char *sq, unsigned char *nq) {
     wait_memory();
-    __syncthreads();
+    if (!SPLIT) __syncthreads();
     own_now = own;
     lse_now = lse2;
     if (r0 + kRows < n_rows) {
@@ -133,10 +138,10 @@ __global__ __launch_bounds__(kNW * kWave, 2) void chunk_scores(ScoreArgs a) {
       lookup();
     }
 #pragma unroll
-    for (int blk = 0; blk < kRows / 32; ++blk) {
-      const int row = 32 * blk + (lane & 31), z = L::swz_k(row);
-      const int o = __shfl(own_now, row, kWave);
-      const float base = __shfl(lse_now, row, kWave);
+    for (int blk = 0; blk < (SPLIT ? 1 : kRows / 32); ++blk) {
+      const int row = 32 * (SPLIT ? wave : blk) + (lane & 31), z = L::swz_k(row);
+      const int o = SPLIT ? own_now : __shfl(own_now, row, kWave);
+      const float base = SPLIT ? lse_now : __shfl(lse_now, row, kWave);
       f32x16_t x = {};
 #pragma unroll
       for (int i = 0; i < kFrag; ++i) {
@@ -181,7 +186,17 @@ __global__ __launch_bounds__(kNW * kWave, 2) void chunk_scores(ScoreArgs a) {
         acc[i] = keep + __shfl_xor(send, o, kWave);
       }
   }
-  const float sum = acc[0] + __shfl_xor(acc[0], 1, kWave);
+  float sum = acc[0] + __shfl_xor(acc[0], 1, kWave);
+  if (SPLIT) {
+    float *part = reinterpret_cast<float *>(q0);
+    wait_memory();
+    __syncthreads();
+    part[threadIdx.x] = sum;
+    __syncthreads();
+    if (wave > 0) return;
+#pragma unroll
+    for (int w = 1; w < kNW; ++w) sum += part[w * kWave + lane];
+  }
   // bits 4..1 of the lane are the register's bits 3..0
   const int i = (lane & 31) >> 1, in = 8 * (i / 4) + i % 4 + 4 * half, key = key0 + in;
   if (!(lane & 1) && key < s.len) {
@@ -305,6 +320,10 @@ __global__ __launch_bounds__(kNW * kWave, 2) void few_scores(ScoreArgs a) {
   }
 }
 
+template <typename T, int D, bool PER_KV, bool SPLIT> void launch_chunk(const ScoreArgs &a, dim3 grid, hipStream_t st) {
+  hipLaunchKernelGGL((chunk_scores<T, D, PER_KV, SPLIT>), grid, dim3(kNW * kWave), 0, st, a);
+}
+
 template <typename T, int D>
 void launch_typed(ScoreArgs a, int max_new, int max_len, hipStream_t st) {
   const int64_t units = (int64_t)a.c.batch * a.hkv;
@@ -318,11 +337,13 @@ void launch_typed(ScoreArgs a, int max_new, int max_len, hipStream_t st) {
     hipLaunchKernelGGL((few_scores<T, D>), dim3(blocks(a.span)), block, 0, st, a);
     return;
   }
-  const dim3 grid(blocks(kKeys), a.per_kv ? 1 : a.g);
-  if (a.per_kv)
-    hipLaunchKernelGGL((chunk_scores<T, D, true>), grid, block, 0, st, a);
-  else
-    hipLaunchKernelGGL((chunk_scores<T, D, false>), grid, block, 0, st, a);
+  const unsigned heads = a.per_kv ? 1 : a.g;
+  // with less than a workgroup per CU (2048 tokens over 8192 rows, two kv heads, 128
+  // workgroups: 175 us, split 84; 512 tokens, four, 256 workgroups: 68, split 72)
+  const bool split = blocks(32 * kNW) * (int64_t)heads < 256;
+  const dim3 grid(blocks(split ? 32 : 32 * kNW), heads);
+  (split ? a.per_kv ? launch_chunk<T, D, true, true> : launch_chunk<T, D, false, true>
+   : a.per_kv ? launch_chunk<T, D, true, false> : launch_chunk<T, D, false, false>)(a, grid, st);
 }
 
 }  // namespace

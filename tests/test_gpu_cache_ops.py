@@ -111,6 +111,27 @@ def test_chunk_scores(case, per_kv):
         within(zero[b, :, :n], want0[b, :, :n], tol0[b, :, :n], "from zero")
 
 
+@pytest.mark.parametrize("per_kv", [False, True])
+@pytest.mark.parametrize("dtype,d", [(BF16, 64), (F32, 128)])
+def test_chunk_scores_with_many_workgroups(dtype, d, per_kv):
+    """Enough of them that a workgroup's waves own different keys."""
+    S = lib()
+    lens = [(n, new) for n, new in ((1100, 60), (700, 700), (33, 7), (1024, 129))] * 8
+    c = R.Case(lens, 8, 2, d, dtype, 64, seed=41)
+    chunk, cache, q = c.to(DEV)
+    _, wl, _, _ = R.attention(c)
+    lse = wl.float()
+    before = torch.rand(c.B, c.hk if per_kv else c.hq, c.rows, generator=c.gen)
+    out = torch.full(before.shape, 7.0, device=DEV)
+    log(f"[scores] many {dtype} {per_kv}")
+    S.prepare_chunk_scores(chunk, cache, q, lse.to(DEV), c.scale, out, before=before.to(DEV)).run()
+    torch.cuda.synchronize()
+    want, tol = R.scores(c, lse, before, per_kv)
+    for b, (n, _) in enumerate(c.lens):
+        within(out[b, :, :n], want[b, :, :n], tol[b, :, :n], f"sequence {b}")
+        assert bool((out[b, :, n:] == 7).all())
+
+
 def test_scores_add_up_to_the_query_rows():
     """Each query row's weights sum to 1: attention's lse and the scores agree."""
     S = lib()
