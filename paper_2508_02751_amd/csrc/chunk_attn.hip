@@ -18,9 +18,10 @@
 // Two forms:
 //   many rows -- NW waves of 32 rows each share every tile of rows in LDS;
 //                tiles are double-buffered, copied from memory to LDS directly;
-//   few rows  -- where no sequence has more than 32 rows (a decode step): one
-//                column of 32 rows, each wave walks its own tiles of 32 keys,
-//                without a barrier, and the waves' results are joined at the end.
+//   few rows  -- where no sequence has more than 32 rows (16 in fp32; a decode
+//                step): one column of rows, each wave walks its own tiles of 32 (16)
+//                keys, without a barrier, and the waves' results are joined at the
+//                end.
 // Where the (tile, kv head) pairs are too few to fill the GPU the cached rows are
 // cut into spans, and attn_merge joins their records.  The span is found on the
 // device from the sequences' own lengths, as the shortest with which the spans of
@@ -81,40 +82,38 @@ __device__ __forceinline__ int spans_of(int len, int span) {
   return span == kWhole ? 1 : max((len + span - 1) / span, 1);
 }
 
-// The shortest span, in steps of `round` rows, with which all units fit `splits`;
-// kWhole where the tiles alone do not.  The first 64 sequences are in `n` (tiles)
-// and `len` of each lane, the others are read again.
-template <int BM> __device__ __forceinline__ int find_span(const AttnArgs &a, int round) {
-  if (!a.splits) return kWhole;
-  const int lane = threadIdx.x & (kWave - 1);
-  int tiles0 = 0, len0 = 0;
-  auto each = [&](auto &&use) {
-    for (int b0 = 0; b0 < a.c.batch; b0 += kWave) {
-      int n = tiles0, len = len0;
-      if (b0 > 0) {
-        n = len = 0;
-        if (b0 + lane < a.c.batch) {
-          const Seq s = sequence(a.c, b0 + lane, a.kv.cap);
-          n = (s.n_new * a.g + BM - 1) / BM;
-          len = s.len;
-        }
-      }
-      use(n, len);
-    }
-  };
-  if (lane < a.c.batch) {
-    const Seq s = sequence(a.c, lane, a.kv.cap);
-    tiles0 = (s.n_new * a.g + BM - 1) / BM;
-    len0 = s.len;
+// The sequences of a batch, one per lane: the first 64 stay in registers, the others
+// are read again by every pass.
+template <int BM> struct Lanes {
+  Seq s0;
+
+  __device__ __forceinline__ static Seq read(const AttnArgs &a, int b) {
+    return b < a.c.batch ? sequence(a.c, b, a.kv.cap) : Seq{0, 0, 0};
   }
-  int tiles = 0;
+  __device__ __forceinline__ explicit Lanes(const AttnArgs &a) : s0(read(a, threadIdx.x & (kWave - 1))) {}
+  __device__ __forceinline__ static int tiles(const AttnArgs &a, const Seq &s) {
+    return (s.n_new * a.g + BM - 1) / BM;
+  }
+  template <typename F> __device__ __forceinline__ void each(const AttnArgs &a, F &&use) const {
+    for (int b0 = 0; b0 < a.c.batch; b0 += kWave) {
+      const Seq s = b0 ? read(a, b0 + (int)(threadIdx.x & (kWave - 1))) : s0;
+      if (use(b0, s, tiles(a, s))) return;
+    }
+  }
+};
+
+// The shortest span, in steps of `round` rows, with which all units fit `splits`;
+// kWhole where the tiles alone do not.
+template <int BM> __device__ __forceinline__ int find_span(const AttnArgs &a, const Lanes<BM> &lanes, int round) {
+  if (!a.splits) return kWhole;
+  int tiles = 0, longest = 0;
   float work = 0.0f;  // cached rows over all tiles, in steps of `round`
-  int longest = 0;
-  each([&](int n, int len) {
+  lanes.each(a, [&](int, const Seq &s, int n) {
     tiles += last_lane(wave_scan(n));
-    const int steps = (len + round - 1) / round;
-    longest = max(longest, (int)wave_max(n ? (float)steps : 0.0f));
-    work += wave_sum((float)n * (float)steps);
+    const float steps = n ? (float)((s.len + round - 1) / round) : 0.0f;
+    longest = max(longest, (int)wave_max(steps));
+    work += wave_sum((float)n * steps);
+    return false;
   });
   if (tiles >= a.splits) return kWhole;
   // between work / splits, and work / (splits - tiles): there they fit for sure
@@ -122,7 +121,10 @@ template <int BM> __device__ __forceinline__ int find_span(const AttnArgs &a, in
   while (lo < hi) {
     const int mid = (lo + hi) >> 1;
     int units = 0;
-    each([&](int n, int len) { units += last_lane(wave_scan(n * spans_of(len, mid * round))); });
+    lanes.each(a, [&](int, const Seq &s, int n) {
+      units += last_lane(wave_scan(n * spans_of(s.len, mid * round)));
+      return false;
+    });
     if (units <= a.splits)
       hi = mid;
     else
@@ -133,43 +135,40 @@ template <int BM> __device__ __forceinline__ int find_span(const AttnArgs &a, in
 
 // Units (or tiles) are numbered sequence by sequence, tile by tile and span by span;
 // the last rows of a sequence, which see the most keys, come first.
-template <int BM, bool UNITS> __device__ __forceinline__ bool locate(const AttnArgs &a, int span, int flat, Tile &t) {
-  const int lane = threadIdx.x & (kWave - 1);
+template <int BM, bool UNITS>
+__device__ __forceinline__ bool locate(const AttnArgs &a, const Lanes<BM> &lanes, int span, int flat, Tile &t) {
   int unit = 0;  // of the sequences before
-  for (int b0 = 0; b0 < a.c.batch; b0 += kWave) {
-    int n = 0, ns = 0;
-    if (b0 + lane < a.c.batch) {
-      const Seq s = sequence(a.c, b0 + lane, a.kv.cap);
-      n = (s.n_new * a.g + BM - 1) / BM;
-      ns = spans_of(s.len, span);
-    }
+  bool found = false;
+  lanes.each(a, [&](int b0, const Seq &s, int n) {
+    const int ns = spans_of(s.len, span);
     const int units = wave_scan(n * ns), x = UNITS ? units : wave_scan(n);
     const uint64_t m = __ballot(x > flat);
-    if (m) {
-      const int l = __builtin_amdgcn_readfirstlane(__ffsll((long long)m) - 1);
-      const int tiles = __builtin_amdgcn_readlane(n, l);
-      t.b = b0 + l;
-      t.n_split = __builtin_amdgcn_readlane(ns, l);
-      const int per = UNITS ? t.n_split : 1, in = flat - (__builtin_amdgcn_readlane(x, l) - tiles * per);
-      const int tile = in / per;
-      t.split = in - tile * per;
-      t.unit0 = unit + __builtin_amdgcn_readlane(units, l) - (tiles - tile) * t.n_split;
-      t.row0 = (tiles - 1 - tile) * BM;
-      t.s = sequence(a.c, t.b, a.kv.cap);
-      t.rows = t.s.n_new * a.g;
-      return true;
+    if (!m) {
+      flat -= last_lane(x);
+      unit += last_lane(units);
+      return false;
     }
-    flat -= last_lane(x);
-    unit += last_lane(units);
-  }
-  return false;
+    const int l = __builtin_amdgcn_readfirstlane(__ffsll((long long)m) - 1);
+    auto of = [&](int v) { return __builtin_amdgcn_readlane(v, l); };
+    const int tiles = of(n);
+    t.b = b0 + l;
+    t.s = Seq{of(s.first), of(s.n_new), of(s.len)};
+    t.n_split = of(ns);
+    const int per = UNITS ? t.n_split : 1, in = flat - (of(x) - tiles * per), tile = in / per;
+    t.split = in - tile * per;
+    t.unit0 = unit + of(units) - (tiles - tile) * t.n_split;
+    t.row0 = (tiles - 1 - tile) * BM;
+    t.rows = t.s.n_new * a.g;
+    found = true;
+    return true;
+  });
+  return found;
 }
 
 // A wave's share of the copies of one tile of rows.  The page of the lane's row is
 // looked up a tile ahead (without a branch: the value must not be needed before
 // then); the rows' offsets are then passed between lanes.
-template <typename T, int D, int BN, int SHARE> struct Loader {
-  using L = TileLayout<T, D>;
+template <typename L, int BN, int SHARE> struct Loader {
   static constexpr int kRpi = 64 / L::C;        // rows per instruction
   static constexpr int kInstr = SHARE / kRpi;   // instructions per wave, K or V
   static_assert(SHARE % kRpi == 0 && kInstr >= 1, "a wave copies whole instructions");
@@ -418,21 +417,23 @@ __device__ __forceinline__ void masked_tile(State<T, D> &st, const QFrag<T, D> &
   }
 }
 
-// Adds the infinite and NaN values of keys from..to to the lane's own elements of
-// an output row that is written already (any weight > 0 leaves them what they are).
+// Adds the infinite and NaN values of keys from..to to the lane's own elements (groups
+// of four, `step` apart from `at` on) of an output row that is written already (any
+// weight > 0 leaves them what they are).
 template <typename O, typename T, int D>
-__device__ __forceinline__ void give_back(const AttnArgs &a, int b, const unsigned char *v, void *out, int from, int to) {
-  const int half = (threadIdx.x & (kWave - 1)) >> 5;
+__device__ __forceinline__ void give_back(const AttnArgs &a, int b, const unsigned char *v, void *out, int from, int to,
+                                          int at, int step) {
 #pragma unroll 1
   for (int key = from; key <= to; ++key) {
     const int64_t off = row_offset(a.kv, b, key);
     if (off < 0) continue;
 #pragma unroll 1
-    for (int i = 0; i < D / 2; ++i) {
-      const int e = 8 * (i / 4) + i % 4 + 4 * half;
-      const float x = elem<T>::load1(v + off, e);
-      if (!(fabsf(x) <= 3.402823466e38f)) elem<O>::store1(out, e, elem<O>::load1(out, e) + x);
-    }
+    for (int e0 = at; e0 < D; e0 += step)
+#pragma unroll 1
+      for (int e = e0; e < e0 + 4; ++e) {
+        const float x = elem<T>::load1(v + off, e);
+        if (!(fabsf(x) <= 3.402823466e38f)) elem<O>::store1(out, e, elem<O>::load1(out, e) + x);
+      }
   }
 }
 
@@ -447,9 +448,10 @@ template <int BM> struct Share {
 
   __device__ __forceinline__ bool find(const AttnArgs &a, int block, int round, int wave_row) {
     kvh = block % a.hkv;
-    const int span = find_span<BM>(a, round);
+    const Lanes<BM> lanes(a);
+    const int span = find_span<BM>(a, lanes, round);
     if (a.splits && block == 0 && threadIdx.x == 0) *a.span = span;
-    if (!locate<BM, true>(a, span, block / a.hkv, t)) return false;
+    if (!locate<BM, true>(a, lanes, span, block / a.hkv, t)) return false;
     unit = block;
     const int pos0 = t.s.len - t.s.n_new;  // cached row of the first new token
     const int last = min(t.row0 + BM, t.rows) - 1;
@@ -457,7 +459,7 @@ template <int BM> struct Share {
     begin = t.split * span;  // (one span: 0)
     end = min(limit, begin + span);
     if (begin >= limit && t.split > 0) return false;  // (attn_merge reads no record of it)
-    r = t.row0 + wave_row + (int)(threadIdx.x & 31);
+    r = t.row0 + wave_row + (int)(threadIdx.x & (BM < 32 ? BM - 1 : 31));
     live = r < t.rows;
     const int rc = live ? r : t.rows - 1;
     token = t.s.first + rc / a.g;
@@ -470,46 +472,50 @@ template <int BM> struct Share {
   }
 };
 
-// The lane's row of the output, or of the span's record.  taken: values were taken
-// out of a tile of BN keys.
-template <typename T, int D, int BM, int BN>
-__device__ __forceinline__ void write_row(const AttnArgs &a, const Share<BM> &w, const State<T, D> &st, bool taken) {
-  if (!w.live) return;
-  const float l = swap_halves_sum(st.l);
-  const int half = (threadIdx.x & (kWave - 1)) >> 5;
+// The lane's part of a row of the output, or of the span's record: N groups of four
+// elements of o, `step` apart from `at` on, l the row's sum.  writes: one lane per row;
+// taken: values were taken out of a tile of BN keys.
+template <typename T, int D, int BM, int BN, int N>
+__device__ __forceinline__ void write_row(const AttnArgs &a, const Share<BM> &w, const f32x4_t (&x)[N], float m, float l,
+                                          int at, int step, bool writes, bool taken) {
   const int from = max(w.begin, w.first_own + 2 - BN), to = min(w.end - 1, w.own);
   if (w.t.n_split > 1) {
     const int64_t row = (int64_t)w.unit * BM + (w.r - w.t.row0);
     float *o = a.rec + row * D;
 #pragma unroll
-    for (int d = 0; d < D / 32; ++d)
-#pragma unroll
-      for (int i = 0; i < 16; i += 4)
-        *reinterpret_cast<f32x4_t *>(o + d * 32 + 2 * i + 4 * half) =
-            f32x4_t{st.o[d][i], st.o[d][i + 1], st.o[d][i + 2], st.o[d][i + 3]};
-    if (half == 0) {
-      a.rec[a.rec_ml + 2 * row] = st.m;
+    for (int i = 0; i < N; ++i) *reinterpret_cast<f32x4_t *>(o + at + i * step) = x[i];
+    if (writes) {
+      a.rec[a.rec_ml + 2 * row] = m;
       a.rec[a.rec_ml + 2 * row + 1] = l;
     }
-    if (taken) give_back<float, T, D>(a, w.t.b, w.v, o, from, to);
+    if (taken) give_back<float, T, D>(a, w.t.b, w.v, o, from, to, at, step);
     return;
   }
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;  // (0: the row sees no key)
   unsigned char *o = a.out + (w.token * a.o_token + w.head * a.o_head) * (int64_t)sizeof(T);
 #pragma unroll
-  for (int d = 0; d < D / 32; ++d)
+  for (int i = 0; i < N; ++i) {
+    const f32x4_t y = x[i] * inv;
+    if constexpr (sizeof(T) == 4)
+      *reinterpret_cast<f32x4_t *>(o + (at + i * step) * 4) = y;
+    else
+      *reinterpret_cast<bf16x4_t *>(o + (at + i * step) * 2) = __builtin_convertvector(y, bf16x4_t);
+  }
+  if (taken) give_back<T, T, D>(a, w.t.b, w.v, o, from, to, at, step);
+  if (a.lse && writes)
+    a.lse[(int64_t)w.token * a.hq + w.head] = l == 0.0f ? -INFINITY : (m + __log2f(l)) * kLn2;
+}
+
+template <typename T, int D, int BM, int BN>
+__device__ __forceinline__ void write_row(const AttnArgs &a, const Share<BM> &w, const State<T, D> &st, bool taken) {
+  if (!w.live) return;
+  const float l = swap_halves_sum(st.l);
+  const int half = (threadIdx.x & (kWave - 1)) >> 5;
+  f32x4_t x[D / 8];
 #pragma unroll
-    for (int i = 0; i < 16; i += 4) {
-      const f32x4_t x = f32x4_t{st.o[d][i], st.o[d][i + 1], st.o[d][i + 2], st.o[d][i + 3]} * inv;
-      const int e = d * 32 + 2 * i + 4 * half;
-      if constexpr (sizeof(T) == 4)
-        *reinterpret_cast<f32x4_t *>(o + e * 4) = x;
-      else
-        *reinterpret_cast<bf16x4_t *>(o + e * 2) = __builtin_convertvector(x, bf16x4_t);
-    }
-  if (taken) give_back<T, T, D>(a, w.t.b, w.v, o, from, to);
-  if (a.lse && half == 0)
-    a.lse[(int64_t)w.token * a.hq + w.head] = l == 0.0f ? -INFINITY : (st.m + __log2f(l)) * kLn2;
+  for (int i = 0; i < D / 8; ++i)
+    x[i] = f32x4_t{st.o[i / 4][i % 4 * 4], st.o[i / 4][i % 4 * 4 + 1], st.o[i / 4][i % 4 * 4 + 2], st.o[i / 4][i % 4 * 4 + 3]};
+  write_row<T, D, BM, BN>(a, w, x, st.m, l, 4 * half, 8, half == 0, taken);
 }
 
 // Infinite and NaN values of a tile are taken out of it where some row does not see
@@ -545,7 +551,7 @@ __global__ __launch_bounds__(NW * kWave, sizeof(T) == 2 ? 2 : 1) void attn_many(
   st.clear();
   constexpr uint64_t kAll = BN == 64 ? ~0ull : (1ull << (BN & 63)) - 1;
   int row = w.begin;
-  Loader<T, D, BN, kRows> ld;
+  Loader<L, BN, kRows> ld;
   ld.init(a, w.t.b, w.end);
   ld.lookup(a.kv, row);
   uint64_t valid = 0;
@@ -608,14 +614,16 @@ __device__ __forceinline__ void wait_lds() {
   asm volatile("" ::: "memory");
 }
 
-template <typename T, int D, int NW>
-__global__ __launch_bounds__(NW * kWave, sizeof(T) == 2 || D == 64 ? 2 : 1) void attn_few(AttnArgs a) {
+constexpr int kFewWaves = 4;
+
+template <int D> __global__ __launch_bounds__(kFewWaves * kWave, 2) void attn_few_bf16(AttnArgs a) {
+  using T = bf16_t;
   using L = TileLayout<T, D>;
-  constexpr int BN = 32, kTile = BN * L::bytes;
+  constexpr int NW = kFewWaves, BN = 32, kTile = BN * L::bytes;
   // one tile of keys and one of values per wave: the next keys are requested when
   // this tile's are multiplied, the next values after this tile's
   __shared__ __align__(16) unsigned char k0[NW * kTile], v0[NW * kTile];
-  __shared__ float ml[2][(NW + 1) / 2][kWave];
+  __shared__ float ml[2][NW / 2][kWave];
   const int lane = threadIdx.x & (kWave - 1);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   Share<32> w;
@@ -623,7 +631,7 @@ __global__ __launch_bounds__(NW * kWave, sizeof(T) == 2 || D == 64 ? 2 : 1) void
   unsigned char *sk = k0 + wave * kTile, *sv = v0 + wave * kTile;
   constexpr int step = NW * BN;
   int row = w.begin + wave * BN;
-  using Ld = Loader<T, D, BN, BN>;
+  using Ld = Loader<L, BN, BN>;
   Ld ld;
   ld.init(a, w.t.b, w.end);
   ld.lookup(a.kv, row);
@@ -703,6 +711,153 @@ __global__ __launch_bounds__(NW * kWave, sizeof(T) == 2 || D == 64 ? 2 : 1) void
   if (wave == 0) write_row<T, D, 32, BN>(a, w, st, taken);
 }
 
+// The same in fp32, on 16 x 16 tiles: a quarter-wave holds a quarter of the head
+// dimension of the logits' product, and 4 keys of the 16 in registers.
+template <int D> struct FewLayout : TileLayout<float, D> {
+  // values are read 64 bytes of rows 4 apart at once
+  __device__ __forceinline__ static int swz_v(int r) { return (r >> 2 & 3) << 2; }
+};
+
+template <int D> __global__ __launch_bounds__(kFewWaves * kWave, 2) void attn_few_f32(AttnArgs a) {
+  using T = float;
+  using L = FewLayout<D>;
+  constexpr int NW = kFewWaves, BN = 16, kTile = BN * L::bytes, kBlocks = D / 16;
+  __shared__ __align__(16) unsigned char k0[NW * kTile], v0[NW * kTile];
+  __shared__ float ml[2][NW / 2][kWave];
+  const int lane = threadIdx.x & (kWave - 1), quarter = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  Share<16> w;
+  if (!w.find(a, blockIdx.x, NW * BN, 0)) return;
+  unsigned char *sk = k0 + wave * kTile, *sv = v0 + wave * kTile;
+  constexpr int step = NW * BN;
+  int row = w.begin + wave * BN;
+  using Ld = Loader<L, BN, BN>;
+  Ld ld;
+  ld.init(a, w.t.b, w.end);
+  ld.lookup(a.kv, row);
+  f32x4_t q[kBlocks];
+  const float *qrow = reinterpret_cast<const float *>(a.q) + w.token * a.q_token + w.head * a.q_head + quarter * (D / 4);
+#pragma unroll
+  for (int i = 0; i < kBlocks; ++i) q[i] = reinterpret_cast<const f32x4_t *>(qrow)[i];
+  float m = -INFINITY, l = 0.0f;
+  f32x4_t o[kBlocks] = {};
+  wait_copies<0>();  // the queries and the first page number, requested together
+  int64_t off = ld.offset(a.kv, w.t.b, row);
+  bool taken = false;
+  // the next page number is looked up on the way, and the next keys (while this tile's
+  // logits wait for their values) and values requested, if there are any
+  auto logits = [&]() {
+    f32x4_t s[4] = {};
+    const unsigned char *at = sk + (lane & 15) * L::bytes;
+#pragma unroll
+    for (int i = 0; i < kBlocks; ++i) {
+      const f32x4_t k = *reinterpret_cast<const f32x4_t *>(at + (((quarter * kBlocks + i) ^ L::swz_k(lane & 15)) << 4));
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(k[e], q[i][e], s[e], 0, 0, 0);
+    }
+    return (s[0] + s[1]) + (s[2] + s[3]);
+  };
+  auto weigh = [&](f32x4_t &s) {
+    float mx = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
+    mx = swap_halves_max(fmaxf(mx, __shfl_xor(mx, 16, kWave))) * a.scale2;
+    if (__any(mx > m + 8.0f)) {
+      const float top = fmaxf(m, mx), f = __builtin_amdgcn_exp2f(m - (top == -INFINITY ? 0.0f : top));
+      m = top;
+      l *= f;
+#pragma unroll
+      for (int d = 0; d < kBlocks; ++d) o[d] *= f;
+    }
+    const float base = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float x = __builtin_fmaf(fmaxf(s[i], -3.402823466e38f), a.scale2_lo, -base);
+      s[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], a.scale2, x));
+      l += s[i];
+    }
+  };
+  auto values = [&](const f32x4_t &p) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int r = 4 * quarter + i;
+#pragma unroll
+      for (int d = 0; d < kBlocks; ++d) {
+        const int c = d * 4 + ((lane & 15) >> 2);
+        const float v = *reinterpret_cast<const float *>(sv + (r * L::bytes + ((c ^ L::swz_v(r)) << 4) + (lane & 3) * 4));
+        o[d] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, p[i], o[d], 0, 0, 0);
+      }
+    }
+  };
+  auto masked = [&]() {
+    wait_memory();
+    if (min(row + BN, w.end) - 1 > w.first_own) {
+      taken |= __any(take_out<T, BN * L::C>(sv, lane, kWave));
+      wait_lds();
+    }
+    f32x4_t s = logits();
+    const uint32_t valid = (uint32_t)__ballot(off >= 0) >> (4 * quarter);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s[i] = (valid >> i & 1u) && row + 4 * quarter + i <= w.own ? s[i] : -INFINITY;
+    weigh(s);
+    values(s);
+  };
+  if (row < w.end) {
+    Ld::template issue_one<false>(off, w.k, sk);
+    ld.lookup(a.kv, row + step);
+    Ld::template issue_one<true>(off, w.v, sv);
+    for (; row + step < w.end; row += step) {  // (copies as in attn_few_bf16)
+      if (row + BN - 1 <= w.first_own && __ballot(off >= 0) == ~0ull) {
+        wait_copies<Ld::kInstr>();
+        f32x4_t s = logits();
+        wait_lds();
+        off = ld.offset(a.kv, w.t.b, row + step);
+        Ld::template issue_one<false>(off, w.k, sk);
+        weigh(s);
+        wait_copies<Ld::kInstr>();
+        values(s);
+      } else {
+        masked();
+        wait_lds();
+        off = ld.offset(a.kv, w.t.b, row + step);
+        Ld::template issue_one<false>(off, w.k, sk);
+      }
+      wait_lds();
+      ld.lookup(a.kv, row + 2 * step);
+      Ld::template issue_one<true>(off, w.v, sv);
+    }
+    masked();
+  }
+  taken = __syncthreads_or(taken);
+  float *x = reinterpret_cast<float *>(k0);
+#pragma unroll
+  for (int h = NW / 2; h >= 1; h >>= 1) {
+    __syncthreads();
+    float *y = x + (wave & (h - 1)) * (D / 4) * kWave;
+    if (wave >= h && wave < 2 * h) {
+      ml[0][wave - h][lane] = m;
+      ml[1][wave - h][lane] = l;
+#pragma unroll
+      for (int d = 0; d < kBlocks; ++d)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[(d * 4 + i) * kWave + lane] = o[d][i];
+    }
+    __syncthreads();
+    if (wave < h) {
+      const float om = ml[0][wave][lane], ol = ml[1][wave][lane];
+      const float top = fmaxf(m, om), base = top == -INFINITY ? 0.0f : top;
+      const float f = __builtin_amdgcn_exp2f(m - base), fo = __builtin_amdgcn_exp2f(om - base);
+      m = top;
+      l = l * f + ol * fo;
+#pragma unroll
+      for (int d = 0; d < kBlocks; ++d)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[d][i] = o[d][i] * f + y[(d * 4 + i) * kWave + lane] * fo;
+    }
+  }
+  if (wave > 0) return;
+  l = swap_halves_sum(l + __shfl_xor(l, 16, kWave));
+  if (w.live) write_row<T, D, 16, BN>(a, w, o, m, l, 4 * quarter, 16, quarter == 0, taken);
+}
+
 // Joins the records of a tile's spans: four elements of a row per lane, all spans in
 // one pass with the running maximum, so that their loads are in flight together.
 template <int D> constexpr int merge_rows() { return 256 / (D / 4); }  // per workgroup
@@ -710,8 +865,9 @@ template <int D> constexpr int merge_rows() { return 256 / (D / 4); }  // per wo
 template <typename T, int D, int BM>
 __global__ __launch_bounds__(256) void attn_merge(AttnArgs a) {
   const int kvh = blockIdx.x % a.hkv, span = *a.span;
+  const Lanes<BM> lanes(a);
   Tile t;
-  if (span == kWhole || !locate<BM, false>(a, span, blockIdx.x / a.hkv, t) || t.n_split == 1) return;
+  if (span == kWhole || !locate<BM, false>(a, lanes, span, blockIdx.x / a.hkv, t) || t.n_split == 1) return;
   const int in = blockIdx.y * merge_rows<D>() + threadIdx.x / (D / 4), e = threadIdx.x % (D / 4) * 4;
   const int r = t.row0 + in;
   if (r >= t.rows) return;
@@ -745,17 +901,19 @@ __global__ __launch_bounds__(256) void attn_merge(AttnArgs a) {
 
 template <typename T, int D> hipError_t launch_typed(AttnArgs a, const AttnPlan &p, hipStream_t st) {
   constexpr bool h = sizeof(T) == 2;
-  constexpr int NF = h ? 4 : 2, BM = kAttnWaves * 32;
+  constexpr int BM = kAttnWaves * 32, BF = h ? 32 : 16;
   const dim3 grid(p.units * a.hkv), merge(p.tiles * a.hkv, p.rows / merge_rows<D>());
   a.rec_ml = (int64_t)p.units * a.hkv * p.rows * D;
-  if (p.few)
-    hipLaunchKernelGGL((attn_few<T, D, NF>), grid, dim3(NF * kWave), 0, st, a);
-  else
+  if (!p.few)
     hipLaunchKernelGGL((attn_many<T, D, kAttnWaves, h ? 64 : 32>), grid, dim3(kAttnWaves * kWave), 0, st, a);
+  else if constexpr (h)
+    hipLaunchKernelGGL((attn_few_bf16<D>), grid, dim3(kFewWaves * kWave), 0, st, a);
+  else
+    hipLaunchKernelGGL((attn_few_f32<D>), grid, dim3(kFewWaves * kWave), 0, st, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || !p.splits) return e;
   if (p.few)
-    hipLaunchKernelGGL((attn_merge<T, D, 32>), merge, dim3(256), 0, st, a);
+    hipLaunchKernelGGL((attn_merge<T, D, BF>), merge, dim3(256), 0, st, a);
   else
     hipLaunchKernelGGL((attn_merge<T, D, BM>), merge, dim3(256), 0, st, a);
   return hipGetLastError();
@@ -771,17 +929,20 @@ AttnPlan plan_chunk_attn(const smallkv_chunk_t &c, const smallkv_cache_t &kv, co
   AttnPlan p{};
   const int g = q.n_heads / kv.n_heads;
   const int64_t rows = (int64_t)c.max_new * g;
-  p.few = rows <= 32;
-  p.rows = p.few ? 32 : kAttnWaves * 32;
+  const bool f32 = kv.dtype == SMALLKV_F32;
+  const int few = f32 ? 16 : 32;
+  p.few = rows <= few;
+  p.rows = p.few ? few : kAttnWaves * 32;
   // no more tiles than this, whatever the sequences' lengths
   p.tiles = (int)std::min<int64_t>(c.batch * ceil_div(rows, p.rows), (int64_t)c.n_tokens * g / p.rows + c.batch);
   // the workgroups that run at once on 256 CUs: three per CU of bf16 and 64 elements
   // (33 KB of LDS, up to 160 registers), two of 128 elements and of fp32.  (A batch
   // of chunks and tokens of 64 elements: 49 us with 512, 46 with 768, 46 with 1024;
   // a batch-64 decode step of 128 elements: 79 with 256, 70 with 512, 71 with 1024.)
-  const int slots = std::max((kv.head_dim == 64 && kv.dtype == SMALLKV_BF16 ? 768 : 512) / kv.n_heads, 1);
-  const int round = !p.few ? kManyRound : kv.dtype == SMALLKV_F32 ? 64 : 128;
-  if (p.tiles < slots && c.max_len > round) p.splits = slots;
+  const int slots = std::max((kv.head_dim == 64 && !f32 ? 768 : 512) / kv.n_heads, 1);
+  const int round = p.few ? few * kFewWaves : kManyRound;
+  if (p.tiles < slots && c.max_len > round)
+    p.splits = (int)std::min<int64_t>(slots, (int64_t)p.tiles * ceil_div(c.max_len, round));
   p.units = std::max(p.tiles, p.splits);
   if (p.splits) p.ws_bytes = kSpanBytes + (size_t)p.units * kv.n_heads * p.rows * (kv.head_dim + 2) * sizeof(float);
   return p;

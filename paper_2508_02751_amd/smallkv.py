@@ -677,18 +677,23 @@ def _rows(t: torch.Tensor, n_tokens: int, heads: Optional[int], like: torch.Tens
 
 
 class _Call:
-    """A prepared call: the descriptors hold raw pointers, `keep` the tensors."""
+    """A prepared call: `_args` hold raw pointers, `_keep` the tensors."""
 
-    def _start(self, dev, keep):
-        self._dev, self._keep = dev, keep
+    def _prepare(self, name, dev, keep, *args):
+        self._name, self._fn, self._dev, self._keep = name, getattr(lib(), name), dev, keep
+        self._args = tuple(C.byref(x) if isinstance(x, C.Structure) else x for x in args)
 
-    def _run(self, fn, stream, *args):
-        # on the tensors' device, on its current stream unless one is given
-        if torch.cuda.current_device() == self._dev.index:
-            _check(fn, getattr(lib(), fn)(*args, _stream(stream)))
+    def run(self, stream=None):
+        """Enqueue on the tensors' device, on its current stream unless one is given."""
+        i = self._dev.index
+        # (the raw handle: a Stream object costs more than the launch)
+        s = torch._C._cuda_getCurrentRawStream(i) if stream is None else stream.cuda_stream
+        if torch.cuda.current_device() == i:
+            rc = self._fn(*self._args, s)
         else:
-            with torch.cuda.device(self._dev):
-                _check(fn, getattr(lib(), fn)(*args, _stream(stream)))
+            with torch.cuda.device(i):
+                rc = self._fn(*self._args, s)
+        _check(self._name, rc)
 
 
 class AppendCall(_Call):
@@ -714,12 +719,8 @@ class AppendCall(_Call):
                            q_out.data_ptr(), *os, _ptr(positions), _ptr(rope.freq),
                            2 * rope.freq.numel(), int(rope.layout), float(rope.amplitude),
                            _ptr(row_pos), row_pos.shape[2] if row_pos is not None else 0)
-        self._c = (ch, ca)
-        self._start(dev, (chunk, cache, rope, q, k, v, positions, row_pos))
-
-    def run(self, stream=None):
-        self._run("smallkv_append", stream, C.byref(self._c[0]), C.byref(self._c[1]),
-                  C.byref(self.desc))
+        self._prepare("smallkv_append", dev, (chunk, cache, rope, q, k, v, positions, row_pos),
+                      ch, ca, self.desc)
 
 
 def prepare_append(chunk: ChunkSpec, cache: CacheSpec, rope: RopeSpec, q, k, v, positions=None,
@@ -754,13 +755,8 @@ class ChunkAttnCall(_Call):
         _check("smallkv_chunk_attn_workspace_size", lib().smallkv_chunk_attn_workspace_size(
             C.byref(ch), C.byref(ca), C.byref(self.desc), C.byref(n)))
         self.ws = ws if ws is not None else torch.empty(n.value, dtype=torch.uint8, device=dev)
-        self._c = (ch, ca)
-        self._start(dev, (chunk, cache, q))
-
-    def run(self, stream=None):
-        w, wb = _ws(self.ws)
-        self._run("smallkv_chunk_attn", stream, C.byref(self._c[0]), C.byref(self._c[1]),
-                  C.byref(self.desc), w, wb)
+        self._prepare("smallkv_chunk_attn", dev, (chunk, cache, q), ch, ca, self.desc,
+                      *_ws(self.ws))
 
 
 def prepare_chunk_attn(chunk: ChunkSpec, cache: CacheSpec, q, scale: float, out=None, lse=True,
@@ -786,13 +782,8 @@ class ChunkScoresCall(_Call):
                       chunk.length)
         self.out = out
         self.desc = Queries(q.shape[1], float(scale), q.data_ptr(), *qs, None, 0, 0, _ptr(lse))
-        self._c = (ch, ca)
-        self._args = (out.shape[1], _ptr(before), _ptr(out), out.shape[2])
-        self._start(dev, (chunk, cache, q, lse, out, before))
-
-    def run(self, stream=None):
-        self._run("smallkv_chunk_scores", stream, C.byref(self._c[0]), C.byref(self._c[1]),
-                  C.byref(self.desc), *self._args)
+        self._prepare("smallkv_chunk_scores", dev, (chunk, cache, q, lse, out, before), ch, ca,
+                      self.desc, out.shape[1], _ptr(before), _ptr(out), out.shape[2])
 
 
 def prepare_chunk_scores(chunk: ChunkSpec, cache: CacheSpec, q, lse, scale: float, out,
@@ -843,11 +834,8 @@ class EvictCall(_Call):
         _check("smallkv_evict_workspace_size", lib().smallkv_evict_workspace_size(
             C.byref(self.desc), C.byref(n)))
         self.ws = torch.empty(n.value, dtype=torch.uint8, device=dev)
-        self._start(dev, (cache, to, length, keep, recent, scores, row_pos))
-
-    def run(self, stream=None):
-        w, wb = _ws(self.ws)
-        self._run("smallkv_evict", stream, C.byref(self.desc), w, wb)
+        self._prepare("smallkv_evict", dev, (cache, to, length, keep, recent, scores, row_pos),
+                      self.desc, *_ws(self.ws))
 
 
 def prepare_evict(cache: CacheSpec, to: CacheSpec, length, keep, scores, recent=None,

@@ -39,6 +39,9 @@ CASES = [
     ("single tokens", [(300, 1), (1, 1), (777, 1), (64, 1), (0, 0), (129, 1)], 14, 2, 64, BF16, 16, False),
     ("single tokens, pages of one row", [(37, 1), (130, 1)], 8, 2, 128, BF16, 1, True),
     ("a few rows", [(257, 3), (40, 4), (4, 4)], 14, 2, 128, BF16, 32, False),
+    ("a few rows f32", [(257, 2), (40, 1), (2, 2), (16, 2), (70, 0)], 14, 2, 128, F32, 32, False),
+    ("a few rows f32 d64", [(500, 8), (23, 8), (5, 7)], 4, 2, 64, F32, 0, False),
+    ("some rows f32", [(257, 3), (40, 4)], 14, 2, 64, F32, 16, False),
     ("a whole prompt", [(200, 200)], 8, 2, 64, BF16, 0, False),
     ("a whole prompt f32", [(150, 150)], 8, 4, 128, F32, 64, False),
     ("a whole prompt f32 d64", [(75, 75), (33, 20)], 6, 2, 64, F32, 2, True),
@@ -177,7 +180,7 @@ def test_absent_pages(dtype, d):
 
 
 @pytest.mark.parametrize("lens,hq,hk", [([(300, 100)], 8, 2), ([(70, 4), (66, 3)], 8, 2),
-                                        ([(600, 129)], 4, 4)])
+                                        ([(70, 2), (66, 3)], 8, 2), ([(600, 129)], 4, 4)])
 @pytest.mark.parametrize("dtype,d", [(BF16, 128), (BF16, 64), (F32, 128), (F32, 64)])
 def test_infinities_reach_only_the_rows_that_see_them(lens, hq, hk, dtype, d):
     """Values and keys of later tokens that are infinite or NaN leave earlier
@@ -197,7 +200,8 @@ def test_infinities_reach_only_the_rows_that_see_them(lens, hq, hk, dtype, d):
     want, wl, tol, ltol = R.attention(c)
     within(call.out, want, tol, "out")
     within(call.lse, wl, ltol, "lse")
-    assert bool(torch.isfinite(call.out[:1]).all())
+    if lens[0][1] > 2:  # (of two new tokens the first one's own row is the infinite one)
+        assert bool(torch.isfinite(call.out[:1]).all())
 
 
 @pytest.mark.parametrize("dtype,d", [(BF16, 128), (F32, 64)])
