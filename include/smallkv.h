@@ -561,9 +561,11 @@ typedef struct {
   int32_t rot_dim;          /* even, 0 .. head_dim (0: nothing turns) */
   int32_t layout;           /* smallkv_rope_layout_t */
   float amplitude;
-  int32_t *row_pos;         /* optional [B][cache n_heads][pos_rows]: the position of
-                               each appended row, written where row < pos_rows */
-  int32_t pos_rows;
+  int32_t *row_pos;         /* optional [B][cache n_heads][pos_rows], sequences
+                               pos_seq_stride >= n_heads * pos_rows elements apart: the
+                               position of each appended row, written where
+                               row < pos_rows */
+  int64_t pos_rows, pos_seq_stride;
 } smallkv_append_t;
 
 /* q_out = turned q; the cache rows of the new tokens = turned k, and v.  Nothing
@@ -592,12 +594,15 @@ int smallkv_chunk_attn_workspace_size(const smallkv_chunk_t *chunk, const smallk
  * for r < len_b: the new tokens' own rows start from 0, entries r >= len_b are
  * not written, and absent rows receive nothing.  n_score_heads = the query heads
  * (one sum each), or the cache's kv heads (the sum over the query heads of each
- * as well).  before, out: [B][n_score_heads][score_rows] fp32, score_rows >=
- * max_len; out may be before; before NULL: 0.  queries->lse is read, out of it
- * is not used.  Sums are fp32 in a fixed order: deterministic. */
+ * as well).  before, out: [B][n_score_heads][score_rows] fp32, sequences seq_stride
+ * >= n_score_heads * score_rows elements apart (one layer of the decode step's
+ * acc_score: seq_stride = n_small_heads * n_cap), score_rows >= max_len; out may be
+ * before; before NULL: 0.  queries->lse is read, its out is not used.  Sums are
+ * fp32 in a fixed order: deterministic. */
 int smallkv_chunk_scores(const smallkv_chunk_t *chunk, const smallkv_cache_t *cache,
                          const smallkv_queries_t *queries, int32_t n_score_heads,
-                         const float *before, float *out, int64_t score_rows, void *stream);
+                         const float *before, float *out, int64_t score_rows,
+                         int64_t seq_stride, void *stream);
 
 /* Eviction by accumulated attention weight.  Per sequence b and kv head, of the
  * n = len[b] rows of `from`:

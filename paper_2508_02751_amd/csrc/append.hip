@@ -26,7 +26,7 @@ struct AppendArgs {
   const double *freq;
   float amplitude;
   int32_t *row_pos;
-  int pos_rows;
+  int64_t pos_rows, pos_stride;
 };
 
 // cos and sin of `turns` full turns (64 bits): the nearest quarter turn is taken
@@ -140,7 +140,7 @@ __global__ __launch_bounds__(256) void append(AppendArgs a) {
       const int kh = h - a.hq - (value ? a.hk : 0);
       src = value ? a.v + at.token * a.v_token + kh * a.v_head : a.k + at.token * a.k_token + kh * a.k_head;
       if (a.row_pos && !value && c == 0 && at.cached >= 0 && at.cached < a.pos_rows)
-        a.row_pos[((int64_t)at.seq * a.hk + kh) * a.pos_rows + at.cached] = at.pos;
+        a.row_pos[at.seq * a.pos_stride + kh * a.pos_rows + at.cached] = at.pos;
       if (at.row < 0) continue;
       dst = (value ? a.cv : a.ck) + at.row + (((uint64_t)kh * a.kv.head_stride) << 4);
     }
@@ -241,6 +241,7 @@ hipError_t launch_append(const smallkv_chunk_t &c, const smallkv_cache_t &kv, co
   a.amplitude = p.amplitude;
   a.row_pos = p.row_pos;
   a.pos_rows = p.pos_rows;
+  a.pos_stride = p.pos_seq_stride;
   if (kv.dtype == SMALLKV_F32)
     return kv.head_dim == 64 ? launch_typed<float, 64>(a, p.layout, st) : launch_typed<float, 128>(a, p.layout, st);
   return kv.head_dim == 64 ? launch_typed<bf16_t, 64>(a, p.layout, st) : launch_typed<bf16_t, 128>(a, p.layout, st);

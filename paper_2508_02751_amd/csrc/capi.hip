@@ -278,7 +278,8 @@ int check_append(const smallkv_chunk_t *c, const smallkv_cache_t *kv, const smal
   if (a->rot_dim > 0 && !a->freq) return SMALLKV_EINVAL;
   if (a->layout != SMALLKV_ROPE_HALF && a->layout != SMALLKV_ROPE_INTERLEAVED) return SMALLKV_EINVAL;
   if (!(a->amplitude == a->amplitude)) return SMALLKV_EINVAL;
-  if (a->row_pos && a->pos_rows < 1) return SMALLKV_EINVAL;
+  if (a->row_pos && (a->pos_rows < 1 || a->pos_rows > INT32_MAX || a->pos_seq_stride < kv->n_heads * a->pos_rows))
+    return SMALLKV_EINVAL;
   if (a->n_q_heads > (1 << 16)) return SMALLKV_EUNSUPPORTED;
   return SMALLKV_OK;
 }
@@ -621,16 +622,17 @@ int smallkv_chunk_attn(const smallkv_chunk_t *chunk, const smallkv_cache_t *cach
 
 int smallkv_chunk_scores(const smallkv_chunk_t *chunk, const smallkv_cache_t *cache,
                          const smallkv_queries_t *queries, int32_t n_score_heads, const float *before,
-                         float *out, int64_t score_rows, void *stream) {
+                         float *out, int64_t score_rows, int64_t seq_stride, void *stream) {
   const int rc = check_queries(chunk, cache, queries);
   if (rc) return rc;
   if (!queries->lse || !out || score_rows < chunk->max_len) return SMALLKV_EINVAL;
   if (n_score_heads != queries->n_heads && n_score_heads != cache->n_heads) return SMALLKV_EINVAL;
+  if (score_rows > INT32_MAX || seq_stride < n_score_heads * score_rows) return SMALLKV_EINVAL;
   if (((int64_t)chunk->max_len + 127) / 128 * chunk->batch * cache->n_heads > (1 << 30) ||
       queries->n_heads / cache->n_heads > 65535)
     return SMALLKV_EUNSUPPORTED;
   return status_of(launch_chunk_scores(*chunk, *cache, *queries, n_score_heads, before, out, score_rows,
-                                       static_cast<hipStream_t>(stream)));
+                                       seq_stride, static_cast<hipStream_t>(stream)));
 }
 
 int smallkv_evict_workspace_size(const smallkv_evict_t *evict, size_t *bytes) {

@@ -36,7 +36,7 @@ struct ScoreArgs {
   const float *lse;
   const float *before;
   float *out;
-  int64_t rows;   // of before and out
+  int64_t rows, seq_stride;  // of before and out, in elements
   float scale2;   // scale * log2(e)
   int span;       // few: keys per workgroup, a multiple of 128
 };
@@ -200,7 +200,7 @@ __global__ __launch_bounds__(kNW * kWave, SPLIT && sizeof(T) * D == 512 ? 1 : 2)
   // bits 4..1 of the lane are the register's bits 3..0
   const int i = (lane & 31) >> 1, in = 8 * (i / 4) + i % 4 + 4 * half, key = key0 + in;
   if (!(lane & 1) && key < s.len) {
-    const int64_t at = ((int64_t)b * (PER_KV ? a.hkv : a.hq) + (PER_KV ? kvh : head0)) * a.rows + key;
+    const int64_t at = b * a.seq_stride + (PER_KV ? kvh : head0) * a.rows + key;
     const float old = a.before && key < pos0 ? a.before[at] : 0.0f;
     a.out[at] = old + (exists >> in & 1u ? sum : 0.0f);
   }
@@ -296,7 +296,7 @@ __global__ __launch_bounds__(kNW * kWave, 2) void few_scores(ScoreArgs a) {
       for (int i = 0; i < 16; ++i) sum += p[i];
       sum = swap_halves_sum(sum);
       if (half == 0 && inside) {
-        const int64_t at = ((int64_t)b * a.hkv + kvh) * a.rows + key;
+        const int64_t at = b * a.seq_stride + kvh * a.rows + key;
         a.out[at] = (a.before && key < pos0 ? a.before[at] : 0.0f) + sum;
       }
     } else {
@@ -312,7 +312,7 @@ __global__ __launch_bounds__(kNW * kWave, 2) void few_scores(ScoreArgs a) {
         }
         sum = swap_halves_sum(sum);
         if (half == 0 && inside) {
-          const int64_t at = ((int64_t)b * a.hq + kvh * a.g + j) * a.rows + key;
+          const int64_t at = b * a.seq_stride + (kvh * a.g + j) * a.rows + key;
           a.out[at] = (a.before && key < pos0 ? a.before[at] : 0.0f) + sum;
         }
       }
@@ -350,7 +350,7 @@ void launch_typed(ScoreArgs a, int max_new, int max_len, hipStream_t st) {
 
 hipError_t launch_chunk_scores(const smallkv_chunk_t &c, const smallkv_cache_t &kv, const smallkv_queries_t &q,
                                int n_score_heads, const float *before, float *out, int64_t score_rows,
-                               hipStream_t st) {
+                               int64_t seq_stride, hipStream_t st) {
   const int e = kv.dtype == SMALLKV_F32 ? 4 : 2;
   ScoreArgs a{};
   a.c = chunk_view(c);
@@ -366,6 +366,7 @@ hipError_t launch_chunk_scores(const smallkv_chunk_t &c, const smallkv_cache_t &
   a.before = before;
   a.out = out;
   a.rows = score_rows;
+  a.seq_stride = seq_stride;
   a.scale2 = q.scale * kLog2e;
   if (kv.dtype == SMALLKV_F32)
     (kv.head_dim == 64 ? launch_typed<float, 64> : launch_typed<float, 128>)(a, c.max_new, c.max_len, st);

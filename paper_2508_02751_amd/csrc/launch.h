@@ -146,7 +146,7 @@ hipError_t launch_chunk_attn(const smallkv_chunk_t &c, const smallkv_cache_t &kv
                              const smallkv_queries_t &q, const AttnPlan &p, void *ws, hipStream_t st);
 hipError_t launch_chunk_scores(const smallkv_chunk_t &c, const smallkv_cache_t &kv,
                                const smallkv_queries_t &q, int n_score_heads, const float *before,
-                               float *out, int64_t score_rows, hipStream_t st);
+                               float *out, int64_t score_rows, int64_t seq_stride, hipStream_t st);
 hipError_t launch_append(const smallkv_chunk_t &c, const smallkv_cache_t &kv,
                          const smallkv_append_t &a, hipStream_t st);
 size_t evict_workspace(const smallkv_evict_t &e);

@@ -4,12 +4,17 @@
 dict with the same keys) into BatchSpec/ModelSpec objects, allocates the
 caller-owned intermediates and the workspace, and builds the C step
 descriptor; `run` enqueues smallkv_step on the current stream.
+
+`ModelCache` holds the caches that a step reads: a prompt's chunks and decoded
+tokens fill them layer by layer (smallkv_append, smallkv_chunk_attn), the
+attention they spend is kept per cached row (smallkv_chunk_scores), and
+`compress` keeps the rows that received most of it (smallkv_evict).
 """
 from __future__ import annotations
 
 import dataclasses
 import math
-from typing import Optional
+from typing import Optional, Sequence
 
 import torch
 
@@ -101,3 +106,102 @@ def prepare_step(x: dict, mode: int = S.NORM_REMAINING,
     desc = S.make_step(batch, small, large, hm, mode, buf.logits, buf.row_max, buf.row_sum,
                        buf.crit_idx, buf.marg_idx, buf.marg_prob, buf.mass, select, acc)
     return PreparedStep(batch, small, large, hm, mode, buf, desc, x)
+
+
+class ModelCache:
+    """One model's keys and values [B][layers][Hkv][n_rows][d], filled a chunk of new
+    tokens at a time:
+
+        cache.begin([new tokens of each sequence])
+        for layer in range(layers):
+            out, turned_q = cache.layer(layer, q, k, v)   # packed [T][heads][d]
+
+    rows[b]: rows in use; tokens[b]: the sequence's length (more than its rows once
+    the cache is compressed: row_pos [B][layers][Hkv][n_rows] then names the rows'
+    positions).  With keep_scores, scores [B][layers * Hkv][n_rows] sum the
+    attention each row has received, over queries and the query heads of a kv head.
+    Everything runs on the current stream.
+    """
+
+    def __init__(self, batch: int, layers: int, q_heads: int, kv_heads: int, head_dim: int,
+                 n_rows: int, rope: S.RopeSpec, dtype=torch.bfloat16, device="cuda",
+                 keep_scores: bool = False, positions: bool = False):
+        def new(*shape, dt=dtype):
+            return torch.zeros(shape, dtype=dt, device=device)
+        self.layers, self.q_heads, self.kv_heads, self.rope = layers, q_heads, kv_heads, rope
+        self.k = new(batch, layers, kv_heads, n_rows, head_dim)
+        self.v = torch.zeros_like(self.k)
+        self.scores = new(batch, layers * kv_heads, n_rows, dt=torch.float32) if keep_scores else None
+        self.row_pos = new(batch, layers, kv_heads, n_rows, dt=torch.int32) if positions else None
+        self.rows, self.tokens = [0] * batch, [0] * batch
+        self._chunk = None
+
+    @property
+    def n_rows(self) -> int:
+        return self.k.shape[3]
+
+    def _ints(self, v) -> torch.Tensor:
+        return torch.tensor(v, dtype=torch.int32, device=self.k.device)
+
+    def begin(self, new: Sequence[int]) -> int:
+        """Take new[b] more tokens per sequence (packed in this order); their number."""
+        if len(new) != len(self.rows) or min(new) < 0:
+            raise ValueError("begin() takes the number of new tokens of every sequence")
+        rows = [r + n for r, n in zip(self.rows, new)]
+        if max(rows) > self.n_rows:
+            raise ValueError(f"{max(rows)} rows do not fit a cache of {self.n_rows}")
+        start = [0]
+        for n in new:
+            start.append(start[-1] + n)
+        pos = [t + i for t, n in zip(self.tokens, new) for i in range(n)]
+        self._positions = self._ints(pos)
+        self.rows, self.tokens = rows, [t + n for t, n in zip(self.tokens, new)]
+        self._chunk = S.ChunkSpec(self._ints(start), self._ints(rows), start[-1],
+                                  max(max(new), 1), max(max(rows), 1))
+        return start[-1]
+
+    def layer(self, layer: int, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor):
+        """The chunk's queries, keys and values in one layer: (attention output, turned
+        queries), [T][Hq][d] both."""
+        if self._chunk is None:
+            raise ValueError("begin() first")
+        cache = S.CacheSpec(self.k[:, layer], self.v[:, layer])
+        scale = softmax_scale(self.k.shape[-1])
+        pos = None if self.row_pos is None else self.row_pos[:, layer]
+        add = S.prepare_append(self._chunk, cache, self.rope, q, k, v, positions=self._positions,
+                               row_pos=pos)
+        add.run()
+        attn = S.prepare_chunk_attn(self._chunk, cache, add.q_out, scale)
+        attn.run()
+        if self.scores is not None:
+            h = slice(layer * self.kv_heads, (layer + 1) * self.kv_heads)
+            S.prepare_chunk_scores(self._chunk, cache, add.q_out, attn.lse, scale,
+                                   self.scores[:, h], before=self.scores[:, h]).run()
+        return attn.out, add.q_out
+
+    def compress(self, keep: Sequence[int], recent: Optional[Sequence[int]] = None, sinks: int = 0,
+                 n_rows: Optional[int] = None) -> "ModelCache":
+        """A cache of n_rows rows (default: the largest keep) that holds keep[b] of each
+        sequence's rows: the first `sinks`, the last recent[b], and those that
+        received most attention.  Needs keep_scores."""
+        if self.scores is None:
+            raise ValueError("compress() needs a cache with keep_scores")
+        B, L, H, _, d = self.k.shape
+        to = ModelCache(B, L, self.q_heads, H, d, n_rows or max(max(keep), 1), self.rope,
+                        self.k.dtype, self.k.device, keep_scores=True, positions=True)
+        pos = None if self.row_pos is None else self.row_pos.view(B, L * H, -1)
+        S.prepare_evict(S.CacheSpec(self.k.flatten(1, 2), self.v.flatten(1, 2)),
+                        S.CacheSpec(to.k.flatten(1, 2), to.v.flatten(1, 2)), self._ints(self.rows),
+                        self._ints(keep), self.scores,
+                        recent=None if recent is None else self._ints(recent), sinks=sinks,
+                        row_pos=pos, out_pos=to.row_pos.view(B, L * H, -1), out_scores=to.scores).run()
+        to.rows = [max(0, min(k, r, to.n_rows)) for k, r in zip(keep, self.rows)]
+        to.tokens = list(self.tokens)
+        return to
+
+    def small_inputs(self) -> dict:
+        """The small model's entries of a step's inputs (see prepare_step)."""
+        x = {"s_k": self.k, "s_v": self.v}
+        if self.row_pos is not None:
+            x.update(s_held=self._ints(self.rows), s_row_pos=self.row_pos)
+        return x

@@ -103,7 +103,7 @@ class Append(C.Structure):
                 ("q_out_token_stride", C.c_int64), ("q_out_head_stride", C.c_int64),
                 ("positions", C.c_void_p), ("freq", C.c_void_p), ("rot_dim", C.c_int32),
                 ("layout", C.c_int32), ("amplitude", C.c_float), ("row_pos", C.c_void_p),
-                ("pos_rows", C.c_int32)]
+                ("pos_rows", C.c_int64), ("pos_seq_stride", C.c_int64)]
 
 
 class Evict(C.Structure):
@@ -178,7 +178,7 @@ def lib():
         L.smallkv_chunk_attn_workspace_size.argtypes = [P(Chunk), P(Cache), P(Queries),
                                                         P(C.c_size_t)]
         L.smallkv_chunk_scores.argtypes = [P(Chunk), P(Cache), P(Queries), C.c_int32, C.c_void_p,
-                                           C.c_void_p, C.c_int64, C.c_void_p]
+                                           C.c_void_p, C.c_int64, C.c_int64, C.c_void_p]
         L.smallkv_evict.argtypes = [P(Evict), C.c_void_p, C.c_size_t, C.c_void_p]
         L.smallkv_evict_workspace_size.argtypes = [P(Evict), P(C.c_size_t)]
         L.smallkv_status_string.argtypes = [C.c_int]
@@ -598,6 +598,21 @@ def _need(t: Optional[torch.Tensor], dtype, shape, what: str, optional=False):
         raise ValueError(f"{what} must be contiguous")
 
 
+def _planes(t: Optional[torch.Tensor], dtype, shape, what: str):
+    """(rows, elements between sequences) of a [B][heads][rows] tensor whose sequences
+    may lie apart (a layer of a [B][layers][heads][rows] tensor)."""
+    if t is None or t.dim() != 3 or t.dtype != dtype or tuple(t.shape[:2]) != tuple(shape[:2]) or \
+            (len(shape) > 2 and t.shape[2] != shape[2]):
+        raise ValueError(f"{what} must be {dtype} {tuple(shape)}{' x rows' if len(shape) == 2 else ''}")
+    B, H, n = t.shape
+    if (n > 1 and t.stride(2) != 1) or (H > 1 and t.stride(1) != n):
+        raise ValueError(f"{what}: the rows of a sequence must be contiguous")
+    seq = t.stride(0) if B > 1 else H * n
+    if seq < H * n:
+        raise ValueError(f"{what}: sequences overlap")
+    return n, seq
+
+
 def _strides(t: torch.Tensor, what: str):
     """Strides of the leading dimensions (0 where the extent is 1); rows contiguous."""
     if t.shape[-1] > 1 and t.stride(-1) != 1:
@@ -677,15 +692,21 @@ def _rows(t: torch.Tensor, n_tokens: int, heads: Optional[int], like: torch.Tens
 
 
 class _Call:
-    """A prepared call: `_args` hold raw pointers, `_keep` the tensors."""
+    """A prepared call: `_args` hold raw pointers, `_keep` the caller's tensors, `_own`
+    those allocated with the call."""
 
-    def _prepare(self, name, dev, keep, *args):
+    def _prepare(self, name, dev, keep, own, *args):
         self._name, self._fn, self._dev, self._keep = name, getattr(lib(), name), dev, keep
+        self._own = [t for t in own if t is not None]
         self._args = tuple(C.byref(x) if isinstance(x, C.Structure) else x for x in args)
 
     def run(self, stream=None):
-        """Enqueue on the tensors' device, on its current stream unless one is given."""
+        """Enqueue on the tensors' device, on its current stream unless one is given (the
+        caller orders it after what the tensors' own streams still do)."""
         i = self._dev.index
+        if stream is not None:
+            for t in self._own:  # not reused before that stream is done with them
+                t.record_stream(stream)
         # (the raw handle: a Stream object costs more than the launch)
         s = torch._C._cuda_getCurrentRawStream(i) if stream is None else stream.cuda_stream
         if torch.cuda.current_device() == i:
@@ -702,25 +723,25 @@ class AppendCall(_Call):
     def __init__(self, chunk, cache, rope, q, k, v, positions, q_out, row_pos):
         ch, ca = chunk.c(), cache.c(chunk.length.numel())
         T, like = chunk.n_tokens, cache.k
+        own = []
         if q_out is None:
             q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            own.append(q_out)
         qs, os = _rows(q, T, None, like, "q"), _rows(q_out, T, q.shape[1], like, "q_out")
         ks, vs = _rows(k, T, ca.n_heads, like, "k"), _rows(v, T, ca.n_heads, like, "v")
         _need(rope.freq, torch.float64, (rope.freq.numel(),), "freq")
         _need(positions, torch.int32, (T,), "positions", optional=True)
-        if row_pos is not None:
-            if row_pos.dim() != 3:
-                raise ValueError("row_pos must be [B][Hkv][rows]")
-            _need(row_pos, torch.int32, (ch.batch, ca.n_heads, row_pos.shape[2]), "row_pos")
+        planes = (0, 0) if row_pos is None else _planes(row_pos, torch.int32,
+                                                        (ch.batch, ca.n_heads), "row_pos")
         dev = _on_gpu(q, k, v, q_out, positions, row_pos, rope.freq, cache.k, cache.v,
                       cache.page_table, chunk.start, chunk.length)
         self.q_out = q_out
         self.desc = Append(q.data_ptr(), k.data_ptr(), v.data_ptr(), *qs, *ks, *vs, q.shape[1],
                            q_out.data_ptr(), *os, _ptr(positions), _ptr(rope.freq),
                            2 * rope.freq.numel(), int(rope.layout), float(rope.amplitude),
-                           _ptr(row_pos), row_pos.shape[2] if row_pos is not None else 0)
+                           None if row_pos is None else row_pos.data_ptr(), *planes)
         self._prepare("smallkv_append", dev, (chunk, cache, rope, q, k, v, positions, row_pos),
-                      ch, ca, self.desc)
+                      own, ch, ca, self.desc)
 
 
 def prepare_append(chunk: ChunkSpec, cache: CacheSpec, rope: RopeSpec, q, k, v, positions=None,
@@ -728,7 +749,8 @@ def prepare_append(chunk: ChunkSpec, cache: CacheSpec, rope: RopeSpec, q, k, v, 
     """The new tokens' q [T][Hq][d], k and v [T][Hkv][d] (views of a fused projection
     will do): q turned into q_out (allocated if None, q itself will do), k turned
     and v written to the cache.  positions int32 [T] (None: the tokens' cached
-    rows); row_pos int32 [B][Hkv][rows]: receives the appended rows' positions."""
+    rows); row_pos int32 [B][Hkv][rows], or one layer of a [B][layers][Hkv][rows]
+    tensor: receives the appended rows' positions."""
     return AppendCall(chunk, cache, rope, q, k, v, positions, q_out, row_pos)
 
 
@@ -740,11 +762,14 @@ class ChunkAttnCall(_Call):
         T = chunk.n_tokens
         qs = _rows(q, T, None, cache.k, "q")
         hq = q.shape[1]
+        own = []
         if out is None:
             out = torch.empty((T, hq, q.shape[2]), dtype=q.dtype, device=q.device)
+            own.append(out)
         os = _rows(out, T, hq, cache.k, "out")
         if lse is True:
             lse = torch.empty((T, hq), dtype=torch.float32, device=q.device)
+            own.append(lse)
         lse = lse if lse is not False else None
         _need(lse, torch.float32, (T, hq), "lse", optional=True)
         dev = _on_gpu(q, out, lse, ws, cache.k, cache.v, cache.page_table, chunk.start,
@@ -754,8 +779,11 @@ class ChunkAttnCall(_Call):
         n = C.c_size_t()
         _check("smallkv_chunk_attn_workspace_size", lib().smallkv_chunk_attn_workspace_size(
             C.byref(ch), C.byref(ca), C.byref(self.desc), C.byref(n)))
-        self.ws = ws if ws is not None else torch.empty(n.value, dtype=torch.uint8, device=dev)
-        self._prepare("smallkv_chunk_attn", dev, (chunk, cache, q), ch, ca, self.desc,
+        if ws is None:
+            ws = torch.empty(n.value, dtype=torch.uint8, device=dev)
+            own.append(ws)
+        self.ws = ws
+        self._prepare("smallkv_chunk_attn", dev, (chunk, cache, q), own, ch, ca, self.desc,
                       *_ws(self.ws))
 
 
@@ -775,22 +803,25 @@ class ChunkScoresCall(_Call):
         qs = _rows(q, T, None, cache.k, "q")
         _need(lse, torch.float32, (T, q.shape[1]), "lse")
         if out.dim() != 3:
-            raise ValueError("scores must be [B][Hq or Hkv][rows]")
-        _need(out, torch.float32, (ch.batch, out.shape[1], out.shape[2]), "out")
-        _need(before, torch.float32, out.shape, "before", optional=True)
+            raise ValueError("out must be [B][Hq or Hkv][rows]")
+        planes = _planes(out, torch.float32, (ch.batch, out.shape[1]), "out")
+        if before is not None and _planes(before, torch.float32, out.shape, "before") != planes:
+            raise ValueError("before must have out's strides")
         dev = _on_gpu(q, lse, out, before, cache.k, cache.v, cache.page_table, chunk.start,
                       chunk.length)
         self.out = out
         self.desc = Queries(q.shape[1], float(scale), q.data_ptr(), *qs, None, 0, 0, _ptr(lse))
-        self._prepare("smallkv_chunk_scores", dev, (chunk, cache, q, lse, out, before), ch, ca,
-                      self.desc, out.shape[1], _ptr(before), _ptr(out), out.shape[2])
+        self._prepare("smallkv_chunk_scores", dev, (chunk, cache, q, lse, out, before), [], ch,
+                      ca, self.desc, out.shape[1], None if before is None else before.data_ptr(),
+                      out.data_ptr(), *planes)
 
 
 def prepare_chunk_scores(chunk: ChunkSpec, cache: CacheSpec, q, lse, scale: float, out,
                          before=None) -> ChunkScoresCall:
     """The attention weight of the new tokens per cached row (lse: of
     prepare_chunk_attn), added to `before` (None: 0; `out` itself will do) into
-    out float32 [B][Hq or Hkv][rows]."""
+    out float32 [B][Hq or Hkv][rows], or one layer of a [B][layers][heads][rows] tensor
+    (both alike)."""
     return ChunkScoresCall(chunk, cache, q, lse, scale, out, before)
 
 
@@ -816,12 +847,15 @@ class EvictCall(_Call):
         rows = to.capacity if out_pos is None else out_pos.shape[-1]
         dev = _on_gpu(length, keep, recent, scores, row_pos, out_pos, out_scores, held, cache.k,
                       cache.v, cache.page_table, to.k, to.v, to.page_table)
+        own = []
         if out_pos is None:
             out_pos = torch.zeros((B, H, rows), dtype=torch.int32, device=dev)
+            own.append(out_pos)
         _need(out_pos, torch.int32, (B, H, rows), "out_pos")
         _need(out_scores, torch.float32, (B, scores.shape[1], rows), "out_scores", optional=True)
         if held is None:
             held = torch.zeros(B, dtype=torch.int32, device=dev)
+            own.append(held)
         if max_len is None:
             max_len = min(cache.capacity, scores.shape[2],
                           row_pos.shape[2] if row_pos is not None else 1 << 30)
@@ -835,7 +869,7 @@ class EvictCall(_Call):
             C.byref(self.desc), C.byref(n)))
         self.ws = torch.empty(n.value, dtype=torch.uint8, device=dev)
         self._prepare("smallkv_evict", dev, (cache, to, length, keep, recent, scores, row_pos),
-                      self.desc, *_ws(self.ws))
+                      own + [self.ws], self.desc, *_ws(self.ws))
 
 
 def prepare_evict(cache: CacheSpec, to: CacheSpec, length, keep, scores, recent=None,

@@ -39,7 +39,7 @@ def queries(**over):
 
 def append(**over):
     a = S.Append(P, P, P, 28 * 128, 128, 4 * 128, 128, 4 * 128, 128, 28, P + 4096, 28 * 128, 128,
-                 None, P, 128, 0, 1.0, None, 0)
+                 None, P, 128, 0, 1.0, None, 0, 0)
     for k, v in over.items():
         setattr(a, k, v)
     return a
@@ -80,7 +80,7 @@ def test_every_call_rejects_a_bad_cache(over, status):
     q = queries(n_heads=hq)
     L = S.lib()
     assert L.smallkv_chunk_scores(C.byref(chunk()), C.byref(cache(**over)), C.byref(q), hq, None, P, 128,
-                                  None) == status
+                                  1 << 40, None) == status
     assert L.smallkv_append(C.byref(chunk()), C.byref(cache(**over)), C.byref(append()), None) == status
     n = C.c_size_t()
     for e in (evict(frm=cache(**over)), evict(to=cache(**dict(dict(k=P + 4096, v=P + 8192), **over)))):
@@ -99,7 +99,7 @@ def test_bad_chunks(over, status):
     assert try_attn(chunk(**over), cache(), queries()) == status
     ca, q = cache(), queries()
     assert S.lib().smallkv_chunk_scores(C.byref(chunk(**over)), C.byref(ca), C.byref(q), 28, None, P, 1 << 31,
-                                        None) == status
+                                        1 << 40, None) == status
 
 
 @pytest.mark.parametrize("over,status", [
@@ -147,11 +147,14 @@ def test_scores_refusals():
     L = S.lib()
     ch, ca = chunk(), cache()
 
-    def call(q, heads=28, out=P, rows=128):
-        return L.smallkv_chunk_scores(C.byref(ch), C.byref(ca), C.byref(q), heads, None, out, rows, None)
+    def call(q, heads=28, out=P, rows=128, seq=28 * 128):
+        return L.smallkv_chunk_scores(C.byref(ch), C.byref(ca), C.byref(q), heads, None, out, rows, seq,
+                                      None)
     assert call(queries(lse=None)) == S.EINVAL
     assert call(queries(), out=None) == S.EINVAL
     assert call(queries(), rows=127) == S.EINVAL
+    assert call(queries(), seq=28 * 128 - 1) == S.EINVAL
+    assert call(queries(token_stride=1 << 31)) == S.EUNSUPPORTED
     assert call(queries(), heads=14) == S.EINVAL
     assert call(queries(n_heads=27), heads=27) == S.EINVAL
     assert call(queries(scale=0.0)) == S.EINVAL
@@ -165,7 +168,7 @@ def test_scores_refusals():
     (dict(n_q_heads=0), S.EINVAL), (dict(n_q_heads=30), S.EINVAL), (dict(rot_dim=-2), S.EINVAL),
     (dict(rot_dim=31), S.EINVAL), (dict(rot_dim=130), S.EINVAL), (dict(freq=None), S.EINVAL),
     (dict(layout=2), S.EINVAL), (dict(amplitude=math.nan), S.EINVAL),
-    (dict(row_pos=P, pos_rows=0), S.EINVAL),
+    (dict(row_pos=P, pos_rows=0), S.EINVAL), (dict(row_pos=P, pos_rows=9, pos_seq_stride=35), S.EINVAL),
     (dict(q_out=P, q_out_token_stride=128, q_out_head_stride=50 * 128), S.EINVAL),  # in place, other strides
 ])
 def test_append_refusals(over, status):
@@ -298,6 +301,10 @@ def test_binding_checks_scores_append_and_evict():
     refuses("lse must be", S.prepare_chunk_scores, ch, ca, q, lse[:-1], 0.1, out)
     refuses("out must be", S.prepare_chunk_scores, ch, ca, q, lse, 0.1, out[:1])
     refuses("before must be", S.prepare_chunk_scores, ch, ca, q, lse, 0.1, out, before=out[:, :2])
+    refuses("out's strides", S.prepare_chunk_scores, ch, ca, q, lse, 0.1, out,
+            before=torch.zeros(2, 16, 24)[:, :8])
+    refuses("contiguous", S.prepare_chunk_scores, ch, ca, q, lse, 0.1, out.transpose(1, 2)[:, :8, :8])
+    refuses("overlap", S.prepare_chunk_scores, ch, ca, q, lse, 0.1, out[:1].expand(2, 8, 24))
     rope = S.RopeSpec(torch.zeros(32, dtype=torch.float64))
     kv = torch.zeros(11, 2, 64, dtype=torch.bfloat16)
     refuses("on a GPU", S.prepare_append, ch, ca, rope, q, kv, kv)
