@@ -65,18 +65,6 @@ struct Tile {
   Seq s;
 };
 
-// Inclusive sums over the wave (row_shr 1, 2, 4, 8, then across rows of 16 lanes).
-__device__ __forceinline__ int wave_scan(int x) {
-  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
-  return x;
-}
-__device__ __forceinline__ int last_lane(int x) { return __builtin_amdgcn_readlane(x, kWave - 1); }
-
 // Spans of a sequence's rows: at least one, so that rows that see no key are written.
 __device__ __forceinline__ int spans_of(int len, int span) {
   return span == kWhole ? 1 : max((len + span - 1) / span, 1);

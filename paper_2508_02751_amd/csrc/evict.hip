@@ -61,20 +61,27 @@ template <int KPT> struct Keys {
   __device__ __forceinline__ void load(const EvictArgs &a, const float *f, int r0, int lo, int hi) {
     const int lane = threadIdx.x & (kWave - 1);
     float s[KPT];
+    for (int i = 0; i < a.gs; ++i, f += a.score_rows) {
+      uint32_t row = r0 + lane;
+      asm volatile("" : "+v"(row));
 #pragma unroll
-    for (int j = 0; j < KPT; ++j) {
-      const int row = min(r0 + j * kWave + lane, max(hi - 1, 0));
-      s[j] = f[row];
+      for (int j = 0; j < KPT; ++j) {
+        const float x = f[min(row + j * kWave, (uint32_t)max(hi - 1, 0))];
+        s[j] = i ? s[j] + x : x;
+        if (j % 16 == 15) __builtin_amdgcn_sched_barrier(0);  // (loads in flight at a time)
+      }
     }
-    for (int i = 1; i < a.gs; ++i)
-#pragma unroll
-      for (int j = 0; j < KPT; ++j) s[j] += f[i * a.score_rows + min(r0 + j * kWave + lane, max(hi - 1, 0))];
 #pragma unroll
     for (int j = 0; j < KPT; ++j) k[j] = s[j] != s[j] ? 0u : logit_key(s[j]);
   }
   template <typename F> __device__ __forceinline__ void each(const EvictArgs &, const float *, int r0, int, F &&use) const {
+    int row = r0 + (int)(threadIdx.x & (kWave - 1));
+    asm volatile("" : "+v"(row));  // (the rows' numbers are not kept between passes)
 #pragma unroll
-    for (int j = 0; j < KPT; ++j) use(r0 + j * kWave + (int)(threadIdx.x & (kWave - 1)), k[j]);
+    for (int j = 0; j < KPT; ++j) {
+      use(row + j * kWave, k[j]);
+      if (KPT > 8) __builtin_amdgcn_sched_barrier(0);  // (few masks alive at a time)
+    }
   }
 };
 template <> struct Keys<0> {
@@ -98,7 +105,7 @@ template <> struct Keys<0> {
 constexpr int kBins = 2 * kST;
 
 template <int KPT>
-__global__ __launch_bounds__(kST, KPT <= 8 ? 8 : 4) void evict_select(EvictArgs a) {
+__global__ __launch_bounds__(kST, KPT <= 16 ? 8 : 4) void evict_select(EvictArgs a) {
   __shared__ uint32_t hist[kBins];
   __shared__ uint32_t part[2][kSW];
   __shared__ uint32_t pick[3];  // the bin, how many of it are wanted, and its count
@@ -124,11 +131,8 @@ __global__ __launch_bounds__(kST, KPT <= 8 ? 8 : 4) void evict_select(EvictArgs 
         mx = max(mx, k);
       }
     });
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-      mn = min(mn, (uint32_t)__shfl_xor((int)mn, o, kWave));
-      mx = max(mx, (uint32_t)__shfl_xor((int)mx, o, kWave));
-    }
+    mn = ~wave_umax(~mn);
+    mx = wave_umax(mx);
     if (lane == 0) {
       part[0][wave] = mn;
       part[1][wave] = mx;
@@ -136,6 +140,7 @@ __global__ __launch_bounds__(kST, KPT <= 8 ? 8 : 4) void evict_select(EvictArgs 
     hist[threadIdx.x] = 0u;
     hist[threadIdx.x + kST] = 0u;
     __syncthreads();
+#pragma unroll
     for (int w = 0; w < kSW; ++w) {
       mn = min(mn, part[0][w]);
       mx = max(mx, part[1][w]);
@@ -150,16 +155,12 @@ __global__ __launch_bounds__(kST, KPT <= 8 ? 8 : 4) void evict_select(EvictArgs 
       });
       __syncthreads();
       const uint32_t c0 = hist[2 * threadIdx.x], c1 = hist[2 * threadIdx.x + 1];
-      uint32_t s = c0 + c1;
-#pragma unroll
-      for (int o = 1; o < kWave; o <<= 1) {
-        const uint32_t y = __shfl_up((int)s, o, kWave);
-        if (lane >= o) s += y;
-      }
+      const uint32_t s = (uint32_t)wave_scan((int)(c0 + c1));
       if (lane == kWave - 1) part[0][wave] = s;
       __syncthreads();
       uint32_t above = s - c0 - c1;
-      for (int w = 0; w < wave; ++w) above += part[0][w];
+#pragma unroll
+      for (int w = 0; w < kSW; ++w) above += w < wave ? part[0][w] : 0u;
       if (above < want && above + c0 >= want) {
         pick[0] = 2 * threadIdx.x;
         pick[1] = want - above;
@@ -201,9 +202,10 @@ __global__ __launch_bounds__(kST, KPT <= 8 ? 8 : 4) void evict_select(EvictArgs 
   }
   __syncthreads();
   uint32_t at = 0, before = 0;  // kept rows and ties of the runs before
-  for (int w = 0; w < wave; ++w) {
-    at += part[0][w];
-    before += part[1][w];
+#pragma unroll
+  for (int w = 0; w < kSW; ++w) {
+    at += w < wave ? part[0][w] : 0u;
+    before += w < wave ? part[1][w] : 0u;
   }
   at += min(before, want);
   const uint64_t below = (1ull << lane) - 1;
