@@ -436,10 +436,21 @@ template <int BM> struct Share {
 
   __device__ __forceinline__ bool find(const AttnArgs &a, int block, int round, int wave_row) {
     kvh = block % a.hkv;
-    const Lanes<BM> lanes(a);
-    const int span = find_span<BM>(a, lanes, round);
-    if (a.splits && block == 0 && threadIdx.x == 0) *a.span = span;
-    if (!locate<BM, true>(a, lanes, span, block / a.hkv, t)) return false;
+    int span = kWhole;
+    if (BM <= 32 && !a.splits) {
+      // no spans and a tile per sequence: many sequences, not searched one by one
+      t.b = block / a.hkv;
+      t.s = sequence(a.c, t.b, a.kv.cap);
+      t.rows = t.s.n_new * a.g;
+      t.row0 = t.split = t.unit0 = 0;
+      t.n_split = 1;
+      if (t.rows == 0) return false;
+    } else {
+      const Lanes<BM> lanes(a);
+      span = find_span<BM>(a, lanes, round);
+      if (a.splits && block == 0 && threadIdx.x == 0) *a.span = span;
+      if (!locate<BM, true>(a, lanes, span, block / a.hkv, t)) return false;
+    }
     unit = block;
     const int pos0 = t.s.len - t.s.n_new;  // cached row of the first new token
     const int last = min(t.row0 + BM, t.rows) - 1;

@@ -240,6 +240,43 @@ def test_large_logits():
         within(call.lse, wl, ltol, "lse")
 
 
+@pytest.mark.parametrize("batch,longest,new,hk,dtype", [
+    (100, 500, 1, 2, BF16), (400, 40, 1, 2, BF16), (130, 300, 2, 1, F32), (90, 90, 30, 2, BF16)])
+def test_many_sequences(batch, longest, new, hk, dtype):
+    """More sequences than a wave has lanes, with and without spans; some without new
+    tokens or rows."""
+    S = lib()
+    g = torch.Generator().manual_seed(batch)
+    lens = []
+    for b in range(batch):
+        n = int(torch.randint(0, longest + 1, (1,), generator=g))
+        lens.append((n, min(n, int(torch.randint(0, new + 1, (1,), generator=g)) if b % 3 else new)))
+    c = R.Case(lens, 4 * hk, hk, 64, dtype, 16, seed=batch)
+    chunk, cache, q = c.to(DEV)
+    log(f"[many] {batch} sequences")
+    call = S.prepare_chunk_attn(chunk, cache, q, c.scale)
+    call.run()
+    want, wl, tol, ltol = R.attention(c)
+    out = torch.zeros(c.B, c.hk, c.rows, device=DEV)
+    S.prepare_chunk_scores(chunk, cache, q, wl.float().to(DEV), c.scale, out).run()
+    torch.cuda.synchronize()
+    within(call.out, want, tol, "out")
+    within(call.lse, wl, ltol, "lse")
+    ws, wt = R.scores(c, wl.float(), torch.zeros(c.B, c.hk, c.rows), True)
+    for b, (n, _) in enumerate(lens):
+        within(out[b, :, :n], ws[b, :, :n], wt[b, :, :n], f"scores {b}")
+    # the same sequences appended
+    kv = torch.randn(c.T, 2 * hk, 64, generator=g).to(dtype)
+    freq, amp = S.rope_freqs(64, 10000.0)
+    S.prepare_append(chunk, cache, S.RopeSpec(freq, S.ROPE_HALF, amp), q, kv.to(DEV)[:, :hk], kv.to(DEV)[:, hk:]).run()
+    torch.cuda.synchronize()
+    v = cache.v.cpu()
+    for b, (n, m) in enumerate(lens):
+        for i in range(m):
+            p, at = c.slot(b, n - m + i)
+            assert torch.equal(v[p, :, at], kv[c.starts[b] + i, hk:])
+
+
 def test_strided_queries_and_outputs():
     """q inside a fused projection, out in a [heads][tokens] layout; one layer of
     a dense [B][L][Hkv][n_cap][d] cache."""
