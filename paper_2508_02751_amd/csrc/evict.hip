@@ -1,9 +1,9 @@
 // Eviction from a cache by accumulated attention weight.
 //
-//   evict_select -- one workgroup per (sequence, kv head): the rows' summed
-//                   scores as order-preserving 32-bit keys, read once and kept in
-//                   registers (up to 32768 rows; longer rows are read again by
-//                   every pass), the exact threshold of the top ones by counting
+//   evict_select -- one workgroup of one to sixteen waves per (sequence, kv head):
+//                   the rows' summed scores as order-preserving 32-bit keys, read once
+//                   and kept in registers (up to 32768 rows; longer rows are read again
+//                   by every pass), the exact threshold of the top ones by counting
 //                   passes, then the kept rows' numbers in ascending order, ties to
 //                   the lowest rows;
 //   evict_copy   -- the kept rows as a flat array of 16-byte pieces, K and V, and
@@ -16,8 +16,7 @@
 namespace smallkv {
 namespace {
 
-constexpr int kST = 1024, kSW = kST / kWave;  // evict_select threads, waves
-constexpr int kCT = 256;                      // evict_copy threads
+constexpr int kCT = 256;  // evict_copy threads
 
 struct EvictArgs {
   int batch, max_len, heads, gs, sinks;
@@ -96,16 +95,16 @@ template <> struct Keys<0> {
 };
 
 // The threshold of the `top` largest keys of rows lo..hi-1, by counting: the
-// range between the smallest and the largest key is cut into kBins equal bins
+// range between the smallest and the largest key is cut into equal bins
 // (keys of floats are spread about evenly in it, where the bits of one digit are
 // not: scores share their leading bits, and the counters of a few bins would be
 // hit by all lanes at once), the bin that holds the threshold becomes the next
 // range, and the descent ends when its keys are equal or all wanted: two or three
 // passes instead of four by 8-bit digits.
-constexpr int kBins = 2 * kST;
-
-template <int KPT>
-__global__ __launch_bounds__(kST, KPT <= 16 ? 8 : 4) void evict_select(EvictArgs a) {
+template <int NT, int KPT>
+__global__ __launch_bounds__(NT, KPT <= 16 ? 8 : 4) void evict_select(EvictArgs a) {
+  constexpr int kSW = NT / kWave;
+  constexpr int kBits = NT == 1024 ? 11 : 9, kBins = 1 << kBits, kOwn = kBins / NT;  // bins per thread
   __shared__ uint32_t hist[kBins];
   __shared__ uint32_t part[2][kSW];
   __shared__ uint32_t pick[3];  // the bin, how many of it are wanted, and its count
@@ -137,8 +136,8 @@ __global__ __launch_bounds__(kST, KPT <= 16 ? 8 : 4) void evict_select(EvictArgs
       part[0][wave] = mn;
       part[1][wave] = mx;
     }
-    hist[threadIdx.x] = 0u;
-    hist[threadIdx.x + kST] = 0u;
+#pragma unroll
+    for (int i = 0; i < kOwn; ++i) hist[threadIdx.x * kOwn + i] = 0u;
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < kSW; ++w) {
@@ -149,29 +148,30 @@ __global__ __launch_bounds__(kST, KPT <= 16 ? 8 : 4) void evict_select(EvictArgs
     high = mx;
     while (low < high) {
       // bins of 2^shift keys, bin 0 the highest keys
-      const int bits = 32 - __clz(high - low), shift = max(bits - 11, 0);  // (kBins = 2^11)
+      const int bits = 32 - __clz(high - low), shift = max(bits - kBits, 0);
       keys.each(a, f, r0, r1, [&](int row, uint32_t k) {
         if (row >= lo && row < hi && k >= low && k <= high) atomicAdd(&hist[(high - k) >> shift], 1u);
       });
       __syncthreads();
-      const uint32_t c0 = hist[2 * threadIdx.x], c1 = hist[2 * threadIdx.x + 1];
-      const uint32_t s = (uint32_t)wave_scan((int)(c0 + c1));
+      uint32_t c[kOwn], own = 0;
+#pragma unroll
+      for (int i = 0; i < kOwn; ++i) own += c[i] = hist[threadIdx.x * kOwn + i];
+      const uint32_t s = (uint32_t)wave_scan((int)own);
       if (lane == kWave - 1) part[0][wave] = s;
       __syncthreads();
-      uint32_t above = s - c0 - c1;
+      uint32_t above = s - own;
 #pragma unroll
       for (int w = 0; w < kSW; ++w) above += w < wave ? part[0][w] : 0u;
-      if (above < want && above + c0 >= want) {
-        pick[0] = 2 * threadIdx.x;
-        pick[1] = want - above;
-        pick[2] = c0;
-      } else if (above + c0 < want && above + c0 + c1 >= want) {
-        pick[0] = 2 * threadIdx.x + 1;
-        pick[1] = want - above - c0;
-        pick[2] = c1;
+#pragma unroll
+      for (int i = 0; i < kOwn; ++i) {
+        if (above < want && above + c[i] >= want) {
+          pick[0] = threadIdx.x * kOwn + i;
+          pick[1] = want - above;
+          pick[2] = c[i];
+        }
+        above += c[i];
+        hist[threadIdx.x * kOwn + i] = 0u;
       }
-      hist[2 * threadIdx.x] = 0u;
-      hist[2 * threadIdx.x + 1] = 0u;
       __syncthreads();
       const uint32_t from = pick[0] << shift;
       want = pick[1];
@@ -221,16 +221,16 @@ __global__ __launch_bounds__(kST, KPT <= 16 ? 8 : 4) void evict_select(EvictArgs
   });
 }
 
-// blockIdx.x: (sequence, kv head); blockIdx.y: interleaved shares of the pieces;
-// blockIdx.z: K (0), V (1), or positions and scores (2).
-constexpr int kShares = 32;
+// blockIdx.x: (sequence, kv head); blockIdx.y: interleaved shares of the pieces, as many
+// as a piece per thread asks for, up to 32; blockIdx.z: K (0), V (1), or positions and
+// scores (2).
 
 __global__ __launch_bounds__(kCT) void evict_copy(EvictArgs a) {
   const int unit = blockIdx.x, b = unit / a.heads, h = unit % a.heads;
   const Budget x = budget(a, b);
   const int32_t *src = a.src + unit * a.cap;
   if (blockIdx.z == 2) {
-    for (int r = blockIdx.y * kCT + threadIdx.x; r < x.kept; r += kShares * kCT) {
+    for (int r = blockIdx.y * kCT + threadIdx.x; r < x.kept; r += gridDim.y * kCT) {
       const int row = src[r];
       a.out_pos[unit * a.out_rows + r] = a.row_pos ? a.row_pos[unit * a.pos_rows + row] : row;
       if (a.out_scores)
@@ -244,7 +244,7 @@ __global__ __launch_bounds__(kCT) void evict_copy(EvictArgs a) {
   const int64_t items = (int64_t)x.kept << psh;
   const unsigned char *from = (blockIdx.z ? a.from.v : a.from.k) + (((uint64_t)h * a.from.head_stride) << 4);
   unsigned char *to = (blockIdx.z ? a.to_v : a.to_k) + (((uint64_t)h * a.to.head_stride) << 4);
-  for (int64_t q = blockIdx.y * kCT + threadIdx.x; q < items; q += kShares * kCT) {
+  for (int64_t q = blockIdx.y * kCT + threadIdx.x; q < items; q += (int64_t)gridDim.y * kCT) {
     const int r = (int)(q >> psh), p = (int)(q & ((1 << psh) - 1));
     const int64_t s = row_offset(a.from, b, src[r]), d = row_offset(a.to, b, r);
     if (s < 0 || d < 0) continue;
@@ -252,8 +252,8 @@ __global__ __launch_bounds__(kCT) void evict_copy(EvictArgs a) {
   }
 }
 
-template <int KPT> void launch_select(const EvictArgs &a, unsigned units, hipStream_t st) {
-  hipLaunchKernelGGL((evict_select<KPT>), dim3(units), dim3(kST), 0, st, a);
+template <int NT, int KPT> void launch_select(const EvictArgs &a, unsigned units, hipStream_t st) {
+  hipLaunchKernelGGL((evict_select<NT, KPT>), dim3(units), dim3(NT), 0, st, a);
 }
 
 int64_t kept_cap(const smallkv_evict_t &e) {
@@ -293,13 +293,15 @@ hipError_t launch_evict(const smallkv_evict_t &e, void *ws, hipStream_t st) {
   a.src = static_cast<int32_t *>(ws);
   a.cap = kept_cap(e);
   const unsigned units = (unsigned)(e.batch * e.from.n_heads);
-  // the smallest number of keys per thread that covers the longest sequence
-  const int kpt = (std::min(a.max_len, a.from.cap) + kST - 1) / kST;
-  (kpt <= 2 ? launch_select<2> : kpt <= 8 ? launch_select<8> : kpt <= 16 ? launch_select<16>
-   : kpt <= 32 ? launch_select<32> : launch_select<0>)(a, units, st);
+  // eight keys per thread and as few waves as hold the longest sequence (one layer of
+  // 1237 rows: 9.8 us with four waves, 11.8 with sixteen; 1088 kv heads of 861: 18, 27)
+  const int n = std::min(a.max_len, a.from.cap);
+  (n <= 512 ? launch_select<64, 8> : n <= 2048 ? launch_select<256, 8> : n <= 8192 ? launch_select<1024, 8>
+   : n <= 16384 ? launch_select<1024, 16> : n <= 32768 ? launch_select<1024, 32> : launch_select<1024, 0>)(a, units, st);
   const hipError_t err = hipGetLastError();
   if (err != hipSuccess) return err;
-  hipLaunchKernelGGL(evict_copy, dim3(units, kShares, 3), dim3(kCT), 0, st, a);
+  const unsigned shares = (unsigned)std::min<int64_t>((a.cap * (a.row_bytes / 16) + kCT - 1) / kCT, 32);
+  hipLaunchKernelGGL(evict_copy, dim3(units, shares, 3), dim3(kCT), 0, st, a);
   return hipGetLastError();
 }
 
