@@ -18,10 +18,10 @@
 // Two forms:
 //   many rows -- NW waves of 32 rows each share every tile of rows in LDS;
 //                tiles are double-buffered, copied from memory to LDS directly;
-//   few rows  -- where no sequence has more than 32 rows (16 in fp32; a decode
-//                step): one column of rows, each wave walks its own tiles of 32 (16)
-//                keys, without a barrier, and the waves' results are joined at the
-//                end.
+//   few rows  -- where no sequence has more than 32 rows (64 in fp32; a decode
+//                step): a column of 32 (16) rows, each wave walks its own tiles of 32
+//                (16) keys, without a barrier, and the waves' results are joined at
+//                the end.
 // Where the (tile, kv head) pairs are too few to fill the GPU the cached rows are
 // cut into spans, and attn_merge joins their records.  The span is found on the
 // device from the sequences' own lengths, as the shortest with which the spans of
@@ -45,10 +45,12 @@ struct AttnArgs {
   int64_t q_token, q_head, o_token, o_head;  // in elements
   float *lse;     // [n_tokens][hq] or null
   float scale2, scale2_lo;  // scale * log2(e), and what its rounding left
+  int single;     // no spans, and a tile per sequence
   int splits;     // (tile, span) units that may run at once, per kv head; 0: no spans
   float *rec;     // [unit * hkv][rows][D] fp32, then [unit * hkv][rows][2]
   int64_t rec_ml; // where the second array starts, in floats
   int *span;      // the span, for attn_merge
+  int parts;      // of a row's spans in attn_merge, a power of two
 };
 
 constexpr double kLog2e = 1.4426950408889634074;
@@ -437,7 +439,7 @@ template <int BM> struct Share {
   __device__ __forceinline__ bool find(const AttnArgs &a, int block, int round, int wave_row) {
     kvh = block % a.hkv;
     int span = kWhole;
-    if (BM <= 32 && !a.splits) {
+    if (BM <= 32 && a.single) {
       // no spans and a tile per sequence: many sequences, not searched one by one
       t.b = block / a.hkv;
       t.s = sequence(a.c, t.b, a.kv.cap);
@@ -857,37 +859,53 @@ template <int D> __global__ __launch_bounds__(kFewWaves * kWave, 2) void attn_fe
   if (w.live) write_row<T, D, 16, BN>(a, w, o, m, l, 4 * quarter, 16, quarter == 0, taken);
 }
 
-// Joins the records of a tile's spans: four elements of a row per lane, all spans in
-// one pass with the running maximum, so that their loads are in flight together.
-template <int D> constexpr int merge_rows() { return 256 / (D / 4); }  // per workgroup
+// Joins the records of a tile's spans: four elements of a row per lane, and a row's
+// spans dealt to `parts` groups of such lanes, which each take theirs in one pass with
+// the running maximum and are joined in LDS.
+constexpr int kMaxParts = 32;
 
 template <typename T, int D, int BM>
-__global__ __launch_bounds__(256) void attn_merge(AttnArgs a) {
+__global__ __launch_bounds__(kMaxParts * (D / 4)) void attn_merge(AttnArgs a) {
+  constexpr int W = D / 4;  // lanes of a row
+  __shared__ f32x4_t so[kMaxParts * W];
+  __shared__ float2 sml[kMaxParts];
   const int kvh = blockIdx.x % a.hkv, span = *a.span;
   const Lanes<BM> lanes(a);
   Tile t;
   if (span == kWhole || !locate<BM, false>(a, lanes, span, blockIdx.x / a.hkv, t) || t.n_split == 1) return;
-  const int in = blockIdx.y * merge_rows<D>() + threadIdx.x / (D / 4), e = threadIdx.x % (D / 4) * 4;
-  const int r = t.row0 + in;
-  if (r >= t.rows) return;
+  const int group = threadIdx.x / W, e = threadIdx.x % W * 4;
+  const int n_rows = blockDim.x / W / a.parts, part = group / n_rows;
+  const int in = blockIdx.y * n_rows + group % n_rows, r = t.row0 + in;
   const int own = t.s.len - t.s.n_new + r / a.g;
   const int token = t.s.first + r / a.g, head = kvh * a.g + r % a.g;
   // spans that hold a row this one sees; the others wrote nothing it needs
-  const int n = own < 0 ? 0 : min(own / span + 1, t.n_split);
+  const int n = r >= t.rows || own < 0 ? 0 : min(own / span + 1, t.n_split);
   const int64_t stride = (int64_t)a.hkv * BM, at = ((int64_t)t.unit0 * a.hkv + kvh) * BM + in;
   const float *ml = a.rec + a.rec_ml + 2 * at, *rec = a.rec + at * D + e;
   float m = -INFINITY, l = 0.0f;
   f32x4_t o = {};
-#pragma unroll 8
-  for (int s = 0; s < n; ++s) {
-    const float2 x = *reinterpret_cast<const float2 *>(ml + 2 * s * stride);
-    const f32x4_t v = *reinterpret_cast<const f32x4_t *>(rec + s * stride * D);
+  auto join = [&](float2 x, const f32x4_t &v) {
     const float top = fmaxf(m, x.x), base = top == -INFINITY ? 0.0f : top;
     const float f = __builtin_amdgcn_exp2f(m - base), w = __builtin_amdgcn_exp2f(x.x - base);
     m = top;
     l = l * f + x.y * w;
     o = o * f + v * w;
+  };
+  const int count = n > part ? (n - part - 1) / a.parts + 1 : 0;
+  const int64_t step = stride * a.parts;
+  ml += 2 * part * stride;
+  rec += part * stride * D;
+#pragma unroll 8
+  for (int s = 0; s < count; ++s)
+    join(*reinterpret_cast<const float2 *>(ml + 2 * s * step), *reinterpret_cast<const f32x4_t *>(rec + s * step * D));
+  if (a.parts > 1) {
+    so[threadIdx.x] = o;
+    if (e == 0) sml[group] = make_float2(m, l);
+    __syncthreads();
+    if (part == 0)
+      for (int g = group + n_rows; g < n_rows * a.parts; g += n_rows) join(sml[g], so[g * W + threadIdx.x % W]);
   }
+  if (part > 0 || r >= t.rows) return;
   const f32x4_t x = o * (l == 0.0f ? 0.0f : 1.0f / l);
   unsigned char *out = a.out + (token * a.o_token + head * a.o_head) * (int64_t)sizeof(T);
   if constexpr (sizeof(T) == 4)
@@ -901,7 +919,15 @@ __global__ __launch_bounds__(256) void attn_merge(AttnArgs a) {
 template <typename T, int D> hipError_t launch_typed(AttnArgs a, const AttnPlan &p, hipStream_t st) {
   constexpr bool h = sizeof(T) == 2;
   constexpr int BM = kAttnWaves * 32, BF = h ? 32 : 16;
-  const dim3 grid(p.units * a.hkv), merge(p.tiles * a.hkv, p.rows / merge_rows<D>());
+  const dim3 grid(p.units * a.hkv);
+  // As many parts per row as there can be spans, and all lanes run at once (256 CUs
+  // of 2048 lanes).  (One token over 32768 rows of 4 kv heads, 128 spans: 39.5 us
+  // with one part, 7.9 with 32.)
+  const int64_t lanes = (int64_t)p.tiles * a.hkv * p.rows * (D / 4);
+  a.parts = 1;
+  while (a.parts < kMaxParts && a.parts < p.splits - p.tiles && 2 * a.parts * lanes <= 256 * 2048) a.parts *= 2;
+  const int threads = std::max(a.parts * (D / 4), 256), n_rows = threads / (D / 4) / a.parts;
+  const dim3 merge(p.tiles * a.hkv, p.rows / n_rows);
   a.rec_ml = (int64_t)p.units * a.hkv * p.rows * D;
   if (!p.few)
     hipLaunchKernelGGL((attn_many<T, D, kAttnWaves, h ? 64 : 32>), grid, dim3(kAttnWaves * kWave), 0, st, a);
@@ -912,9 +938,9 @@ template <typename T, int D> hipError_t launch_typed(AttnArgs a, const AttnPlan 
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || !p.splits) return e;
   if (p.few)
-    hipLaunchKernelGGL((attn_merge<T, D, BF>), merge, dim3(256), 0, st, a);
+    hipLaunchKernelGGL((attn_merge<T, D, BF>), merge, dim3(threads), 0, st, a);
   else
-    hipLaunchKernelGGL((attn_merge<T, D, BM>), merge, dim3(256), 0, st, a);
+    hipLaunchKernelGGL((attn_merge<T, D, BM>), merge, dim3(threads), 0, st, a);
   return hipGetLastError();
 }
 
@@ -930,7 +956,10 @@ AttnPlan plan_chunk_attn(const smallkv_chunk_t &c, const smallkv_cache_t &kv, co
   const int64_t rows = (int64_t)c.max_new * g;
   const bool f32 = kv.dtype == SMALLKV_F32;
   const int few = f32 ? 16 : 32;
-  p.few = rows <= few;
+  // (fp32, whose products bound it, up to four tiles: 28 rows over 8 x 4096 and 32 x 2048
+  // cached rows 46 us against 96, 56 rows 143 against 180, 112 rows 264 against 200;
+  // bf16, 56 rows over 32 x 2048: 38 us against 35)
+  p.few = rows <= (f32 ? 64 : 32);
   p.rows = p.few ? few : kAttnWaves * 32;
   // no more tiles than this, whatever the sequences' lengths
   p.tiles = (int)std::min<int64_t>(c.batch * ceil_div(rows, p.rows), (int64_t)c.n_tokens * g / p.rows + c.batch);
@@ -966,6 +995,7 @@ hipError_t launch_chunk_attn(const smallkv_chunk_t &c, const smallkv_cache_t &kv
   a.scale2 = (float)(q.scale * kLog2e);
   a.scale2_lo = (float)(q.scale * kLog2e - a.scale2);
   a.splits = p.splits;
+  a.single = p.few && !p.splits && p.tiles <= c.batch;
   a.span = static_cast<int *>(ws);
   if (ws) a.rec = reinterpret_cast<float *>(static_cast<char *>(ws) + kSpanBytes);
   if (kv.dtype == SMALLKV_F32)

@@ -54,6 +54,10 @@ CASES = [
     ("more new tokens than rows", [(5, 9), (30, 30), (0, 3)], 8, 2, 64, BF16, 8, False),
     ("many query heads, one token", [(400, 1), (70, 1)], 64, 1, 128, BF16, 16, False),
     ("long", [(9000, 1), (8191, 40)], 8, 2, 64, BF16, 256, False),
+    ("few rows in tiles f32", [(300, 9), (41, 2), (9, 9), (17, 3)], 14, 2, 64, F32, 16, True),
+    ("few rows in tiles over spans f32", [(5000, 8), (70, 1), (1100, 5)], 16, 2, 128, F32, 64, False),
+    ("one token over many spans", [(20001, 1)], 14, 2, 128, BF16, 0, False),
+    ("tokens and a chunk over many spans", [(16000, 1), (3, 1), (12000, 37)], 14, 2, 64, BF16, 32, False),
 ]
 IDS = [c[0].replace(" ", "-") for c in CASES]
 
@@ -503,6 +507,13 @@ def test_evict_caps_and_rows_as_positions():
 
 def test_evict_long():
     evict_case([40000, 9000], [300, 100], [20, 1], 4, 2, 1, 64, BF16, 256, 0)
+
+
+@pytest.mark.parametrize("longest", [512, 513, 2049, 8193, 16385, 32768])
+def test_evict_lengths(longest):
+    """Lengths around those at which the lanes' share of the keys changes, each batch
+    with short sequences beside the longest."""
+    evict_case([longest, 37, longest - 1, 1], [250, 30, 511, 1], [16, 2, 0, 1], 4, 1, 1, 64, BF16, 64, 0)
 
 
 @pytest.mark.parametrize("group", [1, 2])
