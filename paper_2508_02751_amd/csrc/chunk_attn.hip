@@ -386,15 +386,15 @@ __device__ __forceinline__ void full_tile(State<T, D> &st, const QFrag<T, D> &q,
   for (int b = 0; b < BN / 32; ++b) values32<T, D>(sv, 32 * b, s[b], st.o);
 }
 
-// Any other, 32 keys at a time.  own: the lane's own row; valid: bit t set iff key
-// row0 + t exists.
+// Any other, 32 keys at a time.  own: the lane's own row; highest: of the wave's; valid:
+// bit t set iff key row0 + t exists.
 template <typename T, int D, int BN>
 __device__ __forceinline__ void masked_tile(State<T, D> &st, const QFrag<T, D> &q, const unsigned char *sk,
-                                            const unsigned char *sv, int row0, int own, uint64_t valid,
-                                            float c, float c_lo) {
+                                            const unsigned char *sv, int row0, int own, int highest,
+                                            uint64_t valid, float c, float c_lo) {
   const int half = (threadIdx.x & (kWave - 1)) >> 5;
 #pragma unroll 1
-  for (int k0 = 0; k0 < BN; k0 += 32) {
+  for (int k0 = 0; k0 < BN && row0 + k0 <= highest; k0 += 32) {
     f32x16_t s[1] = {logits32<T, D>(sk, k0, q)};
     const uint32_t bits = (uint32_t)(valid >> k0) >> (4 * half);
 #pragma unroll
@@ -408,9 +408,9 @@ __device__ __forceinline__ void masked_tile(State<T, D> &st, const QFrag<T, D> &
 }
 
 // Adds the infinite and NaN values of keys from..to to the lane's own elements (groups
-// of four, `step` apart from `at` on) of an output row that is written already (any
+// of W, `step` apart from `at` on) of an output row that is written already (any
 // weight > 0 leaves them what they are).
-template <typename O, typename T, int D>
+template <typename O, typename T, int D, int W>
 __device__ __forceinline__ void give_back(const AttnArgs &a, int b, const unsigned char *v, void *out, int from, int to,
                                           int at, int step) {
 #pragma unroll 1
@@ -420,7 +420,7 @@ __device__ __forceinline__ void give_back(const AttnArgs &a, int b, const unsign
 #pragma unroll 1
     for (int e0 = at; e0 < D; e0 += step)
 #pragma unroll 1
-      for (int e = e0; e < e0 + 4; ++e) {
+      for (int e = e0; e < e0 + W; ++e) {
         const float x = elem<T>::load1(v + off, e);
         if (!(fabsf(x) <= 3.402823466e38f)) elem<O>::store1(out, e, elem<O>::load1(out, e) + x);
       }
@@ -489,7 +489,7 @@ __device__ __forceinline__ void write_row(const AttnArgs &a, const Share<BM> &w,
       a.rec[a.rec_ml + 2 * row] = m;
       a.rec[a.rec_ml + 2 * row + 1] = l;
     }
-    if (taken) give_back<float, T, D>(a, w.t.b, w.v, o, from, to, at, step);
+    if (taken) give_back<float, T, D, 4>(a, w.t.b, w.v, o, from, to, at, step);
     return;
   }
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;  // (0: the row sees no key)
@@ -502,16 +502,40 @@ __device__ __forceinline__ void write_row(const AttnArgs &a, const Share<BM> &w,
     else
       *reinterpret_cast<bf16x4_t *>(o + (at + i * step) * 2) = __builtin_convertvector(y, bf16x4_t);
   }
-  if (taken) give_back<T, T, D>(a, w.t.b, w.v, o, from, to, at, step);
+  if (taken) give_back<T, T, D, 4>(a, w.t.b, w.v, o, from, to, at, step);
   if (a.lse && writes)
     a.lse[(int64_t)w.token * a.hq + w.head] = l == 0.0f ? -INFINITY : (m + __log2f(l)) * kLn2;
 }
 
 template <typename T, int D, int BM, int BN>
 __device__ __forceinline__ void write_row(const AttnArgs &a, const Share<BM> &w, const State<T, D> &st, bool taken) {
-  if (!w.live) return;
   const float l = swap_halves_sum(st.l);
   const int half = (threadIdx.x & (kWave - 1)) >> 5;
+  if (sizeof(T) == 2 && w.t.n_split == 1) {
+    // half-waves exchange four elements of 16, so that each lane writes eight at once
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    unsigned char *o = a.out + (w.token * a.o_token + w.head * a.o_head) * 2;
+#pragma unroll
+    for (int j = 0; j < D / 16; ++j) {
+      uint32_t y[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int e = j % 2 * 8 + 2 * i;
+        const f32x2_t v = {st.o[j / 2][e] * inv, st.o[j / 2][e + 1] * inv};
+        y[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2_t));
+      }
+      const auto p = __builtin_amdgcn_permlane32_swap(y[0], y[2], false, false);
+      const auto q = __builtin_amdgcn_permlane32_swap(y[1], y[3], false, false);
+      if (w.live) *reinterpret_cast<uint4 *>(o + j * 32 + half * 16) = make_uint4(p[0], q[0], p[1], q[1]);
+    }
+    if (!w.live) return;
+    if (taken)
+      give_back<T, T, D, 8>(a, w.t.b, w.v, o, max(w.begin, w.first_own + 2 - BN), min(w.end - 1, w.own), 8 * half, 16);
+    if (a.lse && half == 0)
+      a.lse[(int64_t)w.token * a.hq + w.head] = l == 0.0f ? -INFINITY : (st.m + __log2f(l)) * kLn2;
+    return;
+  }
+  if (!w.live) return;
   f32x4_t x[D / 8];
 #pragma unroll
   for (int i = 0; i < D / 8; ++i)
@@ -597,7 +621,7 @@ __global__ __launch_bounds__(NW * kWave, sizeof(T) == 2 ? 2 : 1) void attn_many(
     full = true;
     if (min(row + BN, w.end) - 1 > w.first_own)
       taken |= __syncthreads_or(take_out<T, BN * L::C>(sv, threadIdx.x, NW * kWave));
-    if (!idle && row <= highest) masked_tile<T, D, BN>(st, q, sk, sv, row, w.own, now, a.scale2, a.scale2_lo);
+    if (!idle) masked_tile<T, D, BN>(st, q, sk, sv, row, w.own, highest, now, a.scale2, a.scale2_lo);
     row += BN;
     odd = !odd;
   }
@@ -649,7 +673,7 @@ template <int D> __global__ __launch_bounds__(kFewWaves * kWave, 2) void attn_fe
       taken |= __any(take_out<T, BN * L::C>(sv, lane, kWave));
       wait_lds();
     }
-    masked_tile<T, D, BN>(st, q, sk, sv, row, w.own, (uint32_t)__ballot(off >= 0), a.scale2, a.scale2_lo);
+    masked_tile<T, D, BN>(st, q, sk, sv, row, w.own, w.end, (uint32_t)__ballot(off >= 0), a.scale2, a.scale2_lo);
   };
   if (row < w.end) {
     Ld::template issue_one<false>(off, w.k, sk);
