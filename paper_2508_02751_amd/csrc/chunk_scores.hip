@@ -234,9 +234,11 @@ __global__ __launch_bounds__(kNW * kWave, 2) void few_scores(ScoreArgs a) {
   // whose logits it will hold
   uint4 qf[kFrag];
   {
-    const int r = lane & 31;
+    // rows past the last repeat the first, so that no product of theirs is NaN where
+    // the others' are not (of keys with infinities)
+    const int r = (lane & 31) < rows ? lane & 31 : 0;
     const int64_t t = s.first + r / a.g, h = kvh * a.g + r % a.g;
-    const unsigned char *row = r < rows ? a.q + t * a.q_token + h * a.q_head : zero_row;
+    const unsigned char *row = rows > 0 ? a.q + t * a.q_token + h * a.q_head : zero_row;
 #pragma unroll
     for (int i = 0; i < kFrag; ++i)
       qf[i] = reinterpret_cast<const uint4 *>(row)[kBf16 ? 2 * i + half : half * kFrag + i];
@@ -286,7 +288,7 @@ __global__ __launch_bounds__(kNW * kWave, 2) void few_scores(ScoreArgs a) {
     float p[16];
 #pragma unroll
     for (int i = 0; i < 16; ++i) p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], a.scale2, -lse2[i]));
-    if (base + 31 > pos0 || __any(!exists)) {  // some row may not see some key
+    if (base + 31 > pos0 || rows == 0 || __any(!exists)) {  // some row may not see some key
 #pragma unroll
       for (int i = 0; i < 16; ++i) p[i] = exists && key <= own[i] ? p[i] : 0.0f;
     }

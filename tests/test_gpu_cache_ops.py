@@ -225,6 +225,36 @@ def test_nan_keys_of_later_tokens(dtype, d):
     assert bool(torch.isnan(call.out[59]).all())
 
 
+@pytest.mark.parametrize("new", [1, 3, 40])
+@pytest.mark.parametrize("dtype,d", [(BF16, 128), (F32, 64)])
+def test_logits_of_minus_infinity(dtype, d, new):
+    """Rows that every query sees with a logit of -inf count as little as absent ones."""
+    S = lib()
+    c = R.Case([(300, new), (70, min(new, 1))], 8, 2, d, dtype, 8, seed=37)
+    c.q = c.q.abs()
+    c.k[int(c.table[0, 5]), :, :, 3] = -math.inf
+    chunk, cache, q = c.to(DEV)
+    c.table = c.table.clone()
+    c.table[0, 5] = -1  # for the plain form
+    want, wl, tol, ltol = R.attention(c)
+    log(f"[-inf] {dtype} {new}")
+    if new:
+        call = S.prepare_chunk_attn(chunk, cache, q, c.scale)
+        call.run()
+    lse = wl.float()
+    for heads in (c.hq, c.hk):
+        before = torch.rand(c.B, heads, c.rows, generator=c.gen)
+        out = before.to(DEV)
+        S.prepare_chunk_scores(chunk, cache, q, lse.to(DEV), c.scale, out, before=out).run()
+        torch.cuda.synchronize()
+        ws, wt = R.scores(c, lse, before, heads == c.hk)
+        for b, (n, _) in enumerate(c.lens):
+            within(out[b, :, :n], ws[b, :, :n], wt[b, :, :n], f"scores {b}")
+    if new:
+        within(call.out, want, tol, "out")
+        within(call.lse, wl, ltol, "lse")
+
+
 def test_large_logits():
     """Logits of several hundred with a maximum that moves many times."""
     S = lib()
