@@ -494,7 +494,8 @@ typedef struct {
  * cached rows (token i of n: row len[b] - n + i).  A sequence may have none.
  * Device values are clamped (start into [0, n_tokens], the new tokens to
  * max_new, len to max_len and the cache's rows); tokens in no sequence are
- * neither read nor written, and neither are those past max_new. */
+ * neither read nor written, and neither are those past max_new.  With n_tokens 0
+ * the pointers to the tokens' own operands may be NULL. */
 typedef struct {
   int32_t batch;     /* B >= 1 */
   int32_t n_tokens;  /* packed tokens, >= 0 */
@@ -576,8 +577,8 @@ int smallkv_append(const smallkv_chunk_t *chunk, const smallkv_cache_t *cache,
 /* For every new token and query head: the softmax attention over the cached
  * rows up to and including the token's own (logits scale * <q, K_r>):
  *   out = sum softmax_r V_r,  lse = ln sum_r exp(logit_r)
- * A token that sees no row (its row number is negative, or every page absent)
- * gets out = 0 and lse = -inf.  Infinities and NaN in rows a token does not see
+ * A token that sees no row (its row number is negative, or every page absent),
+ * or whose logits are all -inf, gets out = 0 and lse = -inf.  Infinities and NaN in rows a token does not see
  * do not reach it.  bf16 models: the probabilities are rounded to bf16 for the
  * product with V (2^-8 relative); sums, logits and statistics are fp32.
  * ws: smallkv_chunk_attn_workspace_size (may be 0); calls that share one must

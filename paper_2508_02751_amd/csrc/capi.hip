@@ -230,7 +230,7 @@ int check_chunk(const smallkv_chunk_t *c, const smallkv_cache_t *kv) {
 int check_queries(const smallkv_chunk_t *c, const smallkv_cache_t *kv, const smallkv_queries_t *q) {
   const int rc = check_chunk(c, kv);
   if (rc) return rc;
-  if (!q || !q->q || q->n_heads < 1 || q->n_heads % kv->n_heads) return SMALLKV_EINVAL;
+  if (!q || (!q->q && c->n_tokens > 0) || q->n_heads < 1 || q->n_heads % kv->n_heads) return SMALLKV_EINVAL;
   if (!(q->scale > 0.0f) || !(q->scale <= 3.402823e38f)) return SMALLKV_EINVAL;
   if (!aligned16(q->q) || !stride_ok(q->token_stride, kv->dtype) || !stride_ok(q->head_stride, kv->dtype))
     return SMALLKV_EINVAL;
@@ -245,7 +245,7 @@ int check_queries(const smallkv_chunk_t *c, const smallkv_cache_t *kv, const sma
 int check_attn(const smallkv_chunk_t *c, const smallkv_cache_t *kv, const smallkv_queries_t *q) {
   const int rc = check_queries(c, kv, q);
   if (rc) return rc;
-  if (!q->out || !aligned16(q->out) || !stride_ok(q->out_token_stride, kv->dtype) ||
+  if ((!q->out && c->n_tokens > 0) || !aligned16(q->out) || !stride_ok(q->out_token_stride, kv->dtype) ||
       !stride_ok(q->out_head_stride, kv->dtype))
     return SMALLKV_EINVAL;
   if ((c->n_tokens > 1 && q->out_token_stride < kv->head_dim) ||
@@ -257,7 +257,8 @@ int check_attn(const smallkv_chunk_t *c, const smallkv_cache_t *kv, const smallk
 int check_append(const smallkv_chunk_t *c, const smallkv_cache_t *kv, const smallkv_append_t *a) {
   const int rc = check_chunk(c, kv);
   if (rc) return rc;
-  if (!a || !a->q || !a->k || !a->v || !a->q_out || a->n_q_heads < 1) return SMALLKV_EINVAL;
+  if (!a || a->n_q_heads < 1) return SMALLKV_EINVAL;
+  if (c->n_tokens > 0 && (!a->q || !a->k || !a->v || !a->q_out)) return SMALLKV_EINVAL;
   if (a->n_q_heads % kv->n_heads) return SMALLKV_EINVAL;
   if (!writable(*kv)) return SMALLKV_EINVAL;
   if ((c->n_tokens > 1 && a->q_out_token_stride < kv->head_dim) ||
@@ -271,7 +272,7 @@ int check_append(const smallkv_chunk_t *c, const smallkv_cache_t *kv, const smal
                              a->q_out_head_stride};
   for (const int64_t s : strides)
     if (!stride_ok(s, kv->dtype)) return SMALLKV_EINVAL;
-  if (a->q_out == a->q && (a->q_out_token_stride != a->q_token_stride ||
+  if (a->q_out && a->q_out == a->q && (a->q_out_token_stride != a->q_token_stride ||
                            a->q_out_head_stride != a->q_head_stride))
     return SMALLKV_EINVAL;
   if (a->rot_dim < 0 || a->rot_dim > kv->head_dim || a->rot_dim % 2) return SMALLKV_EINVAL;
@@ -625,7 +626,7 @@ int smallkv_chunk_scores(const smallkv_chunk_t *chunk, const smallkv_cache_t *ca
                          float *out, int64_t score_rows, int64_t seq_stride, void *stream) {
   const int rc = check_queries(chunk, cache, queries);
   if (rc) return rc;
-  if (!queries->lse || !out || score_rows < chunk->max_len) return SMALLKV_EINVAL;
+  if ((!queries->lse && chunk->n_tokens > 0) || !out || score_rows < chunk->max_len) return SMALLKV_EINVAL;
   if (n_score_heads != queries->n_heads && n_score_heads != cache->n_heads) return SMALLKV_EINVAL;
   if (score_rows > INT32_MAX || seq_stride < n_score_heads * score_rows) return SMALLKV_EINVAL;
   if (((int64_t)chunk->max_len + 127) / 128 * chunk->batch * cache->n_heads > (1 << 30) ||

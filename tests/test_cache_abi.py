@@ -141,6 +141,11 @@ def test_no_tokens_is_no_work():
     assert L.smallkv_chunk_attn_workspace_size(C.byref(ch), C.byref(ca), C.byref(q), C.byref(n)) == S.OK
     assert L.smallkv_chunk_attn(C.byref(ch), C.byref(ca), C.byref(q), P, n.value, None) == S.OK
     assert L.smallkv_append(C.byref(ch), C.byref(ca), C.byref(a), None) == S.OK
+    # and no operands of the tokens
+    q, a = queries(q=None, out=None, lse=None), append(q=None, k=None, v=None, q_out=None)
+    assert L.smallkv_chunk_attn_workspace_size(C.byref(ch), C.byref(ca), C.byref(q), C.byref(n)) == S.OK
+    assert L.smallkv_chunk_attn(C.byref(ch), C.byref(ca), C.byref(q), P, n.value, None) == S.OK
+    assert L.smallkv_append(C.byref(ch), C.byref(ca), C.byref(a), None) == S.OK
 
 
 def test_scores_refusals():

@@ -225,7 +225,7 @@ def test_nan_keys_of_later_tokens(dtype, d):
     assert bool(torch.isnan(call.out[59]).all())
 
 
-@pytest.mark.parametrize("new", [1, 3, 40])
+@pytest.mark.parametrize("new", [0, 1, 3, 40])
 @pytest.mark.parametrize("dtype,d", [(BF16, 128), (F32, 64)])
 def test_logits_of_minus_infinity(dtype, d, new):
     """Rows that every query sees with a logit of -inf count as little as absent ones."""
@@ -362,6 +362,52 @@ def test_another_stream_and_a_graph():
         assert torch.equal(got[0], call.out) and torch.equal(got[1], out)
         if scale == 1.0:
             assert torch.equal(got[0], eager[0]) and torch.equal(got[1], eager[1])
+
+
+def test_a_graph_follows_the_lengths():
+    """A captured decode step of capacity lengths, replayed as its sequences grow."""
+    S = lib()
+    cap, hq, hk, d = 700, 8, 2, 64
+    c = R.Case([(cap, 1)] * 3, hq, hk, d, BF16, 16, seed=43)
+    _, cache, q = c.to(DEV)
+    start = torch.arange(4, dtype=torch.int32, device=DEV)
+    length = torch.zeros(3, dtype=torch.int32, device=DEV)
+    chunk = S.ChunkSpec(start, length, 3, 1, cap)
+    kv = torch.randn(3, 2 * hk, d, generator=c.gen).to(DEV, BF16)
+    freq, amp = S.rope_freqs(d, 10000.0)
+    add = S.prepare_append(chunk, cache, S.RopeSpec(freq, S.ROPE_HALF, amp), q, kv[:, :hk], kv[:, hk:])
+    call = S.prepare_chunk_attn(chunk, cache, add.q_out, c.scale)
+    sc = torch.zeros(3, hk, cap, device=DEV)
+    score = S.prepare_chunk_scores(chunk, cache, add.q_out, call.lse, c.scale, sc, before=sc)
+    calls = (add, call, score)
+
+    def state():
+        return [t.clone() for t in (cache.k, cache.v, call.out, call.lse, sc)]
+    log("[graph] lengths")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        for x in calls:
+            x.run()
+    for lens in ((1, 300, 40), (2, 301, 0), (3, 302, 699), (400, 0, 700), (401, 1, 1)):
+        length.copy_(torch.tensor(lens, dtype=torch.int32))
+        first = state()
+        graph.replay()
+        torch.cuda.synchronize()
+        got = state()
+        for t, x in zip((cache.k, cache.v, call.out, call.lse, sc), first):
+            t.copy_(x)
+        for x in calls:
+            x.run()
+        torch.cuda.synchronize()
+        for x, y in zip(got, state()):
+            bits = torch.int16 if x.dtype == BF16 else torch.int32
+            assert torch.equal(x.view(bits), y.view(bits))
+        now = R.Case([(n, 1) for n in lens], hq, hk, d, BF16, 16, seed=43, cap=cap)
+        now.table, now.q = c.table, add.q_out.cpu()
+        now.k, now.v = cache.k.cpu(), cache.v.cpu()
+        want, wl, tol, ltol = R.attention(now)
+        within(call.out, want, tol, "out")
+        within(call.lse, wl, ltol, "lse")
 
 
 # ------------------------------------------------------------------ append --

@@ -198,6 +198,31 @@ def test_scores_start_the_accumulated_selection():
             assert sorted(order.tolist()) == crit[j][:k].tolist()
 
 
+def test_no_new_tokens():
+    """A chunk without tokens leaves a cache, its scores and its lengths as they were."""
+    from paper_2508_02751_amd import pipeline as P
+    from paper_2508_02751_amd import smallkv as S
+    freq, amp = S.rope_freqs(64, 10000.0)
+    c = P.ModelCache(2, 1, 4, 2, 64, 40, S.RopeSpec(freq, S.ROPE_HALF, amp), torch.bfloat16, DEV,
+                     keep_scores=True)
+    g = torch.Generator().manual_seed(3)
+
+    def step(*new):
+        T = c.begin(new)
+        x = [torch.randn(T, h, 64, generator=g).to(DEV, torch.bfloat16) for h in (4, 2, 2)]
+        return c.layer(0, *x)
+    log("[pipeline] no new tokens")
+    step(20, 9)
+    before = c.k.clone(), c.v.clone(), c.scores.clone()
+    out, q = step(0, 0)
+    assert out.shape == (0, 4, 64) and q.shape == (0, 4, 64)
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(before, (c.k, c.v, c.scores)))
+    step(0, 1)
+    torch.cuda.synchronize()
+    assert c.rows == [20, 10] and torch.equal(c.scores[0], before[2][0])
+
+
 def test_begin_refuses():
     from paper_2508_02751_amd import pipeline as P
     from paper_2508_02751_amd import smallkv as S
