@@ -159,7 +159,7 @@ __global__ __launch_bounds__(256) void append(AppendArgs a) {
     }
     const int turning = half / V;  // slots of turning halves
     const bool halves = FORM == kHalf && !value && c < turning;
-    const int p0 = halves ? c : FORM == kHalf && !value ? 2 * c : 2 * c;
+    const int p0 = halves ? c : 2 * c;
     const int p1 = halves ? c + turning : p0 + 1;
     uint4 x = reinterpret_cast<const uint4 *>(src)[p0], y = reinterpret_cast<const uint4 *>(src)[p1];
     if (halves) {

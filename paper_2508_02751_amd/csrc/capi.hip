@@ -211,6 +211,9 @@ int check_cache(const smallkv_cache_t *c, int batch) {
   return SMALLKV_OK;
 }
 
+// Workgroups of 256 threads in one launch: the threads are counted in 32 bits.
+constexpr int64_t kMaxGroups = (1 << 24) - 1;
+
 // Rows that are written: no broadcast strides.
 bool writable(const smallkv_cache_t &c) {
   return (c.page_rows == 1 || c.row_stride >= c.head_dim) && (c.n_heads == 1 || c.head_stride >= c.head_dim) &&
@@ -251,6 +254,7 @@ int check_attn(const smallkv_chunk_t *c, const smallkv_cache_t *kv, const smallk
   if ((c->n_tokens > 1 && q->out_token_stride < kv->head_dim) ||
       (q->n_heads > 1 && q->out_head_stride < kv->head_dim))
     return SMALLKV_EINVAL;
+  if ((int64_t)plan_chunk_attn(*c, *kv, *q).units * kv->n_heads > kMaxGroups) return SMALLKV_EUNSUPPORTED;
   return SMALLKV_OK;
 }
 
@@ -281,7 +285,7 @@ int check_append(const smallkv_chunk_t *c, const smallkv_cache_t *kv, const smal
   if (!(a->amplitude == a->amplitude)) return SMALLKV_EINVAL;
   if (a->row_pos && (a->pos_rows < 1 || a->pos_rows > INT32_MAX || a->pos_seq_stride < kv->n_heads * a->pos_rows))
     return SMALLKV_EINVAL;
-  if (a->n_q_heads > (1 << 16)) return SMALLKV_EUNSUPPORTED;
+  if (a->n_q_heads > (1 << 16) || c->n_tokens > kMaxGroups) return SMALLKV_EUNSUPPORTED;
   return SMALLKV_OK;
 }
 
@@ -298,7 +302,9 @@ int check_evict(const smallkv_evict_t *e) {
   if (e->out_pos == e->row_pos || e->out_scores == e->scores) return SMALLKV_EINVAL;
   if (e->n_score_heads < 1 || e->n_score_heads % e->from.n_heads) return SMALLKV_EINVAL;
   if (e->score_rows < e->max_len || (e->row_pos && e->pos_rows < e->max_len)) return SMALLKV_EINVAL;
-  if (e->n_score_heads / e->from.n_heads > 64 || e->max_len > (1 << 20)) return SMALLKV_EUNSUPPORTED;
+  if (e->n_score_heads / e->from.n_heads > 64 || e->max_len > (1 << 20) ||
+      (int64_t)e->batch * e->from.n_heads > kMaxGroups / 4)
+    return SMALLKV_EUNSUPPORTED;
   return SMALLKV_OK;
 }
 
@@ -629,7 +635,7 @@ int smallkv_chunk_scores(const smallkv_chunk_t *chunk, const smallkv_cache_t *ca
   if ((!queries->lse && chunk->n_tokens > 0) || !out || score_rows < chunk->max_len) return SMALLKV_EINVAL;
   if (n_score_heads != queries->n_heads && n_score_heads != cache->n_heads) return SMALLKV_EINVAL;
   if (score_rows > INT32_MAX || seq_stride < n_score_heads * score_rows) return SMALLKV_EINVAL;
-  if (((int64_t)chunk->max_len + 127) / 128 * chunk->batch * cache->n_heads > (1 << 30) ||
+  if (((int64_t)chunk->max_len + 127) / 128 * chunk->batch * cache->n_heads > kMaxGroups ||
       queries->n_heads / cache->n_heads > 65535)
     return SMALLKV_EUNSUPPORTED;
   return status_of(launch_chunk_scores(*chunk, *cache, *queries, n_score_heads, before, out, score_rows,

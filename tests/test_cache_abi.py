@@ -121,6 +121,28 @@ def test_a_dense_cache_has_a_page_per_sequence():
     assert try_attn(chunk(batch=3), dense(), queries()) == S.EINVAL
 
 
+def test_launches_stay_below_their_limits():
+    """Calls whose workgroups a launch cannot count are refused on the host."""
+    L = S.lib()
+    n = C.c_size_t()
+    big = dict(batch=1 << 22, n_tokens=1 << 22, max_new=1)
+    assert try_attn(chunk(**big), cache(), queries()) == S.EUNSUPPORTED
+    assert try_attn(chunk(**dict(big, batch=(1 << 22) - 1)), cache(), queries()) == S.OK
+    many = chunk(batch=1, n_tokens=1 << 30, max_new=1 << 24)  # 7 query heads a kv head
+    assert try_attn(many, cache(), queries()) == S.OK         # 2^24 * 7 / 128 tiles * 4
+    assert try_attn(chunk(batch=8, n_tokens=1 << 27, max_new=1 << 24), cache(), queries()) == S.EUNSUPPORTED
+    ca, q = cache(table_width=1 << 20), queries()
+    ch = chunk(batch=1 << 10, max_len=1 << 24)
+    assert L.smallkv_chunk_scores(C.byref(ch), C.byref(ca), C.byref(q), 28, None, P, 1 << 24, 1 << 40,
+                                  None) == S.EUNSUPPORTED
+    ch, a = chunk(n_tokens=1 << 24), append()
+    assert L.smallkv_append(C.byref(ch), C.byref(cache()), C.byref(a), None) == S.EUNSUPPORTED
+    e = evict(batch=1 << 20)
+    assert L.smallkv_evict_workspace_size(C.byref(e), C.byref(n)) == S.EUNSUPPORTED
+    e = evict(batch=(1 << 20) - 1)
+    assert L.smallkv_evict_workspace_size(C.byref(e), C.byref(n)) == S.OK
+
+
 def test_attention_needs_its_workspace():
     n = C.c_size_t()
     ch, ca, q = chunk(batch=1, n_tokens=1, max_new=1, max_len=100000), cache(table_width=6250), queries()
