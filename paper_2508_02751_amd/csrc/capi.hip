@@ -242,6 +242,7 @@ int check_queries(const smallkv_chunk_t *c, const smallkv_cache_t *kv, const sma
   // rows (token, query head of a group) and tiles of 32 of them are counted in 32 bits
   const int64_t rows = (int64_t)c->max_new * (q->n_heads / kv->n_heads);
   if (rows > (1 << 30) || (rows + 31) / 32 * c->batch * kv->n_heads > (1 << 30)) return SMALLKV_EUNSUPPORTED;
+  if ((int64_t)plan_chunk_attn(*c, *kv, *q).units * kv->n_heads > kMaxGroups) return SMALLKV_EUNSUPPORTED;
   return SMALLKV_OK;
 }
 
@@ -254,7 +255,6 @@ int check_attn(const smallkv_chunk_t *c, const smallkv_cache_t *kv, const smallk
   if ((c->n_tokens > 1 && q->out_token_stride < kv->head_dim) ||
       (q->n_heads > 1 && q->out_head_stride < kv->head_dim))
     return SMALLKV_EINVAL;
-  if ((int64_t)plan_chunk_attn(*c, *kv, *q).units * kv->n_heads > kMaxGroups) return SMALLKV_EUNSUPPORTED;
   return SMALLKV_OK;
 }
 
