@@ -364,6 +364,76 @@ def test_another_stream_and_a_graph():
             assert torch.equal(got[0], eager[0]) and torch.equal(got[1], eager[1])
 
 
+@pytest.mark.parametrize("lens", [[(130, 40), (77, 9)], [(700, 1), (64, 1)]])
+def test_broadcast_queries_and_keys(lens):
+    """One query row for all heads, one layer's rows for all sequences, no lse."""
+    S = lib()
+    c = R.Case(lens, 8, 2, 64, BF16, seed=53)
+    chunk, cache, q = c.to(DEV)
+    n = min(n for n, _ in lens)  # rows that sequence 0 and its readers share
+    chunk = S.ChunkSpec(chunk.start, torch.full_like(chunk.length, n), c.T, c.max_new, c.rows)
+    one, (k, v) = q[:, :1].expand(-1, 8, -1), (x[:1].expand(c.B, -1, -1, -1) for x in (cache.k, cache.v))
+    log("[broadcast]")
+    call = S.prepare_chunk_attn(chunk, S.CacheSpec(k, v), one, c.scale, lse=False)
+    call.run()
+    torch.cuda.synchronize()
+    assert call.lse is None
+    c.lens, c.q = [(n, new) for _, new in lens], one.cpu()
+    c.k, c.v = k.cpu(), v.cpu()
+    want, _, tol, _ = R.attention(c)
+    within(call.out, want, tol, "out")
+
+
+@pytest.mark.parametrize("page", [0, 16])
+def test_offsets_past_32_bits(page):
+    """Caches, queries and outputs whose elements lie more than 2^32 bytes apart: every
+    operator as over compact tensors."""
+    S = lib()
+    hq, hk, d, new = 4, 2, 64, 3
+    c = R.Case([(150, new), (90, new), (130, new)], hq, hk, d, BF16, page, seed=47)
+    chunk, cache, q = c.to(DEV)
+    far = (1 << 31) + 5 * 64  # elements between pages, bf16: past 2^32 bytes
+    pool = torch.empty(far + (1 << 22), dtype=BF16, device=DEV)
+    pool2 = torch.empty_like(pool)
+    n_pages = c.k.shape[0]
+    if page:  # every other page far away: pages of 4 KB, numbered over the whole pool
+        per = page * hk * d
+        spread = torch.tensor([i if i % 2 else far // per + i for i in range(n_pages)], dtype=torch.int32)
+        shape = (pool.numel() // per, hk, page, d)
+        k, v = pool[:shape[0] * per].view(shape), pool2[:shape[0] * per].view(shape)
+        k[spread.long().to(DEV)], v[spread.long().to(DEV)] = cache.k, cache.v
+        wide = S.CacheSpec(k, v, spread[c.table.long()].to(DEV).contiguous())
+    else:
+        st = (far // 2, c.rows * d, d, 1)
+        k, v = (x.as_strided((3, hk, c.rows, d), st) for x in (pool, pool2))
+        k.copy_(cache.k)
+        v.copy_(cache.v)
+        wide = S.CacheSpec(k, v)
+    log(f"[far] page {page}")
+    freq, amp = S.rope_freqs(d, 10000.0)
+    rope = S.RopeSpec(freq, S.ROPE_HALF, amp)
+    kv = torch.randn(c.T, 2 * hk, d, generator=c.gen).to(DEV, BF16)
+    big = torch.empty((c.T - 1) * (far // 8) + hq * d, dtype=BF16, device=DEV)
+    big2 = torch.empty_like(big)
+    fq, fo = (x.as_strided((c.T, hq, d), (far // 8 - far // 8 % 8, d, 1)) for x in (big, big2))
+    fq.copy_(q)
+    outs = []
+    for ca, x, o in ((cache, q.clone(), torch.empty_like(q)), (wide, fq, fo)):
+        S.prepare_append(chunk, ca, rope, x, kv[:, :hk], kv[:, hk:], q_out=x).run()
+        attn = S.prepare_chunk_attn(chunk, ca, x, c.scale, out=o)
+        attn.run()
+        sc = torch.zeros(c.B, hk, c.rows, device=DEV)
+        S.prepare_chunk_scores(chunk, ca, x, attn.lse, c.scale, sc).run()
+        dst = [torch.zeros(c.B, hk, 40, d, dtype=BF16, device=DEV) for _ in range(2)]
+        keep = torch.full((c.B,), 40, dtype=torch.int32, device=DEV)
+        ev = S.prepare_evict(ca, S.CacheSpec(*dst), chunk.length, keep, sc, sinks=2)
+        ev.run()
+        torch.cuda.synchronize()
+        outs.append([x.clone(), o.clone(), attn.lse, sc, *dst, ev.out_pos, ev.held])
+    for x, y in zip(*outs):
+        assert torch.equal(x, y)
+
+
 def test_a_graph_follows_the_lengths():
     """A captured decode step of capacity lengths, replayed as its sequences grow."""
     S = lib()
