@@ -56,8 +56,10 @@ struct AttnArgs {
 constexpr double kLog2e = 1.4426950408889634074;
 constexpr float kLn2 = 0.693147180559945309417f;
 
-// Steps of the many-rows form's spans.
-constexpr int kManyRound = 256;
+// Steps of the many-rows form's spans (whole tiles), and the shortest in steps.  (179
+// tokens over 23719 rows: 86.6 us, 88.9 in steps of 256; 16 over 8192: 25.5 us, 24.1 and
+// twice the records with 128 as the shortest.)
+constexpr int kManyRound = 64, kManyLeast = 4;
 constexpr int kWhole = 1 << 30;  // a span no sequence is longer than
 
 // A tile of rows: its sequence, first row and the sequence's rows; the span's
@@ -92,9 +94,10 @@ template <int BM> struct Lanes {
   }
 };
 
-// The shortest span, in steps of `round` rows, with which all units fit `splits`;
-// kWhole where the tiles alone do not.
-template <int BM> __device__ __forceinline__ int find_span(const AttnArgs &a, const Lanes<BM> &lanes, int round) {
+// The shortest span, in steps of `round` rows and of at least `least` of them, with
+// which all units fit `splits`; kWhole where the tiles alone do not.
+template <int BM>
+__device__ __forceinline__ int find_span(const AttnArgs &a, const Lanes<BM> &lanes, int round, int least) {
   if (!a.splits) return kWhole;
   int tiles = 0, longest = 0;
   float work = 0.0f;  // cached rows over all tiles, in steps of `round`
@@ -107,7 +110,7 @@ template <int BM> __device__ __forceinline__ int find_span(const AttnArgs &a, co
   });
   if (tiles >= a.splits) return kWhole;
   // between work / splits, and work / (splits - tiles): there they fit for sure
-  int lo = max((int)(work / (float)a.splits), 1), hi = max(min((int)(work / (float)(a.splits - tiles)) + 2, longest), lo);
+  int lo = max((int)(work / (float)a.splits), least), hi = max(min((int)(work / (float)(a.splits - tiles)) + 2, longest), lo);
   while (lo < hi) {
     const int mid = (lo + hi) >> 1;
     int units = 0;
@@ -436,7 +439,7 @@ template <int BM> struct Share {
   bool live;
   const unsigned char *k, *v; // of the kv head
 
-  __device__ __forceinline__ bool find(const AttnArgs &a, int block, int round, int wave_row) {
+  __device__ __forceinline__ bool find(const AttnArgs &a, int block, int round, int least, int wave_row) {
     kvh = block % a.hkv;
     int span = kWhole;
     if (BM <= 32 && a.single) {
@@ -449,7 +452,7 @@ template <int BM> struct Share {
       if (t.rows == 0) return false;
     } else {
       const Lanes<BM> lanes(a);
-      span = find_span<BM>(a, lanes, round);
+      span = find_span<BM>(a, lanes, round, least);
       if (a.splits && block == 0 && threadIdx.x == 0) *a.span = span;
       if (!locate<BM, true>(a, lanes, span, block / a.hkv, t)) return false;
     }
@@ -566,7 +569,7 @@ __global__ __launch_bounds__(NW * kWave, sizeof(T) == 2 ? 2 : 1) void attn_many(
   __shared__ __align__(16) unsigned char k0[kBuf], v0[kBuf], k1[kBuf], v1[kBuf];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   Share<BM> w;
-  if (!w.find(a, blockIdx.x, kManyRound, wave * 32)) return;
+  if (!w.find(a, blockIdx.x, kManyRound, kManyLeast, wave * 32)) return;
   const int w0 = w.t.row0 + wave * 32;
   const bool idle = w0 >= w.t.rows;
   const int highest = w.t.s.len - w.t.s.n_new + min(w0 + 31, w.t.rows - 1) / a.g;  // of the wave's rows
@@ -652,7 +655,7 @@ template <int D> __global__ __launch_bounds__(kFewWaves * kWave, 2) void attn_fe
   const int lane = threadIdx.x & (kWave - 1);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   Share<32> w;
-  if (!w.find(a, blockIdx.x, NW * 32, 0)) return;
+  if (!w.find(a, blockIdx.x, NW * 32, 1, 0)) return;
   unsigned char *sk = k0 + wave * kTile, *sv = v0 + wave * kTile;
   constexpr int step = NW * BN;
   int row = w.begin + wave * BN;
@@ -752,7 +755,7 @@ template <int D> __global__ __launch_bounds__(kFewWaves * kWave, 2) void attn_fe
   const int lane = threadIdx.x & (kWave - 1), quarter = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   Share<16> w;
-  if (!w.find(a, blockIdx.x, NW * BN, 0)) return;
+  if (!w.find(a, blockIdx.x, NW * BN, 1, 0)) return;
   unsigned char *sk = k0 + wave * kTile, *sv = v0 + wave * kTile;
   constexpr int step = NW * BN;
   int row = w.begin + wave * BN;
@@ -992,7 +995,7 @@ AttnPlan plan_chunk_attn(const smallkv_chunk_t &c, const smallkv_cache_t &kv, co
   // of chunks and tokens of 64 elements: 49 us with 512, 46 with 768, 46 with 1024;
   // a batch-64 decode step of 128 elements: 79 with 256, 70 with 512, 71 with 1024.)
   const int slots = std::max((kv.head_dim == 64 && !f32 ? 768 : 512) / kv.n_heads, 1);
-  const int round = p.few ? few * kFewWaves : kManyRound;
+  const int round = p.few ? few * kFewWaves : kManyRound * kManyLeast;
   if (p.tiles < slots && c.max_len > round)
     p.splits = (int)std::min<int64_t>(slots, (int64_t)p.tiles * ceil_div(c.max_len, round));
   p.units = std::max(p.tiles, p.splits);
