@@ -472,8 +472,9 @@ int smallkv_match(const smallkv_match_t *match, void *ws, size_t ws_bytes, void 
  * smallkv_evict's outputs are the small model's k, v, held and row_pos.
  * SMALLKV_EUNSUPPORTED for what one launch cannot count: batch * n_heads from 2^24
  * (smallkv_evict: 2^22), 2^24 tokens to append, 2^24 tiles of 16 or more (token, query
- * head) rows or, for smallkv_chunk_scores, 2^24 blocks of 128 of max_len's rows, over
- * all sequences and kv heads. */
+ * head) rows over all sequences and kv heads, or, for smallkv_chunk_scores of more than
+ * 32 of them in a sequence, 2^24 blocks of 128 of max_len's rows over all sequences and
+ * score heads. */
 
 /* The keys and values of every sequence: row r of sequence b and kv head h is
  * at k + page * page_stride + h * head_stride + (r % page_rows) * row_stride

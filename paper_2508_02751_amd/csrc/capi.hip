@@ -635,8 +635,9 @@ int smallkv_chunk_scores(const smallkv_chunk_t *chunk, const smallkv_cache_t *ca
   if ((!queries->lse && chunk->n_tokens > 0) || !out || score_rows < chunk->max_len) return SMALLKV_EINVAL;
   if (n_score_heads != queries->n_heads && n_score_heads != cache->n_heads) return SMALLKV_EINVAL;
   if (score_rows > INT32_MAX || seq_stride < n_score_heads * score_rows) return SMALLKV_EINVAL;
-  if (((int64_t)chunk->max_len + 127) / 128 * chunk->batch * cache->n_heads > kMaxGroups ||
-      queries->n_heads / cache->n_heads > 65535)
+  // (a decode step's keys are cut into as many pieces as run at once)
+  if ((int64_t)chunk->max_new * (queries->n_heads / cache->n_heads) > 32 &&
+      ((int64_t)chunk->max_len + 127) / 128 * chunk->batch * n_score_heads > kMaxGroups)
     return SMALLKV_EUNSUPPORTED;
   return status_of(launch_chunk_scores(*chunk, *cache, *queries, n_score_heads, before, out, score_rows,
                                        seq_stride, static_cast<hipStream_t>(stream)));
