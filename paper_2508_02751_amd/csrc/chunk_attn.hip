@@ -33,7 +33,7 @@
 //     the same loops take 3.8 ms: the matrix cores at the clock that power leaves.
 //     Heads of 64: 750 TFLOP/s, half as many products per exponential.
 //   a token each of 64 sequences of 1024 - 4096 rows, 28 and 4 heads of 128: 63 us for
-//     336 MB of keys and values, 5.3 TB/s (+ 5 us to find nothing to join): memory.
+//     336 MB of keys and values, 5.3 TB/s, + 5 us to join two spans each: memory.
 //   one token over 32768 rows of 4 kv heads: 17 + 8 us, 67 MB: latency and two launches.
 //   a 4096-token prompt in fp32, 32 and 8 heads of 128: 1.31 ms, 105 TFLOP/s of 153; the
 //     matrix cores are busy 75% of the time.
