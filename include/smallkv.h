@@ -515,7 +515,7 @@ typedef struct {
  * dtype and head_dim; head h reads kv head h / (n_heads / cache n_heads). */
 typedef struct {
   int32_t n_heads;
-  float scale;       /* softmax scale, > 0 */
+  float scale;       /* softmax scale, > 0, at most 1e38 */
   const void *q;
   int64_t token_stride, head_stride;
   void *out;         /* smallkv_chunk_attn: the output, laid out by its own strides */

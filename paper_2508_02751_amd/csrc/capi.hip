@@ -234,7 +234,7 @@ int check_queries(const smallkv_chunk_t *c, const smallkv_cache_t *kv, const sma
   const int rc = check_chunk(c, kv);
   if (rc) return rc;
   if (!q || (!q->q && c->n_tokens > 0) || q->n_heads < 1 || q->n_heads % kv->n_heads) return SMALLKV_EINVAL;
-  if (!(q->scale > 0.0f) || !(q->scale <= 3.402823e38f)) return SMALLKV_EINVAL;
+  if (!(q->scale > 0.0f) || !(q->scale <= 1e38f)) return SMALLKV_EINVAL;  // (times log2 e: finite)
   if (!aligned16(q->q) || !stride_ok(q->token_stride, kv->dtype) || !stride_ok(q->head_stride, kv->dtype))
     return SMALLKV_EINVAL;
   const int64_t bytes = kv->dtype == SMALLKV_F32 ? 4 : 2;

@@ -115,6 +115,11 @@ def test_bad_queries(over, status):
     assert try_attn(chunk(), cache(), queries(**over)) == status
 
 
+def test_a_scale_stays_finite_in_log2_units():
+    assert try_attn(chunk(), cache(), queries(scale=3e38)) == S.EINVAL
+    assert try_attn(chunk(), cache(), queries(scale=1e37)) == S.OK
+
+
 def test_a_dense_cache_has_a_page_per_sequence():
     assert try_attn(chunk(), dense(), queries()) == S.OK
     assert try_attn(chunk(), dense(n_pages=1), queries()) == S.EINVAL

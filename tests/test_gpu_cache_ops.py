@@ -57,6 +57,8 @@ CASES = [
     ("few rows in tiles f32", [(300, 9), (41, 2), (9, 9), (17, 3)], 14, 2, 64, F32, 16, True),
     ("few rows in tiles over spans f32", [(5000, 8), (70, 1), (1100, 5)], 16, 2, 128, F32, 64, False),
     ("one token over many spans", [(20001, 1)], 14, 2, 128, BF16, 0, False),
+    ("a hundred query heads", [(300, 5), (70, 1)], 100, 1, 64, BF16, 16, False),
+    ("a hundred query heads f32", [(90, 2), (33, 1)], 200, 2, 64, F32, 0, False),
     ("tokens and a chunk over many spans", [(16000, 1), (3, 1), (12000, 37)], 14, 2, 64, BF16, 32, False),
 ]
 IDS = [c[0].replace(" ", "-") for c in CASES]
@@ -364,6 +366,57 @@ def test_another_stream_and_a_graph():
             assert torch.equal(got[0], eager[0]) and torch.equal(got[1], eager[1])
 
 
+@pytest.mark.parametrize("new,dtype", [(1, BF16), (40, BF16), (5, F32)])
+def test_lengths_out_of_range_are_clamped(new, dtype):
+    """Starts past the tokens, negative lengths and ones past the cache or the hints, more
+    new tokens than max_new: as the clamped values, nothing else written."""
+    S = lib()
+    cap, hq, hk, d = 96, 8, 2, 64
+    lens = [(cap, new), (0, new), (80, new), (50, 0)]
+    c = R.Case(lens, hq, hk, d, dtype, 16, seed=59, cap=cap, extra_tokens=2)
+    chunk, cache, q = c.to(DEV)
+    start = torch.tensor([-7, *c.starts[1:3], c.starts[3], c.T + 900], dtype=torch.int32, device=DEV)
+    length = torch.tensor([10 ** 9, -10 ** 9, 80, 50], dtype=torch.int32, device=DEV)
+    # the last sequence claims two tokens: the clamped one has them
+    c.lens[3] = (50, 2 if new > 1 else 1)
+    tail = c.T - c.starts[3]
+    c.starts[4:] = [c.starts[3] + tail]
+    T = c.T
+    wild = S.ChunkSpec(start, length, T, max(new, c.lens[3][1]), cap + 1000)
+    if new == 1:  # two claimed, one allowed: the second token is in no sequence
+        c.starts[4] = c.starts[3] + 1
+    log(f"[clamp] {new} {dtype}")
+    k0 = cache.k.clone()
+    qo = torch.full_like(q, 7.0)
+    kv = torch.randn(T, 2 * hk, d, generator=c.gen).to(DEV, dtype)
+    freq, amp = S.rope_freqs(d, 10000.0)
+    pos = torch.full((c.B, hk, 10), -1, dtype=torch.int32, device=DEV)
+    S.prepare_append(wild, cache, S.RopeSpec(freq, S.ROPE_HALF, amp), q, kv[:, :hk], kv[:, hk:], q_out=qo,
+                     row_pos=pos).run()
+    torch.cuda.synchronize()
+    end = c.starts[4]
+    assert bool((qo[end:] == 7).all()) and not bool((qo[:end] == 7).all(-1).any())
+    bits = torch.int16 if dtype == BF16 else torch.int32
+    changed = (cache.k.view(bits) != k0.view(bits)).any(-1).any(1).nonzero().tolist()
+    rows = [list(c.slot(b, r)) for b, (n, m) in enumerate(c.lens) for r in range(max(n - m, 0), n)]
+    assert sorted(changed) == sorted(rows)
+    c.k, c.v, c.q = cache.k.cpu(), cache.v.cpu(), qo.cpu()
+    out = torch.full_like(q, 7.0)
+    lse = torch.full((T, hq), 7.0, device=DEV)
+    S.prepare_chunk_attn(wild, cache, qo, c.scale, out=out, lse=lse).run()
+    sc = torch.full((c.B, hk, cap + 1000), 7.0, device=DEV)
+    S.prepare_chunk_scores(wild, cache, qo, lse, c.scale, sc).run()
+    torch.cuda.synchronize()
+    want, wl, tol, ltol = R.attention(c)
+    within(out[:end], want[:end], tol[:end], "out")
+    within(lse[:end], wl[:end], ltol[:end], "lse")
+    assert bool((out[end:] == 7).all()) and bool((lse[end:] == 7).all())
+    ws, wt = R.scores(c, lse.cpu(), torch.zeros(c.B, hk, cap), True)
+    for b, (n, _) in enumerate(c.lens):
+        within(sc[b, :, :n], ws[b, :, :n], wt[b, :, :n], f"scores {b}")
+        assert bool((sc[b, :, n:] == 7).all())
+
+
 @pytest.mark.parametrize("lens", [[(130, 40), (77, 9)], [(700, 1), (64, 1)]])
 def test_broadcast_queries_and_keys(lens):
     """One query row for all heads, one layer's rows for all sequences, no lse."""
@@ -649,6 +702,47 @@ def test_evict_ties_and_special_scores():
 
 def test_evict_caps_and_rows_as_positions():
     evict_case([900, 50], [600, 50], [10, 3], 4, 1, 2, 64, BF16, 32, 0, cap=77, row_pos=False)
+
+
+def test_evict_in_a_graph():
+    """Captured, replayed with other scores, lengths and budgets, out-of-range ones too."""
+    S = lib()
+    c = R.Case([(700, 0), (300, 0)], 2, 2, 64, BF16, 32, seed=61)
+    chunk, cache, _ = c.to(DEV)
+    k, v = (torch.zeros(2, 2, 100, 64, dtype=BF16, device=DEV) for _ in range(2))
+    length, keep, recent = (torch.zeros(2, dtype=torch.int32, device=DEV) for _ in range(3))
+    scores = torch.zeros(2, 4, 700, device=DEV)
+    outs = torch.zeros(2, 4, 100, device=DEV)
+    call = S.prepare_evict(cache, S.CacheSpec(k, v), length, keep, scores, recent=recent, sinks=2,
+                           out_scores=outs)
+    log("[evict] graph")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call.run()
+    everything = (k, v, outs, call.out_pos, call.held)
+    for lens, kept, rec in (((700, 300), (90, 20), (5, 0)), ((650, 0), (100, 7), (0, 3)),
+                            ((10 ** 9, -4), (10 ** 9, 5), (-3, 10 ** 9)), ((1, 300), (50, -9), (9, 9))):
+        for t, x in ((length, lens), (keep, kept), (recent, rec)):
+            t.copy_(torch.tensor(x, dtype=torch.int32))
+        scores.copy_(torch.rand(scores.shape, generator=c.gen))
+        for t in everything:
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in everything]
+        for t in everything:
+            t.zero_()
+        call.run()
+        torch.cuda.synchronize()
+        for x, y in zip(got, everything):
+            assert torch.equal(x, y)
+        for b in range(2):
+            n = min(max(lens[b], 0), 700)
+            for h in range(2):
+                f = scores[b, 2 * h, :n].cpu() + scores[b, 2 * h + 1, :n].cpu()
+                rows = R.kept_rows(f.tolist(), n, kept[b], rec[b], 2, 100)
+                assert call.held[b] == len(rows)
+                assert call.out_pos[b, h, :len(rows)].tolist() == rows
 
 
 def test_evict_long():
