@@ -2,7 +2,7 @@
 // running score: out[r] = before[r] + sum over (token, head) of exp(s - lse).
 //
 // No sum leaves its workgroup: no atomics, one order, and the logits are never
-// stored.  Two forms:
+// stored.  Three forms:
 //   chunk   -- a workgroup owns keys of one kv head (32 per wave, their K rows in
 //              registers as the left operand of S^T = K Q^T) and walks the
 //              query rows that see them, 64 at a time through LDS.  A lane holds one
@@ -13,6 +13,8 @@
 //              per kv head: the rows are (token, head) pairs.  Where that makes too few
 //              workgroups (SPLIT), one owns 32 keys, its waves deal the rows among
 //              themselves without a barrier, and their sums are added at the end.
+//   heads   -- per query head, up to 128 tokens in a sequence: the same with several heads
+//              to a workgroup, which reads its keys once for them all.
 //   few     -- no sequence has more than 32 (token, head) rows (a decode step): the
 //              rows stay in registers as the left operand of S = Q K^T, a lane holds
 //              one key's logits, and each wave streams its keys' rows, bound by
@@ -24,6 +26,7 @@
 // sequences of 1024 - 4096 rows of 4 kv heads of 128 (168 MB) 41 us, 4.1 TB/s; of 16
 // sequences over 82552 rows of 2 kv heads of 64 (23 MB) 9.1 us: latency.
 #include <algorithm>
+#include <type_traits>
 
 #include "cache.h"
 #include "launch.h"
@@ -45,10 +48,30 @@ struct ScoreArgs {
   int64_t rows, seq_stride;  // of before and out, in elements
   float scale2;   // scale * log2(e)
   int span;       // few: keys per workgroup, a multiple of 128
+  int walk;       // heads: tiles of query rows (of one token range) per workgroup
 };
 
 constexpr float kLog2e = 1.4426950408889634074f;
 constexpr int kNW = 4;
+
+// Sums over ROWS (16 or 32) neighbouring lanes' query rows: each exchange halves the keys
+// that a lane holds.  The lane ends with key register (lane % ROWS) * 16 / ROWS.
+template <int ROWS> __device__ __forceinline__ float sum_rows(float (&acc)[16]) {
+  const int lane = threadIdx.x & (kWave - 1);
+  auto fold = [&](auto n, int o) {
+    const bool up = lane & o;
+#pragma unroll
+    for (int i = 0; i < n; ++i) {
+      const float send = up ? acc[i] : acc[i + n], keep = up ? acc[i + n] : acc[i];
+      acc[i] = keep + __shfl_xor(send, o, kWave);
+    }
+  };
+  fold(std::integral_constant<int, 8>(), ROWS / 2);
+  fold(std::integral_constant<int, 4>(), ROWS / 4);
+  fold(std::integral_constant<int, 2>(), ROWS / 8);
+  fold(std::integral_constant<int, 1>(), ROWS / 16);
+  return ROWS == 32 ? acc[0] + __shfl_xor(acc[0], 1, kWave) : acc[0];
+}
 
 template <typename T, int D, bool PER_KV, bool SPLIT>
 __global__ __launch_bounds__(kNW * kWave, SPLIT && sizeof(T) * D == 512 ? 1 : 2) void chunk_scores(ScoreArgs a) {
@@ -183,18 +206,7 @@ __global__ __launch_bounds__(kNW * kWave, SPLIT && sizeof(T) * D == 512 ? 1 : 2)
     if (r0 >= n_rows) break;
     turn(q1, q0);
   }
-  // sums over the 32 query rows: each exchange halves the keys a lane holds
-#pragma unroll
-  for (int n = 8, o = 16; n >= 1; n >>= 1, o >>= 1) {
-    const bool up = lane & o;
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (i < n) {
-        const float send = up ? acc[i] : acc[i + n], keep = up ? acc[i + n] : acc[i];
-        acc[i] = keep + __shfl_xor(send, o, kWave);
-      }
-  }
-  float sum = acc[0] + __shfl_xor(acc[0], 1, kWave);
+  float sum = sum_rows<32>(acc);
   if (SPLIT) {
     float *part = reinterpret_cast<float *>(q0);
     wait_memory();
@@ -212,6 +224,155 @@ __global__ __launch_bounds__(kNW * kWave, SPLIT && sizeof(T) * D == 512 ? 1 : 2)
     const float old = a.before && key < pos0 ? a.before[at] : 0.0f;
     a.out[at] = old + (exists >> in & 1u ? sum : 0.0f);
   }
+}
+
+// Per query head.  A tile of 64 query rows is 64 tokens of a head, or, where no sequence
+// has more than P < 64, the tokens of 64 / P heads; a workgroup keeps its keys for up to
+// kWalk heads (or such groups of heads), whose sums wait in LDS for the end (a store
+// between tiles would be waited for with the next tile's copies).
+constexpr int kWalk = 4;
+
+template <typename T, int D, int P>
+__global__ __launch_bounds__(kNW * kWave, 2) void head_scores(ScoreArgs a) {
+  using L = TileLayout<T, D>;
+  constexpr bool kBf16 = sizeof(T) == 2;
+  constexpr int kFrag = kBf16 ? D / 16 : D / 8;  // 16-byte pieces of a row per lane
+  constexpr int kHeads = 64 / P, kShare = 64 / kNW, kRpi = 64 / L::C, kInstr = kShare / kRpi;
+  constexpr int kSums = P < 64 ? 2 : 1;  // of a lane per tile
+  __shared__ __align__(16) unsigned char q0[64 * L::bytes], q1[64 * L::bytes];
+  __shared__ float sums[kWalk * kSums][kNW * kWave];  // the lanes' own
+  const int lane = threadIdx.x & (kWave - 1), half = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int per = (a.g + a.walk * kHeads - 1) / (a.walk * kHeads);  // workgroups that share a kv head
+  const int units = a.c.batch * a.hkv * per, unit = blockIdx.x % units;
+  const int b = unit / (a.hkv * per), kvh = unit / per % a.hkv;
+  const Seq s = sequence(a.c, b, a.kv.cap);
+  const int block0 = (blockIdx.x / units) * 32 * kNW, key0 = block0 + wave * 32;
+  if (block0 >= s.len) return;
+  const int pos0 = s.len - s.n_new;
+  const int in_group = unit % per * a.walk * kHeads, n_heads = min(a.walk * kHeads, a.g - in_group);
+  const int head0 = kvh * a.g + in_group;
+  const int first = max(0, block0 - pos0);  // the first token that sees a key of the workgroup
+  const int n_tokens = s.n_new - first;
+
+  uint4 kf[kFrag];
+  uint32_t exists;
+  {
+    const int key = key0 + (lane & 31);
+    const int64_t off = key < s.len ? row_offset(a.kv, b, key) : -1;
+    const unsigned char *row = off >= 0 ? a.kv.k + off + (((uint64_t)kvh * a.kv.head_stride) << 4) : zero_row;
+#pragma unroll
+    for (int i = 0; i < kFrag; ++i)
+      kf[i] = reinterpret_cast<const uint4 *>(row)[kBf16 ? 2 * i + half : half * kFrag + i];
+    exists = (uint32_t)__ballot(off >= 0);
+  }
+  // Row r of tile t of head group h: token 64 t + r % P of head h * kHeads + r / P; past
+  // the last, one that exists.
+  const int groups = (n_heads + kHeads - 1) / kHeads, tiles = P < 64 ? 1 : (n_tokens + 63) / 64;
+  auto head_of = [&](int h, int r) { return min(h * kHeads + r / P, n_heads - 1); };
+  auto token_of = [&](int t, int r) { return min(64 * t + (r & (P - 1)), n_tokens - 1); };
+  auto issue = [&](int h, int t, unsigned char *dst) {
+    const int rr = lane / L::C, p = lane & (L::C - 1);
+#pragma unroll
+    for (int j = 0; j < kInstr; ++j) {
+      const int r = wave * kShare + j * kRpi + rr;
+      const unsigned char *row = a.q + (int64_t)(s.first + first + token_of(t, r)) * a.q_token +
+                                 (int64_t)(head0 + head_of(h, r)) * a.q_head;
+      load_to_lds16(row + ((p ^ L::swz_k(r)) << 4), dst + (wave * kShare + j * kRpi) * L::bytes);
+    }
+  };
+  if (n_tokens > 0) {
+    float lse = 0.0f;
+    auto lookup = [&](int h, int t) {
+      lse = a.lse[(int64_t)(s.first + first + token_of(t, lane)) * a.hq + head0 + head_of(h, lane)];
+    };
+    float acc[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) acc[i] = 0.0f;
+    int h = 0, t = 0;  // the tile that is computed
+    auto turn = [&](unsigned char *sq, unsigned char *nq) {
+      wait_memory();
+      __syncthreads();
+      // own: the row's cached row; -1, which gives no weight: past the last, or sees no key
+      const int token = 64 * t + (lane & (P - 1));
+      const bool dead = token >= n_tokens || lse == -INFINITY;
+      const int own = dead ? -1 : pos0 + first + token;
+      const float lse2 = dead ? 0.0f : lse * kLog2e;
+      const bool last = t + 1 == tiles;
+      const int h_next = last ? h + 1 : h, t_next = last ? 0 : t + 1;
+      if (h_next < groups) {
+        issue(h_next, t_next, nq);
+        lookup(h_next, t_next);
+      }
+      // the weights of 32 query rows, added to acc
+      auto weigh = [&](int blk) {
+        const int row = 32 * blk + (lane & 31), z = L::swz_k(row);
+        const int o = __shfl(own, row, kWave);
+        const float base = __shfl(lse2, row, kWave);
+        f32x16_t x = {};
+#pragma unroll
+        for (int i = 0; i < kFrag; ++i) {
+          const int c = kBf16 ? 2 * i + half : half * kFrag + i;
+          const uint4 w = *reinterpret_cast<const uint4 *>(sq + (row * L::bytes + ((c ^ z) << 4)));
+          if constexpr (kBf16) {
+            x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, kf[i]),
+                                                        __builtin_bit_cast(bf16x8_t, w), x, 0, 0, 0);
+          } else {
+            const f32x4_t ka = __builtin_bit_cast(f32x4_t, kf[i]), qa = __builtin_bit_cast(f32x4_t, w);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x = __builtin_amdgcn_mfma_f32_32x32x2f32(ka[e], qa[e], x, 0, 0, 0);
+          }
+        }
+        if (__any(o < key0 + 31)) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int key = key0 + 8 * (i / 4) + i % 4 + 4 * half;
+            const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], a.scale2, -base));
+            acc[i] += key <= o ? p : 0.0f;
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) acc[i] += __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], a.scale2, -base));
+        }
+      };
+      weigh(0);
+      if constexpr (P < 64) {
+        sums[2 * h][threadIdx.x] = sum_rows<P>(acc);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[i] = 0.0f;
+      }
+      weigh(1);
+      if (last) {
+        sums[P < 64 ? 2 * h + 1 : h][threadIdx.x] = sum_rows<P == 16 ? 16 : 32>(acc);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[i] = 0.0f;
+      }
+      h = h_next;
+      t = t_next;
+    };
+    issue(0, 0, q0);
+    lookup(0, 0);
+    while (true) {
+      turn(q0, q1);
+      if (h >= groups) break;
+      turn(q1, q0);
+      if (h >= groups) break;
+    }
+  }
+  const int k = P == 16 ? lane & 15 : (lane & 31) >> 1, in = 8 * (k / 4) + k % 4 + 4 * half, key = key0 + in;
+  const bool writes = (P == 16 || !(lane & 1)) && key < s.len;
+  // all old scores, then all new ones (which may be the same memory)
+  float old[kWalk * kSums];
+  // the head of a tile's sum of this lane
+  auto head = [&](int n) { return n / kSums * kHeads + (P == 64 ? 0 : P == 32 ? n % 2 : n % 2 * 2 + (lane >> 4 & 1)); };
+  auto at = [&](int n) { return b * a.seq_stride + (head0 + head(n)) * a.rows + key; };
+#pragma unroll
+  for (int n = 0; n < kWalk * kSums; ++n)
+    old[n] = writes && head(n) < n_heads && a.before && key < pos0 ? a.before[at(n)] : 0.0f;
+#pragma unroll
+  for (int n = 0; n < kWalk * kSums; ++n)
+    if (writes && head(n) < n_heads)
+      a.out[at(n)] = old[n] + (n_tokens > 0 && exists >> in & 1u ? sums[n][threadIdx.x] : 0.0f);
 }
 
 template <typename T, int D>
@@ -348,6 +509,20 @@ void launch_typed(ScoreArgs a, int max_new, int max_len, hipStream_t st) {
     return;
   }
   const unsigned heads = a.per_kv ? 1 : a.g;
+  if (!a.per_kv && max_new <= 128) {
+    // (8 sequences of 8192 rows, 32 query heads: 9 tokens 35 us, 120 as a chunk; 64 tokens
+    // 73, 119; 128 tokens 114, 155; with 226 tokens and more no faster, 2048 214 against
+    // 203.)  More heads to a workgroup while four workgroups per CU are left (30 sequences
+    // of 600 rows and 64 heads, 12 tokens: 19 us, 24 with a tile each).
+    const int packed = max_new <= 16 ? 4 : max_new <= 32 ? 2 : 1, tiles = ((int)heads + packed - 1) / packed;
+    const int64_t pieces = blocks(32 * kNW);
+    a.walk = std::min(tiles, kWalk);
+    while (a.walk > 1 && pieces * ((tiles + a.walk - 1) / a.walk) < 1024) --a.walk;
+    const dim3 grid((unsigned)(pieces * ((tiles + a.walk - 1) / a.walk)));
+    auto *kernel = packed == 4 ? head_scores<T, D, 16> : packed == 2 ? head_scores<T, D, 32> : head_scores<T, D, 64>;
+    hipLaunchKernelGGL(kernel, grid, block, 0, st, a);
+    return;
+  }
   // with less than a workgroup per CU (2048 tokens over 8192 rows, two kv heads, 128
   // workgroups: 175 us, split 84; 512 tokens, four, 256 workgroups: 68, split 72)
   const bool split = blocks(32 * kNW) * (int64_t)heads < 256;

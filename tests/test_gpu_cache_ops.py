@@ -141,6 +141,29 @@ def test_chunk_scores_with_many_workgroups(dtype, d, per_kv):
         assert bool((out[b, :, n:] == 7).all())
 
 
+@pytest.mark.parametrize("new,hq,hk,batch", [(9, 14, 2, 2), (16, 8, 2, 40), (17, 14, 2, 40), (32, 5, 1, 30),
+                                             (33, 14, 2, 40), (64, 3, 3, 4), (65, 9, 1, 30), (128, 14, 2, 20)])
+@pytest.mark.parametrize("dtype,d", [(BF16, 128), (BF16, 64), (F32, 128), (F32, 64)])
+def test_chunk_scores_of_several_heads_a_workgroup(dtype, d, new, hq, hk, batch):
+    """Tokens around the sizes at which heads share a tile; groups that do not fill it;
+    many workgroups and few; sequences with fewer tokens, none, and fewer rows than tokens."""
+    S = lib()
+    some = [(400, new), (new, new), (131, 1), (260, new // 2), (150, 0), (max(new - 3, 0), new)]
+    c = R.Case((some * batch)[:batch], hq, hk, d, dtype, 32, seed=67)
+    chunk, cache, q = c.to(DEV)
+    _, wl, _, _ = R.attention(c)
+    lse = wl.float()
+    before = torch.rand(c.B, hq, c.rows, generator=c.gen)
+    out = before.to(DEV)
+    log(f"[scores] heads {dtype} {d} {new} {hq}/{hk} {batch}")
+    S.prepare_chunk_scores(chunk, cache, q, lse.to(DEV), c.scale, out, before=out).run()
+    torch.cuda.synchronize()
+    want, tol = R.scores(c, lse, before, False)
+    for b, (n, _) in enumerate(c.lens):
+        within(out[b, :, :n], want[b, :, :n], tol[b, :, :n], f"sequence {b}")
+        assert torch.equal(out[b, :, n:].cpu(), before[b, :, n:])
+
+
 def test_scores_add_up_to_the_query_rows():
     """Each query row's weights sum to 1: attention's lse and the scores agree."""
     S = lib()
