@@ -11,9 +11,17 @@
 // registers, so the softmax needs one exchange between half-waves, and P^T is
 // already laid out as the right operand of O^T = V^T P^T up to the order of
 // the keys, which the reads of V follow.  Logits, statistics and the output
-// accumulate in fp32; P is rounded to bf16 for the second product of a bf16
-// model (its relative error, at most 2^-8, is averaged over the row's keys and stays
-// below that of the output's own rounding); fp32 models multiply in fp32.
+// accumulate in fp32; fp32 models multiply in fp32.  A bf16 model's P for the second
+// product:
+//   few rows  -- in two bf16 parts, a product each, 2^-16 relative: the rows of K and V
+//                bound the pass, not the products (a token each of 64 sequences 64.4 us
+//                with two parts, 64.5 with one);
+//   many rows -- in one, each weight off by up to 2^-8 of itself, as much as the output's
+//                own rounding: the products bound the pass (4096 tokens over 32768
+//                rows 4.60 ms; with two parts 5.82).  The sum of the rounded P divides the
+//                output, so that the weights add up to 1 and a row's error is at most
+//                2^-8 sum w |v - out|: none where one row has all the weight or where values
+//                agree.  (With the sum of the unrounded P, which the lse takes: 4.47 ms.)
 //
 // Two forms:
 //   many rows -- NW waves of 32 rows each share every tile of rows in LDS;
@@ -28,10 +36,11 @@
 // all sequences still run at once: spans of equal length whatever the mixture.
 //
 // Measured (MI355X), and what bounds it:
-//   2 x 4096 tokens over 32768 rows, 32 query and 8 kv heads of 128, bf16: 4.2 - 4.4 ms,
-//     960 TFLOP/s (a bf16 product of 8192^3 by the library: 1218).  Without any softmax
+//   2 x 4096 tokens over 32768 rows, 32 query and 8 kv heads of 128, bf16: 4.5 - 4.6 ms,
+//     900 TFLOP/s (a bf16 product of 8192^3 by the library: 1218).  Without any softmax
 //     the same loops take 3.8 ms: the matrix cores at the clock that power leaves.
-//     Heads of 64: 750 TFLOP/s, half as many products per exponential.
+//     Heads of 64 (4 x 4096 tokens over 16384 rows, 14 heads): 1.24 ms, 680 TFLOP/s, half as
+//     many products per exponential.
 //   a token each of 64 sequences of 1024 - 4096 rows, 28 and 4 heads of 128: 63 us for
 //     336 MB of keys and values, 5.3 TB/s, + 5 us to join two spans each: memory.
 //   one token over 32768 rows of 4 kv heads: 17 + 8 us, 67 MB: latency and two launches.
@@ -283,21 +292,44 @@ __device__ __forceinline__ f32x16_t logits32(const unsigned char *sk, int key0, 
 // Key of register i of a 32-key block, before the half-wave's 4 * half.
 __device__ __forceinline__ constexpr int reg_key(int i) { return 8 * (i / 4) + i % 4; }
 
-// O^T += V^T P^T over 32 keys.
-template <typename T, int D>
-__device__ __forceinline__ void values32(const unsigned char *sv, int key0, const f32x16_t &p,
-                                         f32x16_t (&o)[D / 32]) {
+template <typename T, int D> struct State {
+  float m, l;  // running maximum (log2 units), this half-wave's part of the sum
+  float r;     // and of the sum of P as it was rounded (many rows, bf16)
+  f32x16_t o[D / 32];
+  __device__ __forceinline__ void clear() {
+    m = -INFINITY;
+    l = r = 0.0f;
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d) o[d] = f32x16_t{};
+  }
+};
+
+// O^T += V^T P^T over 32 keys.  TWO: a bf16 model's P in two parts, a product each;
+// without, one rounded part, whose sum is kept too.
+template <typename T, int D, bool TWO>
+__device__ __forceinline__ void values32(const unsigned char *sv, int key0, const f32x16_t &p, State<T, D> &st) {
   using L = TileLayout<T, D>;
   const int lane = threadIdx.x & (kWave - 1), half = lane >> 5;
   if constexpr (sizeof(T) == 2) {
+    const bf16x2_t ones = {(__bf16)1.0f, (__bf16)1.0f};
+    float sum = 0.0f;
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
-      bf16x8_t pf;
+      bf16x8_t pf, lo;
 #pragma unroll
       for (int e = 0; e < 8; e += 2) {
-        const bf16x2_t w = __builtin_convertvector((f32x2_t{p[8 * s + e], p[8 * s + e + 1]}), bf16x2_t);
+        const f32x2_t x = {p[8 * s + e], p[8 * s + e + 1]};
+        const bf16x2_t w = __builtin_convertvector(x, bf16x2_t);
         pf[e] = w[0];
         pf[e + 1] = w[1];
+        if constexpr (TWO) {
+          const uint32_t u = __builtin_bit_cast(uint32_t, w);
+          const bf16x2_t y = __builtin_convertvector((f32x2_t{x[0] - bf16_lo(u), x[1] - bf16_hi(u)}), bf16x2_t);
+          lo[e] = y[0];
+          lo[e + 1] = y[1];
+        } else {
+          sum = __builtin_amdgcn_fdot2_f32_bf16(w, ones, sum, false);
+        }
       }
       // the transposing read: 16 lanes take 4 rows of 16 elements, lane i of
       // them ends with the 4 rows' element i
@@ -313,9 +345,11 @@ __device__ __forceinline__ void values32(const unsigned char *sv, int key0, cons
           const int at = r * L::bytes + ((c ^ L::swz_v(r)) << 4) + (lane & 1) * 8;
           vf.h[x] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((SMALLKV_LDS s16x4_t *)(sv + at));
         }
-        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf.v, pf, o[d], 0, 0, 0);
+        st.o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf.v, pf, st.o[d], 0, 0, 0);
+        if constexpr (TWO) st.o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf.v, lo, st.o[d], 0, 0, 0);
       }
     }
+    if (!TWO) st.r += sum;
   } else {
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
@@ -324,7 +358,7 @@ __device__ __forceinline__ void values32(const unsigned char *sv, int key0, cons
       for (int d = 0; d < D / 32; ++d) {
         const int c = d * 8 + ((lane & 31) >> 2);
         const float v = *reinterpret_cast<const float *>(sv + r * L::bytes + ((c ^ L::swz_v(r)) << 4) + (lane & 3) * 4);
-        o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, p[i], o[d], 0, 0, 0);
+        st.o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, p[i], st.o[d], 0, 0, 0);
       }
     }
   }
@@ -343,17 +377,6 @@ template <typename T> __device__ __forceinline__ bool drop_not_finite(uint4 &w) 
   return any;
 }
 
-template <typename T, int D> struct State {
-  float m, l;  // running maximum (log2 units), this half-wave's part of the sum
-  f32x16_t o[D / 32];
-  __device__ __forceinline__ void clear() {
-    m = -INFINITY;
-    l = 0.0f;
-#pragma unroll
-    for (int d = 0; d < D / 32; ++d) o[d] = f32x16_t{};
-  }
-};
-
 // The running maximum, sum and output of a tile's logits s.
 template <typename T, int D, int NB>
 __device__ __forceinline__ void softmax_step(State<T, D> &st, f32x16_t (&s)[NB], float c, float c_lo) {
@@ -370,6 +393,7 @@ __device__ __forceinline__ void softmax_step(State<T, D> &st, f32x16_t (&s)[NB],
     const float f = __builtin_amdgcn_exp2f(st.m - (m == -INFINITY ? 0.0f : m));
     st.m = m;
     st.l *= f;
+    st.r *= f;
 #pragma unroll
     for (int d = 0; d < D / 32; ++d)
 #pragma unroll
@@ -399,12 +423,12 @@ __device__ __forceinline__ void full_tile(State<T, D> &st, const QFrag<T, D> &q,
   for (int b = 0; b < BN / 32; ++b) s[b] = logits32<T, D>(sk, 32 * b, q);
   softmax_step<T, D>(st, s, c, c_lo);
 #pragma unroll
-  for (int b = 0; b < BN / 32; ++b) values32<T, D>(sv, 32 * b, s[b], st.o);
+  for (int b = 0; b < BN / 32; ++b) values32<T, D, false>(sv, 32 * b, s[b], st);
 }
 
 // Any other, 32 keys at a time.  own: the lane's own row; highest: of the wave's; valid:
 // bit t set iff key row0 + t exists.
-template <typename T, int D, int BN>
+template <typename T, int D, int BN, bool TWO>
 __device__ __forceinline__ void masked_tile(State<T, D> &st, const QFrag<T, D> &q, const unsigned char *sk,
                                             const unsigned char *sv, int row0, int own, int highest,
                                             uint64_t valid, float c, float c_lo) {
@@ -419,7 +443,7 @@ __device__ __forceinline__ void masked_tile(State<T, D> &st, const QFrag<T, D> &
       s[0][i] = ok ? s[0][i] : -INFINITY;
     }
     softmax_step<T, D>(st, s, c, c_lo);
-    values32<T, D>(sv, k0, s[0], st.o);
+    values32<T, D, TWO>(sv, k0, s[0], st);
   }
 }
 
@@ -523,13 +547,15 @@ __device__ __forceinline__ void write_row(const AttnArgs &a, const Share<BM> &w,
     a.lse[(int64_t)w.token * a.hq + w.head] = l == 0.0f ? -INFINITY : (m + __log2f(l)) * kLn2;
 }
 
-template <typename T, int D, int BM, int BN>
+template <typename T, int D, int BM, int BN, bool TWO>
 __device__ __forceinline__ void write_row(const AttnArgs &a, const Share<BM> &w, const State<T, D> &st, bool taken) {
-  const float l = swap_halves_sum(st.l);
+  // `rounded`: where one rounded P was multiplied its own sum divides the output, so
+  // that the weights add up to 1 (a record holds the output times l / rounded)
+  const float l = swap_halves_sum(st.l), rounded = sizeof(T) == 2 && !TWO ? swap_halves_sum(st.r) : l;
   const int half = (threadIdx.x & (kWave - 1)) >> 5;
   if (sizeof(T) == 2 && w.t.n_split == 1) {
     // half-waves exchange four elements of 16, so that each lane writes eight at once
-    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    const float inv = l == 0.0f ? 0.0f : 1.0f / rounded;
     unsigned char *o = a.out + (w.token * a.o_token + w.head * a.o_head) * 2;
 #pragma unroll
     for (int j = 0; j < D / 16; ++j) {
@@ -552,10 +578,11 @@ __device__ __forceinline__ void write_row(const AttnArgs &a, const Share<BM> &w,
     return;
   }
   if (!w.live) return;
+  const float f = sizeof(T) == 2 && !TWO && l != 0.0f ? l / rounded : 1.0f;
   f32x4_t x[D / 8];
 #pragma unroll
   for (int i = 0; i < D / 8; ++i)
-    x[i] = f32x4_t{st.o[i / 4][i % 4 * 4], st.o[i / 4][i % 4 * 4 + 1], st.o[i / 4][i % 4 * 4 + 2], st.o[i / 4][i % 4 * 4 + 3]};
+    x[i] = f32x4_t{st.o[i / 4][i % 4 * 4], st.o[i / 4][i % 4 * 4 + 1], st.o[i / 4][i % 4 * 4 + 2], st.o[i / 4][i % 4 * 4 + 3]} * f;
   write_row<T, D, BM, BN>(a, w, x, st.m, l, 4 * half, 8, half == 0, taken);
 }
 
@@ -637,11 +664,11 @@ __global__ __launch_bounds__(NW * kWave, 2) void attn_many(AttnArgs a) {
     full = true;
     if (min(row + BN, w.end) - 1 > w.first_own)
       taken |= __syncthreads_or(take_out<T, BN * L::C>(sv, threadIdx.x, NW * kWave));
-    if (!idle) masked_tile<T, D, BN>(st, q, sk, sv, row, w.own, highest, now, a.scale2, a.scale2_lo);
+    if (!idle) masked_tile<T, D, BN, false>(st, q, sk, sv, row, w.own, highest, now, a.scale2, a.scale2_lo);
     row += BN;
     odd = !odd;
   }
-  write_row<T, D, BM, BN>(a, w, st, taken);
+  write_row<T, D, BM, BN, false>(a, w, st, taken);
 }
 
 // Waits until at most N of this wave's copies and loads are outstanding.
@@ -657,7 +684,8 @@ __device__ __forceinline__ void wait_lds() {
 
 constexpr int kFewWaves = 4;
 
-template <int D> __global__ __launch_bounds__(kFewWaves * kWave, 2) void attn_few_bf16(AttnArgs a) {
+// (three waves per SIMD of 64 elements: the plan counts on them)
+template <int D> __global__ __launch_bounds__(kFewWaves * kWave, D == 64 ? 3 : 2) void attn_few_bf16(AttnArgs a) {
   using T = bf16_t;
   using L = TileLayout<T, D>;
   constexpr int NW = kFewWaves, BN = 32, kTile = BN * L::bytes;
@@ -689,7 +717,7 @@ template <int D> __global__ __launch_bounds__(kFewWaves * kWave, 2) void attn_fe
       taken |= __any(take_out<T, BN * L::C>(sv, lane, kWave));
       wait_lds();
     }
-    masked_tile<T, D, BN>(st, q, sk, sv, row, w.own, w.end, (uint32_t)__ballot(off >= 0), a.scale2, a.scale2_lo);
+    masked_tile<T, D, BN, true>(st, q, sk, sv, row, w.own, w.end, (uint32_t)__ballot(off >= 0), a.scale2, a.scale2_lo);
   };
   if (row < w.end) {
     Ld::template issue_one<false>(off, w.k, sk);
@@ -707,7 +735,7 @@ template <int D> __global__ __launch_bounds__(kFewWaves * kWave, 2) void attn_fe
         Ld::template issue_one<false>(off, w.k, sk);
         softmax_step<T, D>(st, s, a.scale2, a.scale2_lo);
         wait_copies<Ld::kInstr>();
-        values32<T, D>(sv, 0, s[0], st.o);
+        values32<T, D, true>(sv, 0, s[0], st);
       } else {
         masked();
         wait_lds();
@@ -749,7 +777,7 @@ template <int D> __global__ __launch_bounds__(kFewWaves * kWave, 2) void attn_fe
         for (int i = 0; i < 16; ++i) st.o[d][i] = st.o[d][i] * f + y[(d * 16 + i) * kWave + lane] * fo;
     }
   }
-  if (wave == 0) write_row<T, D, 32, BN>(a, w, st, taken);
+  if (wave == 0) write_row<T, D, 32, BN, true>(a, w, st, taken);
 }
 
 // The same in fp32, on 16 x 16 tiles: a quarter-wave holds a quarter of the head

@@ -1,0 +1,94 @@
+"""How exactly the cache operators weigh rows: the probabilities of bf16 models, against
+plain forms in 64 bits, within derived bounds."""
+from __future__ import annotations
+
+import math
+
+import pytest
+import torch
+
+import cache_ref as R
+from parity import log
+from test_gpu_cache_ops import within
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda"
+BF16, F32 = torch.bfloat16, torch.float32
+
+
+def lib():
+    from paper_2508_02751_amd import smallkv as S
+    return S
+
+
+# (name, sequences (rows, new), hq, hk, d, page, rows of a token's group that share a tile:
+# few or many)
+SHAPES = [
+    ("chunk in spans", [(700, 150), (300, 90)], 8, 2, 128, 16, False),
+    ("chunk in spans d64", [(700, 150), (300, 90)], 8, 2, 64, 16, False),
+    ("chunks without spans", [(300, 40)] * 32, 16, 16, 128, 32, False),
+    ("chunks without spans d64", [(200, 200), (150, 70)] * 24, 16, 16, 64, 0, False),
+    ("tokens in spans", [(1500, 1), (700, 1), (33, 1)], 14, 2, 64, 16, True),
+    ("tokens in spans d128", [(1500, 3), (700, 2)], 8, 2, 128, 16, True),
+    ("tokens without spans", [(400, 1)] * 40, 16, 16, 128, 0, True),
+]
+IDS = [c[0].replace(" ", "-") for c in SHAPES]
+
+
+def build(case, spread):
+    _, lens, hq, hk, d, page, few = case
+    c = R.Case(lens, hq, hk, d, BF16, page, seed=71)
+    # logits of this spread, the largest of them anywhere in the sequence: single rows
+    # with most of the weight, whose probabilities are not powers of two
+    c.q = (c.q.float() * spread).to(BF16)
+    return c, few
+
+
+@pytest.mark.parametrize("case", SHAPES, ids=IDS)
+def test_the_weights_add_up_to_one(case):
+    """With every value 1 the output is 1: what the weights are rounded to adds up to what
+    they are divided by, up to sums in fp32 (and 2^-16 for P in two parts), less than
+    half a step of bf16 below 1 (2^-9)."""
+    S = lib()
+    c, _ = build(case, 3.0)
+    c.v[~torch.isnan(c.v)] = 1.0
+    chunk, cache, q = c.to(DEV)
+    log(f"[ones] {case[0]}")
+    call = S.prepare_chunk_attn(chunk, cache, q, c.scale)
+    call.run()
+    torch.cuda.synchronize()
+    assert bool((call.out == 1.0).all()), f"{int((call.out != 1.0).sum())} of {call.out.numel()}"
+
+
+@pytest.mark.parametrize("spread", [0.3, 1.0, 3.0])
+@pytest.mark.parametrize("case", SHAPES, ids=IDS)
+def test_probabilities_of_bf16_models(case, spread):
+    """Few rows: P in two bf16 parts, 2^-16 relative.  Many: one part, each weight w off by
+    up to w 2^-8, and divided by the sum of the rounded ones, so that a row's output o moves
+    by at most 2^-8 sum w |v - o| (and second order, below 2^-7 of it)."""
+    S = lib()
+    c, few = build(case, spread)
+    c.v += 2.0  # a common part, which the weights must not scale
+    chunk, cache, q = c.to(DEV)
+    log(f"[bf16 weights] {case[0]} {spread}")
+    call = S.prepare_chunk_attn(chunk, cache, q, c.scale)
+    call.run()
+    torch.cuda.synchronize()
+    h, g = R.HALF[BF16], c.hq // c.hk
+    for b, (n, new) in enumerate(c.lens):
+        x, dx = R.logits(c, b)
+        v, _ = c.gather(c.v, b, n)
+        p = torch.softmax(x, -1)
+        o = torch.matmul(p, v[:, None])
+        away = torch.zeros_like(o)  # sum w |v - o|
+        for t in range(new):
+            away[:, :, t] = (p[:, :, t, :, None] * (v[:, None] - o[:, :, t, None]).abs()).sum(2)
+        a = torch.matmul(p, v.abs()[:, None])
+        tol = a * (2 * dx.amax(-1) + 2 * (n + 64) * R.U)[..., None] + 1.01 * h * o.abs()
+        tol += a * 2.0 ** -16 if few else 1.01 * h * away
+        rows = slice(c.starts[b], c.starts[b] + new)
+
+        def flat(t):
+            return t.movedim(2, 0).reshape(new, c.hq, c.d)
+        within(call.out[rows], flat(o), flat(tol), f"sequence {b}")
