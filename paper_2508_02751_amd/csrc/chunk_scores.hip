@@ -46,13 +46,26 @@ struct ScoreArgs {
   const float *before;
   float *out;
   int64_t rows, seq_stride;  // of before and out, in elements
-  float scale2;   // scale * log2(e)
+  float scale;    // bf16: scale * log2(e), see weight_of
   int span;       // few: keys per workgroup, a multiple of 128
   int walk;       // heads: tiles of query rows (of one token range) per workgroup
 };
 
 constexpr float kLog2e = 1.4426950408889634074f;
 constexpr int kNW = 4;
+
+// exp(scale * x - lse).  fp32 models: both as they were given, one rounding of their
+// difference, then log2(e): exact to 2^-23 of the difference, not of the logit (with the
+// bf16 models' form logits of 1000 gave weights off by 9e-5, most of them one way).
+// bf16 models: in log2 units from the start, an instruction less in a pass that the vector
+// units bound; the attention that made the lse rounds its factor the same way.
+template <typename T> __device__ __forceinline__ float lse_of(float lse) {
+  return sizeof(T) == 4 ? lse : lse * kLog2e;
+}
+template <typename T> __device__ __forceinline__ float weight_of(const ScoreArgs &a, float x, float lse) {
+  const float t = __builtin_fmaf(x, a.scale, -lse);
+  return __builtin_amdgcn_exp2f(sizeof(T) == 4 ? t * kLog2e : t);
+}
 
 // Sums over ROWS (16 or 32) neighbouring lanes' query rows: each exchange halves the keys
 // that a lane holds.  The lane ends with key register (lane % ROWS) * 16 / ROWS.
@@ -133,12 +146,12 @@ __global__ __launch_bounds__(kNW * kWave, SPLIT && sizeof(T) * D == 512 ? 1 : 2)
   };
   // own: its cached row; -1, which gives no weight: past the last, or sees no key
   int own = 0, own_now, r0 = 0;
-  float lse2 = 0.0f, lse_now;
+  float lse_x = 0.0f, lse_now;
   const unsigned char *q = a.q + (s.first + first) * a.q_token + head0 * a.q_head;
   auto issue = [&](unsigned char *dst, int row0) {
     const bool dead = token >= n_tokens || lse == -INFINITY;
     own = dead ? -1 : pos0 + first + token;
-    lse2 = dead ? 0.0f : lse * kLog2e;
+    lse_x = dead ? 0.0f : lse_of<T>(lse);
     const int rr = lane / L::C, p = lane & (L::C - 1);
 #pragma unroll
     for (int j = 0; j < kInstr; ++j) {
@@ -163,7 +176,7 @@ __global__ __launch_bounds__(kNW * kWave, SPLIT && sizeof(T) * D == 512 ? 1 : 2)
     wait_memory();
     if (!SPLIT) __syncthreads();
     own_now = own;
-    lse_now = lse2;
+    lse_now = lse_x;
     if (r0 + kRows < n_rows) {
       issue(nq, r0 + kRows);
       lookup();
@@ -191,12 +204,12 @@ __global__ __launch_bounds__(kNW * kWave, SPLIT && sizeof(T) * D == 512 ? 1 : 2)
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           const int key = key0 + 8 * (i / 4) + i % 4 + 4 * half;
-          const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], a.scale2, -base));
+          const float p = weight_of<T>(a, x[i], base);
           acc[i] += key <= o ? p : 0.0f;
         }
       } else {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) acc[i] += __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], a.scale2, -base));
+        for (int i = 0; i < 16; ++i) acc[i] += weight_of<T>(a, x[i], base);
       }
     }
     r0 += kRows;
@@ -297,7 +310,7 @@ __global__ __launch_bounds__(kNW * kWave, 2) void head_scores(ScoreArgs a) {
       const int token = 64 * t + (lane & (P - 1));
       const bool dead = token >= n_tokens || lse == -INFINITY;
       const int own = dead ? -1 : pos0 + first + token;
-      const float lse2 = dead ? 0.0f : lse * kLog2e;
+      const float lse_x = dead ? 0.0f : lse_of<T>(lse);
       const bool last = t + 1 == tiles;
       const int h_next = last ? h + 1 : h, t_next = last ? 0 : t + 1;
       if (h_next < groups) {
@@ -308,7 +321,7 @@ __global__ __launch_bounds__(kNW * kWave, 2) void head_scores(ScoreArgs a) {
       auto weigh = [&](int blk) {
         const int row = 32 * blk + (lane & 31), z = L::swz_k(row);
         const int o = __shfl(own, row, kWave);
-        const float base = __shfl(lse2, row, kWave);
+        const float base = __shfl(lse_x, row, kWave);
         f32x16_t x = {};
 #pragma unroll
         for (int i = 0; i < kFrag; ++i) {
@@ -327,12 +340,12 @@ __global__ __launch_bounds__(kNW * kWave, 2) void head_scores(ScoreArgs a) {
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
             const int key = key0 + 8 * (i / 4) + i % 4 + 4 * half;
-            const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], a.scale2, -base));
+            const float p = weight_of<T>(a, x[i], base);
             acc[i] += key <= o ? p : 0.0f;
           }
         } else {
 #pragma unroll
-          for (int i = 0; i < 16; ++i) acc[i] += __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], a.scale2, -base));
+          for (int i = 0; i < 16; ++i) acc[i] += weight_of<T>(a, x[i], base);
         }
       };
       weigh(0);
@@ -399,7 +412,7 @@ __global__ __launch_bounds__(kNW * kWave, 2) void few_scores(ScoreArgs a) {
   int key = begin + wave * 32 + (lane & 31);
   int page = page_of(key), page_next = page_of(key + step);
 
-  // the lane's query row, and the lse (log2 units) and own cached row of the 16 rows
+  // the lane's query row, and the lse (see lse_of) and own cached row of the 16 rows
   // whose logits it will hold
   uint4 qf[kFrag];
   {
@@ -412,17 +425,17 @@ __global__ __launch_bounds__(kNW * kWave, 2) void few_scores(ScoreArgs a) {
     for (int i = 0; i < kFrag; ++i)
       qf[i] = reinterpret_cast<const uint4 *>(row)[kBf16 ? 2 * i + half : half * kFrag + i];
   }
-  float lse2[16];
+  float lse_x[16];
   int own[16];
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
     const int r = 8 * (i / 4) + i % 4 + 4 * half;
-    lse2[i] = INFINITY;  // rows past the last, and rows that see no key, give no weight
+    lse_x[i] = INFINITY;  // rows past the last, and rows that see no key, give no weight
     own[i] = -1;
     if (r < rows) {
       const float x = a.lse[(int64_t)(s.first + r / a.g) * a.hq + kvh * a.g + r % a.g];
       if (x != -INFINITY) {
-        lse2[i] = x * kLog2e;
+        lse_x[i] = lse_of<T>(x);
         own[i] = pos0 + r / a.g;
       }
     }
@@ -456,7 +469,7 @@ __global__ __launch_bounds__(kNW * kWave, 2) void few_scores(ScoreArgs a) {
     page_next = page_of(key + 2 * step);
     float p[16];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], a.scale2, -lse2[i]));
+    for (int i = 0; i < 16; ++i) p[i] = weight_of<T>(a, x[i], lse_x[i]);
     if (base + 31 > pos0 || rows == 0 || __any(!exists)) {  // some row may not see some key
 #pragma unroll
       for (int i = 0; i < 16; ++i) p[i] = exists && key <= own[i] ? p[i] : 0.0f;
@@ -552,7 +565,7 @@ hipError_t launch_chunk_scores(const smallkv_chunk_t &c, const smallkv_cache_t &
   a.out = out;
   a.rows = score_rows;
   a.seq_stride = seq_stride;
-  a.scale2 = q.scale * kLog2e;
+  a.scale = e == 4 ? q.scale : q.scale * kLog2e;
   if (kv.dtype == SMALLKV_F32)
     (kv.head_dim == 64 ? launch_typed<float, 64> : launch_typed<float, 128>)(a, c.max_new, c.max_len, st);
   else

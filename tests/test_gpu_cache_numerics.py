@@ -92,3 +92,50 @@ def test_probabilities_of_bf16_models(case, spread):
         def flat(t):
             return t.movedim(2, 0).reshape(new, c.hq, c.d)
         within(call.out[rows], flat(o), flat(tol), f"sequence {b}")
+
+
+@pytest.mark.parametrize("lens,per_kv", [
+    ([(300, 1), (77, 1)], True), ([(300, 1), (77, 3)], False),     # rows of K streamed
+    ([(300, 20), (90, 12)], False), ([(400, 60)], False),          # several heads a workgroup
+    ([(400, 30)], True), ([(500, 140)], False),                    # keys in 32s, rows dealt
+    ([(300, 40)] * 30, True), ([(300, 130)] * 12, False)])         # keys in 128s
+@pytest.mark.parametrize("d", [64, 128])
+def test_fp32_scores_of_large_logits(d, lens, per_kv):
+    """Logits of 4000 that are exact (whole numbers times the scale): what is left is the
+    rounding of logit - lse, of its product with log2(e) and of the exponential, each
+    relative to the difference and not to the logit, and the sums."""
+    S = lib()
+    c = R.Case(lens, 8, 2, d, F32, 16, seed=73)
+    g = torch.Generator().manual_seed(d)
+    u = torch.randint(1, 4, (d,), generator=g).float() * (2 * torch.randint(0, 2, (d,), generator=g) - 1)
+
+    def near(x, shape):  # x and a few elements of it changed
+        change = torch.randint(-1, 2, (*shape, d), generator=g) * (torch.rand(*shape, d, generator=g) < 0.05)
+        return x + change.float()
+    c.scale = float(torch.tensor(1.0 / math.sqrt(d)))
+    size = int(4000 / (float((u * u).sum()) * c.scale) / 4)
+    for b, (n, _) in enumerate(lens):
+        for r in range(n):
+            p, i = c.slot(b, r)
+            c.k[p, :, i] = near(u * size, (c.hk,))
+    c.q = near(u * 4, (c.T, c.hq))
+    chunk, cache, q = c.to(DEV)
+    x = [R.logits(c, b)[0] for b in range(c.B)]
+    lse = torch.cat([torch.logsumexp(x[b], -1).permute(2, 0, 1).reshape(new, c.hq)
+                     for b, (_, new) in enumerate(lens)]).float()
+    assert 3000 < float(lse.min()) and float(lse.max()) < 5000
+    heads = c.hk if per_kv else c.hq
+    out = torch.zeros(c.B, heads, c.rows, device=DEV)
+    log(f"[fp32 scores] {d} {len(lens)} {lens[0]} per_kv={per_kv}")
+    S.prepare_chunk_scores(chunk, cache, q, lse.to(DEV), c.scale, out).run()
+    torch.cuda.synchronize()
+    group = c.hq // c.hk
+    for b, (n, new) in enumerate(lens):
+        e = lse[c.starts[b]: c.starts[b] + new].double().view(new, c.hk, group).permute(1, 2, 0)[..., None]
+        t = x[b] - e
+        w = torch.exp(t)
+        tol = w * ((3 * t.abs().nan_to_num(0, 0, 0) + 4 + (new * group if per_kv else new) + 64) * R.U)
+        w, tol = w.sum(2), tol.sum(2)
+        if per_kv:
+            w, tol = w.sum(1), tol.sum(1)
+        within(out[b, :, :n], w.reshape(heads, n), tol.reshape(heads, n), f"sequence {b}")
