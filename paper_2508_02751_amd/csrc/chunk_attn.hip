@@ -447,26 +447,6 @@ __device__ __forceinline__ void masked_tile(State<T, D> &st, const QFrag<T, D> &
   }
 }
 
-// Adds the infinite and NaN values of keys from..to to the lane's own elements (groups
-// of W, `step` apart from `at` on) of an output row that is written already (any
-// weight > 0 leaves them what they are).
-template <typename O, typename T, int D, int W>
-__device__ __forceinline__ void give_back(const AttnArgs &a, int b, const unsigned char *v, void *out, int from, int to,
-                                          int at, int step) {
-#pragma unroll 1
-  for (int key = from; key <= to; ++key) {
-    const int64_t off = row_offset(a.kv, b, key);
-    if (off < 0) continue;
-#pragma unroll 1
-    for (int e0 = at; e0 < D; e0 += step)
-#pragma unroll 1
-      for (int e = e0; e < e0 + W; ++e) {
-        const float x = elem<T>::load1(v + off, e);
-        if (!(fabsf(x) <= 3.402823466e38f)) elem<O>::store1(out, e, elem<O>::load1(out, e) + x);
-      }
-  }
-}
-
 // A workgroup's share of the work, and the lane's row of it.
 template <int BM> struct Share {
   Tile t;
@@ -513,6 +493,37 @@ template <int BM> struct Share {
   }
 };
 
+// Adds the infinite and NaN values of keys from..to, times their weights, to the lane's own
+// elements (groups of W, `step` apart from `at` on) of an output row that is written
+// already: a weight > 0 leaves them what they are, and a logit of -inf, weight 0, makes
+// them NaN, as the matrix product does in a tile that nothing is taken out of.
+template <typename O, typename T, int D, int W, int BM>
+__device__ __forceinline__ void give_back(const AttnArgs &a, const Share<BM> &w, void *out, int from, int to, int at,
+                                          int step) {
+#pragma unroll 1
+  for (int key = from; key <= to; ++key) {
+    const int64_t off = row_offset(a.kv, w.t.b, key);
+    if (off < 0) continue;
+    bool none = false, known = false;
+#pragma unroll 1
+    for (int e0 = at; e0 < D; e0 += step)
+#pragma unroll 1
+      for (int e = e0; e < e0 + W; ++e) {
+        const float x = elem<T>::load1(w.v + off, e);
+        if (fabsf(x) <= 3.402823466e38f) continue;
+        if (!known) {
+          const unsigned char *q = a.q + (w.token * a.q_token + w.head * a.q_head) * (int64_t)sizeof(T);
+          float s = 0.0f;
+#pragma unroll 1
+          for (int i = 0; i < D; ++i) s = __builtin_fmaf(elem<T>::load1(q, i), elem<T>::load1(w.k + off, i), s);
+          none = s == -INFINITY;
+          known = true;
+        }
+        elem<O>::store1(out, e, none ? NAN : elem<O>::load1(out, e) + x);
+      }
+  }
+}
+
 // The lane's part of a row of the output, or of the span's record: N groups of four
 // elements of o, `step` apart from `at` on, l the row's sum.  writes: one lane per row;
 // taken: values were taken out of a tile of BN keys.
@@ -529,22 +540,23 @@ __device__ __forceinline__ void write_row(const AttnArgs &a, const Share<BM> &w,
       a.rec[a.rec_ml + 2 * row] = m;
       a.rec[a.rec_ml + 2 * row + 1] = l;
     }
-    if (taken) give_back<float, T, D, 4>(a, w.t.b, w.v, o, from, to, at, step);
+    if (taken) give_back<float, T, D, 4>(a, w, o, from, to, at, step);
     return;
   }
-  const float inv = l == 0.0f ? 0.0f : 1.0f / l;  // (0: the row sees no key)
+  const bool none = l == 0.0f;  // the row sees no key, or only logits of -inf
+  const float inv = 1.0f / l;
   unsigned char *o = a.out + (w.token * a.o_token + w.head * a.o_head) * (int64_t)sizeof(T);
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    const f32x4_t y = x[i] * inv;
+    const f32x4_t y = none ? f32x4_t{} : x[i] * inv;
     if constexpr (sizeof(T) == 4)
       *reinterpret_cast<f32x4_t *>(o + (at + i * step) * 4) = y;
     else
       *reinterpret_cast<bf16x4_t *>(o + (at + i * step) * 2) = __builtin_convertvector(y, bf16x4_t);
   }
-  if (taken) give_back<T, T, D, 4>(a, w.t.b, w.v, o, from, to, at, step);
+  if (taken && !none) give_back<T, T, D, 4>(a, w, o, from, to, at, step);
   if (a.lse && writes)
-    a.lse[(int64_t)w.token * a.hq + w.head] = l == 0.0f ? -INFINITY : (m + __log2f(l)) * kLn2;
+    a.lse[(int64_t)w.token * a.hq + w.head] = none ? -INFINITY : (m + __log2f(l)) * kLn2;
 }
 
 template <typename T, int D, int BM, int BN, bool TWO>
@@ -555,7 +567,8 @@ __device__ __forceinline__ void write_row(const AttnArgs &a, const Share<BM> &w,
   const int half = (threadIdx.x & (kWave - 1)) >> 5;
   if (sizeof(T) == 2 && w.t.n_split == 1) {
     // half-waves exchange four elements of 16, so that each lane writes eight at once
-    const float inv = l == 0.0f ? 0.0f : 1.0f / rounded;
+    const bool none = l == 0.0f;
+    const float inv = 1.0f / rounded;
     unsigned char *o = a.out + (w.token * a.o_token + w.head * a.o_head) * 2;
 #pragma unroll
     for (int j = 0; j < D / 16; ++j) {
@@ -563,7 +576,7 @@ __device__ __forceinline__ void write_row(const AttnArgs &a, const Share<BM> &w,
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int e = j % 2 * 8 + 2 * i;
-        const f32x2_t v = {st.o[j / 2][e] * inv, st.o[j / 2][e + 1] * inv};
+        const f32x2_t v = none ? f32x2_t{} : f32x2_t{st.o[j / 2][e] * inv, st.o[j / 2][e + 1] * inv};
         y[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2_t));
       }
       const auto p = __builtin_amdgcn_permlane32_swap(y[0], y[2], false, false);
@@ -571,10 +584,10 @@ __device__ __forceinline__ void write_row(const AttnArgs &a, const Share<BM> &w,
       if (w.live) *reinterpret_cast<uint4 *>(o + j * 32 + half * 16) = make_uint4(p[0], q[0], p[1], q[1]);
     }
     if (!w.live) return;
-    if (taken)
-      give_back<T, T, D, 8>(a, w.t.b, w.v, o, max(w.begin, w.first_own + 2 - BN), min(w.end - 1, w.own), 8 * half, 16);
+    if (taken && !none)
+      give_back<T, T, D, 8>(a, w, o, max(w.begin, w.first_own + 2 - BN), min(w.end - 1, w.own), 8 * half, 16);
     if (a.lse && half == 0)
-      a.lse[(int64_t)w.token * a.hq + w.head] = l == 0.0f ? -INFINITY : (st.m + __log2f(l)) * kLn2;
+      a.lse[(int64_t)w.token * a.hq + w.head] = none ? -INFINITY : (st.m + __log2f(l)) * kLn2;
     return;
   }
   if (!w.live) return;
@@ -974,7 +987,7 @@ __global__ __launch_bounds__(kMaxParts * (D / 4)) void attn_merge(AttnArgs a) {
       for (int g = group + n_rows; g < n_rows * a.parts; g += n_rows) join(sml[g], so[g * W + threadIdx.x % W]);
   }
   if (part > 0 || r >= t.rows) return;
-  const f32x4_t x = o * (l == 0.0f ? 0.0f : 1.0f / l);
+  const f32x4_t x = l == 0.0f ? f32x4_t{} : o * (1.0f / l);
   unsigned char *out = a.out + (token * a.o_token + head * a.o_head) * (int64_t)sizeof(T);
   if constexpr (sizeof(T) == 4)
     *reinterpret_cast<f32x4_t *>(out + e * 4) = x;

@@ -139,3 +139,54 @@ def test_fp32_scores_of_large_logits(d, lens, per_kv):
         if per_kv:
             w, tol = w.sum(1), tol.sum(1)
         within(out[b, :, :n], w.reshape(heads, n), tol.reshape(heads, n), f"sequence {b}")
+
+
+@pytest.mark.parametrize("dtype,d", [(BF16, 64), (BF16, 128), (F32, 64), (F32, 128)])
+@pytest.mark.parametrize("new,hq", [(40, 8), (3, 8), (1, 8), (8, 16)])
+@pytest.mark.parametrize("pages", [[5], [33], [37], list(range(16, 32)), [4, 34, 36]], ids=str)
+def test_infinite_values_of_rows_without_weight(pages, new, hq, dtype, d):
+    """Rows that are seen with a logit of -inf, in tiles that every token sees whole, in the
+    last ones and over whole spans: 0 times their infinite and NaN values is NaN for
+    the tokens that see them, and nothing else of the output changes."""
+    S = lib()
+    c = R.Case([(300, new), (70, min(new, 1))], hq, 2, d, dtype, 8, seed=79)
+    c.q = c.q.abs()
+    lo, at = {}, [3, d // 2, d - 1]
+    for j, page in enumerate(pages):
+        p, e = int(c.table[0, page]), at[j % 3]
+        c.k[p, :, :, 3] = -math.inf
+        c.v[p, :, 2, e] = (math.inf, -math.inf, math.nan)[j % 3]
+        lo[e] = min(lo.get(e, 1 << 30), 8 * page + 2)
+    chunk, cache, q = c.to(DEV)
+    c.table = c.table.clone()
+    c.table[0, pages] = -1  # for the plain form: no weight
+    want, wl, tol, ltol = R.attention(c)
+    for t in range(new):
+        for e, row in lo.items():
+            if row <= 300 - new + t:
+                want[t, :, e] = math.nan
+    log(f"[0 * inf] {dtype} {d} {new} {hq} pages {pages}")
+    call = S.prepare_chunk_attn(chunk, cache, q, c.scale)
+    call.run()
+    torch.cuda.synchronize()
+    within(call.out, want, tol, "out")
+    within(call.lse, wl, ltol, "lse")
+
+
+@pytest.mark.parametrize("dtype,d", [(BF16, 128), (F32, 64)])
+@pytest.mark.parametrize("lens", [[(70, 40), (1000, 3)], [(5, 1), (1000, 2)], [(64, 64), (9, 9)], [(20, 1)] * 300],
+                         ids=str)
+def test_rows_of_minus_infinity_only(lens, dtype, d):
+    """Logits that are all -inf: an output of 0 and an lse of -inf, whatever the values."""
+    S = lib()
+    c = R.Case(lens, 8, 2, d, dtype, 8, seed=83)
+    c.q = c.q.abs()
+    c.k[..., 7] = -math.inf
+    c.v[..., 2] = math.inf
+    c.v[..., 5] = math.nan
+    chunk, cache, q = c.to(DEV)
+    log(f"[only -inf] {dtype} {lens[:2]}")
+    call = S.prepare_chunk_attn(chunk, cache, q, c.scale)
+    call.run()
+    torch.cuda.synchronize()
+    assert bool((call.out == 0).all()) and bool(torch.isneginf(call.lse).all())
