@@ -586,7 +586,7 @@ int smallkv_append(const smallkv_chunk_t *chunk, const smallkv_cache_t *cache,
  * or whose logits are all -inf, gets out = 0 and lse = -inf.  Infinities and NaN in rows a token does not see
  * do not reach it.  A row it sees with a logit of -inf has weight 0: its infinite and
  * NaN values make their elements NaN, as 0 times them is (where a finite logit's weight
- * underflows, below 2^-126 of the row's largest, infinite or NaN).  bf16 models: with max_new tokens of at most 32
+ * underflows, below 2^-100 of the row's largest, infinite or NaN).  bf16 models: with max_new tokens of at most 32
  * (token, query head) rows per kv head the probabilities keep 16 bits in the product
  * with V, else 8 (2^-8 relative) with weights that still add up to 1; sums, logits
  * and statistics are fp32.

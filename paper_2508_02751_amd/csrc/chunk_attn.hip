@@ -318,18 +318,23 @@ __device__ __forceinline__ void values32(const unsigned char *sv, int key0, cons
       bf16x8_t pf, lo;
 #pragma unroll
       for (int e = 0; e < 8; e += 2) {
-        const f32x2_t x = {p[8 * s + e], p[8 * s + e + 1]};
-        const bf16x2_t w = __builtin_convertvector(x, bf16x2_t);
-        pf[e] = w[0];
-        pf[e + 1] = w[1];
+        bf16x2_t w, y;
         if constexpr (TWO) {
-          const uint32_t u = __builtin_bit_cast(uint32_t, w);
-          const bf16x2_t y = __builtin_convertvector((f32x2_t{x[0] - bf16_lo(u), x[1] - bf16_hi(u)}), bf16x2_t);
+          // the first part is cut off and the second never 0, so that an infinite value
+          // times either is the same infinity
+          const uint32_t u0 = __float_as_uint(p[8 * s + e]), u1 = __float_as_uint(p[8 * s + e + 1]);
+          w = __builtin_bit_cast(bf16x2_t, __builtin_amdgcn_perm(u1, u0, 0x07060302));
+          const float y0 = __builtin_fmaf(p[8 * s + e], 0x1p-24f, p[8 * s + e] - bf16_hi(u0));
+          const float y1 = __builtin_fmaf(p[8 * s + e + 1], 0x1p-24f, p[8 * s + e + 1] - bf16_hi(u1));
+          y = __builtin_convertvector((f32x2_t{y0, y1}), bf16x2_t);
           lo[e] = y[0];
           lo[e + 1] = y[1];
         } else {
+          w = __builtin_convertvector((f32x2_t{p[8 * s + e], p[8 * s + e + 1]}), bf16x2_t);
           sum = __builtin_amdgcn_fdot2_f32_bf16(w, ones, sum, false);
         }
+        pf[e] = w[0];
+        pf[e + 1] = w[1];
       }
       // the transposing read: 16 lanes take 4 rows of 16 elements, lane i of
       // them ends with the 4 rows' element i

@@ -190,3 +190,25 @@ def test_rows_of_minus_infinity_only(lens, dtype, d):
     call.run()
     torch.cuda.synchronize()
     assert bool((call.out == 0).all()) and bool(torch.isneginf(call.lse).all())
+
+
+@pytest.mark.parametrize("dtype,d", [(BF16, 64), (BF16, 128), (F32, 64), (F32, 128)])
+@pytest.mark.parametrize("lens", [[(1500, 1), (300, 1)], [(700, 60)], [(300, 3)], [(200, 1)] * 70], ids=str)
+def test_infinite_values_that_every_token_sees(lens, dtype, d):
+    """In tiles that nothing is taken out of: infinite times any weight is infinite."""
+    S = lib()
+    c = R.Case(lens, 8, 8, d, dtype, 16, seed=89)
+    for b in range(c.B):
+        for r, e, x in ((2, 1, math.inf), (40, 5, -math.inf), (130, 9, math.nan), (41, 1, math.inf),
+                        (129, 20, math.inf), (131, 20, -math.inf)):
+            p, i = c.slot(b, r)
+            c.v[p, :, i, e] = x
+    chunk, cache, q = c.to(DEV)
+    log(f"[inf seen] {dtype} {d} {lens[:2]}")
+    call = S.prepare_chunk_attn(chunk, cache, q, c.scale)
+    call.run()
+    torch.cuda.synchronize()
+    want, wl, tol, ltol = R.attention(c)
+    assert bool(torch.isposinf(want[..., 1]).all()) and bool(torch.isneginf(want[..., 5]).all())
+    within(call.out, want, tol, "out")
+    within(call.lse, wl, ltol, "lse")
