@@ -118,7 +118,9 @@ class ModelCache:
 
     rows[b]: rows in use; tokens[b]: the sequence's length (more than its rows once
     the cache is compressed: row_pos [B][layers][Hkv][n_rows] then names the rows'
-    positions).  With keep_scores, scores [B][layers * Hkv][n_rows] sum the
+    positions).  Both count a chunk from the first layer that has taken it: a chunk
+    whose first layer() raised is not part of the cache, and the next begin() replaces
+    it.  With keep_scores, scores [B][layers * Hkv][n_rows] sum the
     attention each row has received, over queries and the query heads of a kv head.
     Everything runs on the current stream.
     """
@@ -134,7 +136,7 @@ class ModelCache:
         self.scores = new(batch, layers * kv_heads, n_rows, dt=torch.float32) if keep_scores else None
         self.row_pos = new(batch, layers, kv_heads, n_rows, dt=torch.int32) if positions else None
         self.rows, self.tokens = [0] * batch, [0] * batch
-        self._chunk = None
+        self._chunk = self._taken = None
 
     @property
     def n_rows(self) -> int:
@@ -144,7 +146,8 @@ class ModelCache:
         return torch.tensor(v, dtype=torch.int32, device=self.k.device)
 
     def begin(self, new: Sequence[int]) -> int:
-        """Take new[b] more tokens per sequence (packed in this order); their number."""
+        """Announce new[b] more tokens per sequence (packed in this order); their number.
+        The layers then take them one by one."""
         if len(new) != len(self.rows) or min(new) < 0:
             raise ValueError("begin() takes the number of new tokens of every sequence")
         rows = [r + n for r, n in zip(self.rows, new)]
@@ -155,28 +158,34 @@ class ModelCache:
             start.append(start[-1] + n)
         pos = [t + i for t, n in zip(self.tokens, new) for i in range(n)]
         self._positions = self._ints(pos)
-        self.rows, self.tokens = rows, [t + n for t, n in zip(self.tokens, new)]
         self._chunk = S.ChunkSpec(self._ints(start), self._ints(rows), start[-1],
                                   max(max(new), 1), max(max(rows), 1))
+        self._taken = rows, [t + n for t, n in zip(self.tokens, new)]
         return start[-1]
 
     def layer(self, layer: int, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor):
-        """The chunk's queries, keys and values in one layer: (attention output, turned
-        queries), [T][Hq][d] both."""
+        """The chunk's queries, keys and values in one layer (negative: from the last):
+        (attention output, turned queries), [T][Hq][d] both.  What is refused is refused
+        before anything is written."""
         if self._chunk is None:
             raise ValueError("begin() first")
+        if not -self.layers <= layer < self.layers:
+            raise IndexError(f"layer {layer} of {self.layers}")
+        layer %= self.layers
         cache = S.CacheSpec(self.k[:, layer], self.v[:, layer])
         scale = softmax_scale(self.k.shape[-1])
         pos = None if self.row_pos is None else self.row_pos[:, layer]
         add = S.prepare_append(self._chunk, cache, self.rope, q, k, v, positions=self._positions,
                                row_pos=pos)
-        add.run()
         attn = S.prepare_chunk_attn(self._chunk, cache, add.q_out, scale)
-        attn.run()
+        calls = [add, attn]
         if self.scores is not None:
             h = slice(layer * self.kv_heads, (layer + 1) * self.kv_heads)
-            S.prepare_chunk_scores(self._chunk, cache, add.q_out, attn.lse, scale,
-                                   self.scores[:, h], before=self.scores[:, h]).run()
+            calls.append(S.prepare_chunk_scores(self._chunk, cache, add.q_out, attn.lse, scale,
+                                                self.scores[:, h], before=self.scores[:, h]))
+        for call in calls:
+            call.run()
+        self.rows, self.tokens = self._taken
         return attn.out, add.q_out
 
     def compress(self, keep: Sequence[int], recent: Optional[Sequence[int]] = None, sinks: int = 0,

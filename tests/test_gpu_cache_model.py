@@ -1,0 +1,72 @@
+"""pipeline.ModelCache on the GPU beside its plain use: layers counted from the last,
+refused calls, far larger caches than their rows, and other streams."""
+from __future__ import annotations
+
+import pytest
+import torch
+
+from parity import log
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda"
+
+
+def lib():
+    from paper_2508_02751_amd import pipeline as P
+    from paper_2508_02751_amd import smallkv as S
+    return P, S
+
+
+def build(layers=2, n_rows=64, batch=2, heads=2, **kw):
+    P, S = lib()
+    freq, amp = S.rope_freqs(64, 10000.0)
+    return P.ModelCache(batch, layers, 2 * heads, heads, 64, n_rows, S.RopeSpec(freq, S.ROPE_HALF, amp),
+                        torch.bfloat16, DEV, **kw)
+
+
+def tokens(g, T, heads=2):
+    return [torch.randn(T, h, 64, generator=g).to(DEV, torch.bfloat16) for h in (2 * heads, heads, heads)]
+
+
+def same(a, b):
+    return all(torch.equal(x, y) for x, y in ((a.k, b.k), (a.v, b.v), (a.scores, b.scores)))
+
+
+def test_layers_from_the_last():
+    a, b = build(keep_scores=True), build(keep_scores=True)
+    g = torch.Generator().manual_seed(1)
+    log("[model cache] negative layers")
+    for new in ([30, 12], [1, 1], [0, 20]):
+        T = a.begin(new)
+        assert b.begin(new) == T
+        for layer in (0, 1):
+            x = tokens(g, T)
+            out, q = a.layer(layer, *x)
+            out2, q2 = b.layer(layer - 2, *x)
+            assert torch.equal(out, out2) and torch.equal(q, q2)
+    torch.cuda.synchronize()
+    assert a.rows == b.rows == [31, 33] and same(a, b)
+
+
+def test_a_refused_call_changes_nothing():
+    a, b = build(keep_scores=True), build(keep_scores=True)
+    g = torch.Generator().manual_seed(2)
+    log("[model cache] refused")
+    for new in ([30, 12], [5, 0]):
+        T = a.begin(new)
+        b.begin(new)
+        for layer in (0, 1):
+            x = tokens(g, T)
+            a.layer(layer, *x)
+            before = b.k.clone(), b.v.clone(), b.scores.clone(), list(b.rows), list(b.tokens)
+            for bad in ((layer, x[0], x[1], x[2][:-1]), (layer, x[0].float(), x[1], x[2]),
+                        (layer, x[0], x[1].cpu(), x[2]), (2, *x), (-3, *x)):
+                with pytest.raises((ValueError, IndexError)):
+                    b.layer(*bad)
+            torch.cuda.synchronize()
+            now = b.k, b.v, b.scores
+            assert all(torch.equal(p, q) for p, q in zip(before, now)) and before[3:] == (b.rows, b.tokens)
+            b.layer(layer, *x)  # the same chunk, as if nothing had been refused
+    torch.cuda.synchronize()
+    assert a.rows == b.rows and a.tokens == b.tokens and same(a, b)
