@@ -203,7 +203,8 @@ class ModelCache:
                         S.CacheSpec(to.k.flatten(1, 2), to.v.flatten(1, 2)), self._ints(self.rows),
                         self._ints(keep), self.scores,
                         recent=None if recent is None else self._ints(recent), sinks=sinks,
-                        row_pos=pos, out_pos=to.row_pos.view(B, L * H, -1), out_scores=to.scores).run()
+                        row_pos=pos, out_pos=to.row_pos.view(B, L * H, -1), out_scores=to.scores,
+                        max_len=max(max(self.rows), 1)).run()
         to.rows = [max(0, min(k, r, to.n_rows)) for k, r in zip(keep, self.rows)]
         to.tokens = list(self.tokens)
         return to

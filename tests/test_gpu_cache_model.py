@@ -70,3 +70,20 @@ def test_a_refused_call_changes_nothing():
             b.layer(layer, *x)  # the same chunk, as if nothing had been refused
     torch.cuda.synchronize()
     assert a.rows == b.rows and a.tokens == b.tokens and same(a, b)
+
+
+def test_compression_goes_by_the_rows_in_use():
+    """A cache of more rows than an eviction takes, most of them unused."""
+    import cache_ref as R
+    n = (1 << 20) + 64
+    c = build(1, n, 1, 1, keep_scores=True)
+    g = torch.Generator().manual_seed(3)
+    log("[model cache] a few rows of many")
+    c.layer(0, *tokens(g, c.begin([150]), 1))
+    small = c.compress([40], [5], 2)
+    torch.cuda.synchronize()
+    rows = R.kept_rows(c.scores[0, 0].tolist()[:150], 150, 40, 5, 2, 40)
+    assert small.row_pos[0, 0, 0].tolist() == rows and small.rows == [40]
+    assert torch.equal(small.k[0, 0, 0], c.k[0, 0, 0, rows]) and torch.equal(small.v[0, 0, 0], c.v[0, 0, 0, rows])
+    # and with no rows at all
+    assert build(1, n, 1, 1, keep_scores=True).compress([7]).rows == [0]
