@@ -145,6 +145,9 @@ class ModelCache:
     def _ints(self, v) -> torch.Tensor:
         return torch.tensor(v, dtype=torch.int32, device=self.k.device)
 
+    def _stream(self) -> Optional[int]:
+        return torch._C._cuda_getCurrentRawStream(self.k.device.index) if self.k.is_cuda else None
+
     def begin(self, new: Sequence[int]) -> int:
         """Announce new[b] more tokens per sequence (packed in this order); their number.
         The layers then take them one by one."""
@@ -161,6 +164,7 @@ class ModelCache:
         self._chunk = S.ChunkSpec(self._ints(start), self._ints(rows), start[-1],
                                   max(max(new), 1), max(max(rows), 1))
         self._taken = rows, [t + n for t, n in zip(self.tokens, new)]
+        self._home = self._stream()
         return start[-1]
 
     def layer(self, layer: int, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor):
@@ -185,6 +189,9 @@ class ModelCache:
                                                 self.scores[:, h], before=self.scores[:, h]))
         for call in calls:
             call.run()
+        if self._stream() != self._home:  # the chunk's tensors, which the next begin() drops
+            for t in (self._chunk.start, self._chunk.length, self._positions):
+                t.record_stream(torch.cuda.current_stream(self.k.device))
         self.rows, self.tokens = self._taken
         return attn.out, add.q_out
 

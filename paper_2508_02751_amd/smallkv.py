@@ -698,17 +698,19 @@ class _Call:
     def _prepare(self, name, dev, keep, own, *args):
         self._name, self._fn, self._dev, self._keep = name, getattr(lib(), name), dev, keep
         self._own = [t for t in own if t is not None]
+        self._home = torch._C._cuda_getCurrentRawStream(dev.index)  # where they were allocated
         self._args = tuple(C.byref(x) if isinstance(x, C.Structure) else x for x in args)
 
     def run(self, stream=None):
         """Enqueue on the tensors' device, on its current stream unless one is given (the
-        caller orders it after what the tensors' own streams still do)."""
+        caller orders it after what the tensors' own streams still do, and keeps the call
+        as long as a graph that captured it)."""
         i = self._dev.index
-        if stream is not None:
-            for t in self._own:  # not reused before that stream is done with them
-                t.record_stream(stream)
         # (the raw handle: a Stream object costs more than the launch)
         s = torch._C._cuda_getCurrentRawStream(i) if stream is None else stream.cuda_stream
+        if s != self._home:
+            for t in self._own:  # not reused before that stream is done with them
+                t.record_stream(torch.cuda.current_stream(i) if stream is None else stream)
         if torch.cuda.current_device() == i:
             rc = self._fn(*self._args, s)
         else:

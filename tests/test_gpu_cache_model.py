@@ -87,3 +87,68 @@ def test_compression_goes_by_the_rows_in_use():
     assert torch.equal(small.k[0, 0, 0], c.k[0, 0, 0, rows]) and torch.equal(small.v[0, 0, 0], c.v[0, 0, 0, rows])
     # and with no rows at all
     assert build(1, n, 1, 1, keep_scores=True).compress([7]).rows == [0]
+
+
+def busy(stream):
+    """Work of some tens of milliseconds on the stream."""
+    with torch.cuda.stream(stream):
+        torch.cuda._sleep(100_000_000)
+
+
+def ready(stream):
+    stream.wait_stream(torch.cuda.current_stream())
+
+
+@pytest.mark.parametrize("given", [False, True])
+def test_memory_of_a_dropped_call_waits_for_its_stream(given):
+    """A call prepared on one stream, run on another (given, or made the current one) that is
+    still busy, and dropped: its output, lse and workspace are not handed out again before
+    that stream has passed it."""
+    _, S = lib()
+    import cache_ref as R
+    c = R.Case([(700, 3), (300, 1)], 8, 2, 128, torch.bfloat16, 16, seed=7)
+    chunk, cache, q = c.to(DEV)
+    side = torch.cuda.Stream()
+    call = S.prepare_chunk_attn(chunk, cache, q, c.scale)
+    ready(side)
+    busy(side)
+    log(f"[streams] dropped call, given={given}")
+    if given:
+        call.run(side)
+    else:
+        with torch.cuda.stream(side):
+            call.run()
+    mine = {t.data_ptr(): t.numel() * t.element_size() for t in (call.out, call.lse, call.ws)}
+    del call
+    others = [torch.zeros(n, dtype=torch.uint8, device=DEV) for n in mine.values()]
+    assert not side.query(), "the stream was done too early to tell"
+    assert not any(t.data_ptr() in mine for t in others)
+    torch.cuda.synchronize()
+
+
+def test_a_chunk_on_another_stream():
+    """begin() on one stream, layer() on another that is still busy when the next chunk
+    begins: the first chunk's lengths and positions are kept until it has read them."""
+    a, b = build(1, keep_scores=True), build(1, keep_scores=True)
+    g = torch.Generator().manual_seed(5)
+    x, y = tokens(g, 42), tokens(g, 2)
+    side = torch.cuda.Stream()
+    log("[streams] chunk")
+    b.begin([30, 12])
+    b.layer(0, *x)
+    b.begin([1, 1])
+    b.layer(0, *y)
+    a.begin([30, 12])
+    ready(side)
+    busy(side)
+    ptrs = {t.data_ptr() for t in (a._chunk.start, a._chunk.length, a._positions)}
+    with torch.cuda.stream(side):
+        a.layer(0, *x)
+    a.begin([1, 1])
+    more = [torch.zeros(n, dtype=torch.int32, device=DEV) for n in (3, 2, 42)]
+    assert not side.query(), "the stream was done too early to tell"
+    assert not any(t.data_ptr() in ptrs for t in (a._chunk.start, a._chunk.length, a._positions, *more))
+    torch.cuda.current_stream().wait_stream(side)
+    a.layer(0, *y)
+    torch.cuda.synchronize()
+    assert a.rows == b.rows and same(a, b)
