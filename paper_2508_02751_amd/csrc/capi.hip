@@ -187,6 +187,9 @@ int check_match(const smallkv_match_t *m) {
 
 // ---- cache operators ----
 
+// Workgroups of 256 threads in one launch: the threads are counted in 32 bits.
+constexpr int64_t kMaxGroups = (1 << 24) - 1;
+
 // A stride in elements: not negative, whole 16-byte pieces.
 bool stride_ok(int64_t s, int dtype) { return s >= 0 && s % (dtype == SMALLKV_F32 ? 4 : 8) == 0; }
 
@@ -207,12 +210,9 @@ int check_cache(const smallkv_cache_t *c, int batch) {
   if (c->head_dim != 64 && c->head_dim != 128) return SMALLKV_EUNSUPPORTED;
   for (const int64_t s : strides)
     if (s / (c->dtype == SMALLKV_F32 ? 4 : 8) > UINT32_MAX) return SMALLKV_EUNSUPPORTED;
-  if ((int64_t)batch * c->n_heads > (1 << 24)) return SMALLKV_EUNSUPPORTED;
+  if ((int64_t)batch * c->n_heads > kMaxGroups) return SMALLKV_EUNSUPPORTED;
   return SMALLKV_OK;
 }
-
-// Workgroups of 256 threads in one launch: the threads are counted in 32 bits.
-constexpr int64_t kMaxGroups = (1 << 24) - 1;
 
 // Rows that are written: no broadcast strides.
 bool writable(const smallkv_cache_t &c) {

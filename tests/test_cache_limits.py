@@ -1,0 +1,20 @@
+"""What the cache operators refuse on the host, at the limits themselves (no GPU needed)."""
+import ctypes as C
+
+import pytest
+
+from paper_2508_02751_amd import smallkv as S
+from test_cache_abi import append, cache, chunk, queries, try_attn
+
+
+@pytest.mark.parametrize("batch,heads", [(1 << 24, 1), (1 << 23, 2), (1, 1 << 24)])
+def test_a_launch_counts_fewer_than_2_to_the_24_workgroups(batch, heads):
+    """2^24 pairs of a sequence and a kv head, a workgroup of 256 threads each, are 2^32
+    threads: refused, for a decode step's scores as for the others."""
+    L, q = S.lib(), queries(n_heads=heads)
+    ch, ca = chunk(batch=batch, n_tokens=0, max_new=1), cache(n_heads=heads)
+    assert L.smallkv_chunk_scores(C.byref(ch), C.byref(ca), C.byref(q), heads, None, 0x1000, 128, 1 << 40,
+                                  None) == S.EUNSUPPORTED
+    assert try_attn(ch, ca, q) == S.EUNSUPPORTED
+    a = append(n_q_heads=heads)
+    assert L.smallkv_append(C.byref(ch), C.byref(ca), C.byref(a), None) == S.EUNSUPPORTED
