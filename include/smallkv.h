@@ -551,7 +551,7 @@ typedef enum {
 /* freq[0 .. rot_dim/2 - 1] (HOST memory) and the amplitude (NULL: not wanted).
  * low, high and orig_len are read by RAMP and BANDS only (0 < low < high,
  * orig_len >= 1).  SMALLKV_EINVAL for an odd rot_dim or one below 2, base <= 1,
- * factor < 1 or an unknown scaling.  Host only. */
+ * factor < 1, a changed base that overflows or an unknown scaling.  Host only. */
 int smallkv_rope_freqs(int32_t rot_dim, double base, int32_t scaling, double factor, double low,
                        double high, int32_t orig_len, double *freq, float *amplitude);
 

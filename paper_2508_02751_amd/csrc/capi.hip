@@ -585,6 +585,7 @@ int smallkv_rope_freqs(int32_t rot_dim, double base, int32_t scaling, double fac
   if ((ramp || bands) && (!(low > 0.0) || !(high > low) || !isfinite(high) || orig_len < 1)) return SMALLKV_EINVAL;
   constexpr double kTwoPi = 6.283185307179586476925;
   if (scaling == SMALLKV_ROPE_BASE && rot_dim > 2) base *= pow(factor, rot_dim / (rot_dim - 2.0));
+  if (!isfinite(base)) return SMALLKV_EINVAL;
   // the pair that turns `turns` times over orig_len positions
   auto pair = [&](double turns) { return rot_dim * log(orig_len / (turns * kTwoPi)) / (2.0 * log(base)); };
   const double from = ramp ? fmax(floor(pair(high)), 0.0) : 0.0;

@@ -18,3 +18,9 @@ def test_a_launch_counts_fewer_than_2_to_the_24_workgroups(batch, heads):
     assert try_attn(ch, ca, q) == S.EUNSUPPORTED
     a = append(n_q_heads=heads)
     assert L.smallkv_append(C.byref(ch), C.byref(ca), C.byref(a), None) == S.EUNSUPPORTED
+
+
+def test_a_base_that_overflows_is_refused():
+    with pytest.raises(S.SmallKVError) as e:
+        S.rope_freqs(64, 1e200, S.ROPE_BASE, 1e150, device="cpu")
+    assert e.value.status == S.EINVAL
