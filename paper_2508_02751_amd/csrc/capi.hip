@@ -594,7 +594,8 @@ int smallkv_rope_freqs(int32_t rot_dim, double base, int32_t scaling, double fac
     const double f = pow(base, -2.0 * j / rot_dim);
     double slow = 0.0;  // the share of f / factor
     if (scaling == SMALLKV_ROPE_LINEAR) slow = 1.0;
-    if (ramp) slow = fmin(fmax((j - from) / fmax(to - from, 1e-3), 0.0), 1.0);
+    // (to < 0: every pair turns fewer than `low` times)
+    if (ramp) slow = to < 0.0 ? 1.0 : fmin(fmax((j - from) / fmax(to - from, 1e-3), 0.0), 1.0);
     if (bands) slow = 1.0 - fmin(fmax((orig_len * f / kTwoPi - low) / (high - low), 0.0), 1.0);
     freq[j] = f / factor * slow + f * (1.0 - slow);
   }

@@ -20,6 +20,17 @@ def test_a_launch_counts_fewer_than_2_to_the_24_workgroups(batch, heads):
     assert L.smallkv_append(C.byref(ch), C.byref(ca), C.byref(a), None) == S.EUNSUPPORTED
 
 
+def test_a_ramp_over_slow_pairs_only():
+    """A length over which no pair turns `low` times: all of them are slow, the first too."""
+    plain, _ = S.rope_freqs(64, 10000.0, device="cpu")
+    f, _ = S.rope_freqs(64, 10000.0, S.ROPE_RAMP, 4.0, low=1.0, high=32.0, orig_len=1, device="cpu")
+    assert (plain / f).tolist() == [4.0] * 32
+    # and as few as none are slow where all turn `high` times
+    f, _ = S.rope_freqs(64, 1.001, S.ROPE_RAMP, 4.0, low=1.0, high=32.0, orig_len=8192, device="cpu")
+    plain, _ = S.rope_freqs(64, 1.001, device="cpu")
+    assert (plain / f).tolist() == [1.0] * 32
+
+
 def test_a_base_that_overflows_is_refused():
     with pytest.raises(S.SmallKVError) as e:
         S.rope_freqs(64, 1e200, S.ROPE_BASE, 1e150, device="cpu")
