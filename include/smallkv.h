@@ -518,7 +518,8 @@ typedef struct {
   float scale;       /* softmax scale, > 0, at most 1e38 */
   const void *q;
   int64_t token_stride, head_stride;
-  void *out;         /* smallkv_chunk_attn: the output, laid out by its own strides */
+  void *out;         /* smallkv_chunk_attn: the output, laid out by its own strides; it
+                        must not overlap q */
   int64_t out_token_stride, out_head_stride;
   float *lse;        /* [n_tokens][n_heads] ln of the sum of exp(logit): written by
                         smallkv_chunk_attn (NULL: not), read by smallkv_chunk_scores */
