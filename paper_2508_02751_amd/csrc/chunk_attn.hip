@@ -14,14 +14,16 @@
 // accumulate in fp32; fp32 models multiply in fp32.  A bf16 model's P for the second
 // product:
 //   few rows  -- in two bf16 parts, a product each, 2^-16 relative: the rows of K and V
-//                bound the pass, not the products (a token each of 64 sequences 64.4 us
-//                with two parts, 64.5 with one);
+//                bound the pass, not the products (a token each of 64 sequences 62.8 us
+//                with two parts, 62.4 with one; heads of 64 19.4 and 19.1);
 //   many rows -- in one, each weight off by up to 2^-8 of itself, as much as the output's
 //                own rounding: the products bound the pass (4096 tokens over 32768
-//                rows 4.60 ms; with two parts 5.82).  The sum of the rounded P divides the
-//                output, so that the weights add up to 1 and a row's error is at most
-//                2^-8 sum w |v - out|: none where one row has all the weight or where values
-//                agree.  (With the sum of the unrounded P, which the lse takes: 4.47 ms.)
+//                rows 4.45 ms, with two parts 5.75; heads of 64 1.10 and 1.43).  The sum
+//                of the rounded P divides the output, so that the weights add up to 1 and a
+//                row's error is at most 2^-8 sum w |v - out|: none where one row has all the
+//                weight or where values agree.  (Divided by the sum of the unrounded P, which
+//                the lse takes: 4.33 and 1.04 ms.  The sum by a matrix product with ones in
+//                place of the two-element dot products: 4.54 and 1.13.)
 //
 // Two forms:
 //   many rows -- NW waves of 32 rows each share every tile of rows in LDS;
@@ -35,17 +37,18 @@
 // device from the sequences' own lengths, as the shortest with which the spans of
 // all sequences still run at once: spans of equal length whatever the mixture.
 //
-// Measured (MI355X), and what bounds it:
-//   2 x 4096 tokens over 32768 rows, 32 query and 8 kv heads of 128, bf16: 4.5 - 4.6 ms,
-//     900 TFLOP/s (a bf16 product of 8192^3 by the library: 1218).  Without any softmax
-//     the same loops take 3.8 ms: the matrix cores at the clock that power leaves.
-//     Heads of 64 (4 x 4096 tokens over 16384 rows, 14 heads): 1.24 ms, 680 TFLOP/s, half as
-//     many products per exponential.
+// Measured (MI355X, after a hundred calls, when the clock has settled), and what bounds it:
+//   2 x 4096 tokens over 32768 rows, 32 query and 8 kv heads of 128, bf16: 4.45 - 4.55 ms,
+//     920 TFLOP/s (a bf16 product of 8192^3 by the library: 1218).  The matrix cores are
+//     busy 43% and the vector units 48% of the cycles, mostly one after the other, at the
+//     1.9 GHz that power leaves; without any softmax the same loops take 3.8 ms.
+//     Heads of 64 (4 x 4096 tokens over 16384 rows, 14 heads): 1.10 ms, 765 TFLOP/s, half as
+//     many products per exponential (34% and 68%).
 //   a token each of 64 sequences of 1024 - 4096 rows, 28 and 4 heads of 128: 63 us for
 //     336 MB of keys and values, 5.3 TB/s, + 5 us to join two spans each: memory.
 //   one token over 32768 rows of 4 kv heads: 17 + 8 us, 67 MB: latency and two launches.
-//   a 4096-token prompt in fp32, 32 and 8 heads of 128: 1.31 ms, 105 TFLOP/s of 153; the
-//     matrix cores are busy 75% of the time.
+//   a 4096-token prompt in fp32, 32 and 8 heads of 128: 1.17 ms, 118 TFLOP/s of 153; the
+//     matrix cores are busy 75% of the cycles.
 #include <algorithm>
 
 #include "cache.h"

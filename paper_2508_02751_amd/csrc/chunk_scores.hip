@@ -20,11 +20,15 @@
 //              one key's logits, and each wave streams its keys' rows, bound by
 //              reading K once.
 //
-// Measured (MI355X): 2048 tokens of 32 query heads of 64 over 16384 rows, bf16 (1.0e9
-// exponentials, 129 GFLOP) 190 us, the vector units busy 81% of the time; 4096 tokens of
-// 32 heads of 128, 96 us, 720 TFLOP/s, fp32 672 us, 102 TFLOP/s.  A token each of 64
-// sequences of 1024 - 4096 rows of 4 kv heads of 128 (168 MB) 41 us, 4.1 TB/s; of 16
-// sequences over 82552 rows of 2 kv heads of 64 (23 MB) 9.1 us: latency.
+// Measured (MI355X, after a hundred calls, when the clock has settled: the first tens of
+// calls, of which the pairs of figures at the rules below are, take up to 15% more): 2048
+// tokens of 32 query heads of 64 over 16384 rows, bf16 (1.0e9 exponentials, 129 GFLOP)
+// 192 us, the vector units busy 78% of the cycles; 4096 tokens of 32 heads of 128, 93 us,
+// 740 TFLOP/s, fp32 596 us, 115 TFLOP/s, the matrix cores busy 74%.  Per kv head, 2048 tokens
+// of 14 heads over 8192 rows of 2 kv heads of 64, 74 us (SPLIT): latency, the vector units
+// busy 42%, the matrix cores 13%.  A token each of 64 sequences of 1024 - 4096 rows of 4 kv
+// heads of 128 (168 MB) 41 us, 4.1 TB/s; of 16 sequences over 82552 rows of 2 kv heads of
+// 64 (23 MB) 9.0 us: latency.
 #include <algorithm>
 #include <type_traits>
 
