@@ -648,6 +648,77 @@ typedef struct {
 int smallkv_evict(const smallkv_evict_t *evict, void *ws, size_t ws_bytes, void *stream);
 int smallkv_evict_workspace_size(const smallkv_evict_t *evict, size_t *bytes);
 
+/* ---------------------------------------------------------------------------
+ * Packed caches: the same rows in 8 or 4 bits an element, with a power of two for
+ * every block of 32 elements of a row (the microscaling formats of the Open Compute
+ * Project).  What a row stands for is exact in bf16 and fp32, so every call below
+ * computes what its plain counterpart computes on the rows that smallkv_read_packed
+ * gives.  Chunks, queries, positions, scores and every rule on absent rows, clamped
+ * lengths, empty chunks, refused sizes and workspaces are those of the calls above. */
+typedef enum {
+  SMALLKV_MXFP8 = 0, /* a byte an element: sign, 4 exponent bits (bias 7), 3 mantissa bits;
+                        up to 448, in steps of 2^-9 below 2^-6; 0x7f and 0xff are NaN */
+  SMALLKV_MXFP4 = 1  /* 4 bits, element 2i in the low half of byte i: sign, 2 exponent bits
+                        (bias 1), 1 mantissa bit: 0, 0.5, 1, 1.5, 2, 3, 4, 6 */
+} smallkv_packed_format_t;
+
+/* Row r of sequence b and kv head h: codes at k + page * page_stride + h * head_stride +
+ * (r % page_rows) * row_stride BYTES, head_dim or head_dim / 2 of them, and a scale byte x,
+ * 2^(x - 127) (255: every element of the block is NaN), for each of its head_dim / 32
+ * blocks at k_scale + page * scale_page_stride + h * scale_head_stride + (r % page_rows) *
+ * scale_row_stride (v alike).  Codes and their strides are multiples of 16 bytes, scales and
+ * theirs of head_dim / 32.  The other fields as in smallkv_cache_t; dtype is that of the
+ * queries, of the rows to append and of the outputs. */
+typedef struct {
+  void *k, *v;
+  uint8_t *k_scale, *v_scale;
+  int32_t format;           /* smallkv_packed_format_t */
+  int32_t dtype, head_dim;  /* smallkv_dtype_t; 64 or 128 */
+  int32_t n_heads, page_rows, n_pages, table_width;
+  int64_t page_stride, head_stride, row_stride;                   /* in bytes, >= 0 */
+  int64_t scale_page_stride, scale_head_stride, scale_row_stride; /* in bytes, >= 0 */
+  const int32_t *page_table;
+} smallkv_packed_t;
+
+/* smallkv_append into a packed cache.  A block of 32 elements x (keys: turned, in 64 bits,
+ * angle = position * freq[j] rounded to 64 bits, and not rounded before) becomes the scale
+ * 2^e, e the smallest integer >= -100 with max |x| <= 464 * 2^e (MXFP4: 7 * 2^e), at most
+ * 119 (125), and the elements nearest to x / 2^e, ties to even codes, magnitudes past
+ * the largest one to it: within half a step of the element's binade, or, below 2^(e - 6)
+ * (2^e), within 2^(e - 10) (2^(e - 2)).  A block with an infinite or NaN element becomes
+ * NaN as a whole (scale 255, codes 0).  q_out and row_pos as in smallkv_append. */
+int smallkv_append_packed(const smallkv_chunk_t *chunk, const smallkv_packed_t *cache,
+                          const smallkv_append_t *append, void *stream);
+
+/* Rows begin[b] (NULL: 0; clamped to [0, len]) .. len[b] - 1 of every sequence and head, read
+ * back into the same rows of `to`: bf16 or fp32 of either cache's dtype, the same head_dim and
+ * n_heads, paged or dense in its own way.  Nothing else of `to` is written, nor are rows
+ * that are absent in either cache or lie past to's.  SMALLKV_EUNSUPPORTED for batch * n_heads
+ * from 2^22.  `to` does not overlap `from`. */
+int smallkv_read_packed(const smallkv_packed_t *from, const smallkv_cache_t *to, int32_t batch,
+                        int32_t max_len, const int32_t *begin, const int32_t *len, void *stream);
+
+/* smallkv_chunk_attn over a packed cache.  bf16 models: the probabilities keep 16 bits in the
+ * product with V with max_new tokens of at most 32 (token, query head) rows per kv head,
+ * else 8, as there. */
+int smallkv_chunk_attn_packed(const smallkv_chunk_t *chunk, const smallkv_packed_t *cache,
+                              const smallkv_queries_t *queries, void *ws, size_t ws_bytes, void *stream);
+int smallkv_chunk_attn_packed_workspace_size(const smallkv_chunk_t *chunk, const smallkv_packed_t *cache,
+                                             const smallkv_queries_t *queries, size_t *bytes);
+
+/* smallkv_chunk_scores over a packed cache. */
+int smallkv_chunk_scores_packed(const smallkv_chunk_t *chunk, const smallkv_packed_t *cache,
+                                const smallkv_queries_t *queries, int32_t n_score_heads,
+                                const float *before, float *out, int64_t score_rows,
+                                int64_t seq_stride, void *stream);
+
+/* smallkv_evict of a packed cache: evict->from and evict->to are not read; `from` and `to` (of
+ * one format) take their places.  Rows are copied as they are. */
+int smallkv_evict_packed(const smallkv_evict_t *evict, const smallkv_packed_t *from,
+                         const smallkv_packed_t *to, void *ws, size_t ws_bytes, void *stream);
+int smallkv_evict_packed_workspace_size(const smallkv_evict_t *evict, const smallkv_packed_t *from,
+                                        const smallkv_packed_t *to, size_t *bytes);
+
 /* A static string for a status code. */
 const char *smallkv_status_string(int status);
 

@@ -7,6 +7,7 @@
 #include <mutex>
 
 #include "launch.h"
+#include "packed.h"
 #include "smallkv.h"
 
 using namespace smallkv;
@@ -230,7 +231,9 @@ int check_chunk(const smallkv_chunk_t *c, const smallkv_cache_t *kv) {
   return SMALLKV_OK;
 }
 
-int check_queries(const smallkv_chunk_t *c, const smallkv_cache_t *kv, const smallkv_queries_t *q) {
+// packed: the packed cache whose codes kv describes, or null.
+int check_queries(const smallkv_chunk_t *c, const smallkv_cache_t *kv, const smallkv_queries_t *q,
+                  const smallkv_packed_t *packed = nullptr) {
   const int rc = check_chunk(c, kv);
   if (rc) return rc;
   if (!q || (!q->q && c->n_tokens > 0) || q->n_heads < 1 || q->n_heads % kv->n_heads) return SMALLKV_EINVAL;
@@ -242,12 +245,14 @@ int check_queries(const smallkv_chunk_t *c, const smallkv_cache_t *kv, const sma
   // rows (token, query head of a group) and tiles of 32 of them are counted in 32 bits
   const int64_t rows = (int64_t)c->max_new * (q->n_heads / kv->n_heads);
   if (rows > (1 << 30) || (rows + 31) / 32 * c->batch * kv->n_heads > (1 << 30)) return SMALLKV_EUNSUPPORTED;
-  if ((int64_t)plan_chunk_attn(*c, *kv, *q).units * kv->n_heads > kMaxGroups) return SMALLKV_EUNSUPPORTED;
+  const AttnPlan p = packed ? plan_packed_attn(*c, *packed, *q) : plan_chunk_attn(*c, *kv, *q);
+  if ((int64_t)p.units * kv->n_heads > kMaxGroups) return SMALLKV_EUNSUPPORTED;
   return SMALLKV_OK;
 }
 
-int check_attn(const smallkv_chunk_t *c, const smallkv_cache_t *kv, const smallkv_queries_t *q) {
-  const int rc = check_queries(c, kv, q);
+int check_attn(const smallkv_chunk_t *c, const smallkv_cache_t *kv, const smallkv_queries_t *q,
+               const smallkv_packed_t *packed = nullptr) {
+  const int rc = check_queries(c, kv, q, packed);
   if (rc) return rc;
   if ((!q->out && c->n_tokens > 0) || !aligned16(q->out) || !stride_ok(q->out_token_stride, kv->dtype) ||
       !stride_ok(q->out_head_stride, kv->dtype))
@@ -258,13 +263,14 @@ int check_attn(const smallkv_chunk_t *c, const smallkv_cache_t *kv, const smallk
   return SMALLKV_OK;
 }
 
-int check_append(const smallkv_chunk_t *c, const smallkv_cache_t *kv, const smallkv_append_t *a) {
+// `packed`: kv describes a packed cache's codes.
+int check_append(const smallkv_chunk_t *c, const smallkv_cache_t *kv, const smallkv_append_t *a, bool packed = false) {
   const int rc = check_chunk(c, kv);
   if (rc) return rc;
   if (!a || a->n_q_heads < 1) return SMALLKV_EINVAL;
   if (c->n_tokens > 0 && (!a->q || !a->k || !a->v || !a->q_out)) return SMALLKV_EINVAL;
   if (a->n_q_heads % kv->n_heads) return SMALLKV_EINVAL;
-  if (!writable(*kv)) return SMALLKV_EINVAL;
+  if (!packed && !writable(*kv)) return SMALLKV_EINVAL;
   if ((c->n_tokens > 1 && a->q_out_token_stride < kv->head_dim) ||
       (a->n_q_heads > 1 && a->q_out_head_stride < kv->head_dim))
     return SMALLKV_EINVAL;
@@ -289,7 +295,7 @@ int check_append(const smallkv_chunk_t *c, const smallkv_cache_t *kv, const smal
   return SMALLKV_OK;
 }
 
-int check_evict(const smallkv_evict_t *e) {
+int check_evict(const smallkv_evict_t *e, bool packed = false) {
   if (!e || e->batch < 1 || e->max_len < 1 || e->sinks < 0 || e->out_rows < 1) return SMALLKV_EINVAL;
   if (!e->len || !e->keep || !e->scores || !e->out_pos || !e->held) return SMALLKV_EINVAL;
   int rc = check_cache(&e->from, e->batch);
@@ -297,13 +303,100 @@ int check_evict(const smallkv_evict_t *e) {
   if ((rc = check_cache(&e->to, e->batch))) return rc;
   if (e->from.dtype != e->to.dtype || e->from.head_dim != e->to.head_dim || e->from.n_heads != e->to.n_heads)
     return SMALLKV_EINVAL;
-  if (!writable(e->to)) return SMALLKV_EINVAL;
+  if (!packed && !writable(e->to)) return SMALLKV_EINVAL;
   if (e->from.k == e->to.k || e->from.v == e->to.v) return SMALLKV_EINVAL;
   if (e->out_pos == e->row_pos || e->out_scores == e->scores) return SMALLKV_EINVAL;
   if (e->n_score_heads < 1 || e->n_score_heads % e->from.n_heads) return SMALLKV_EINVAL;
   if (e->score_rows < e->max_len || (e->row_pos && e->pos_rows < e->max_len)) return SMALLKV_EINVAL;
   if (e->n_score_heads / e->from.n_heads > 64 || e->max_len > (1 << 20) ||
       (int64_t)e->batch * e->from.n_heads > kMaxGroups / 4)
+    return SMALLKV_EUNSUPPORTED;
+  return SMALLKV_OK;
+}
+
+// A packed cache; *codes: its codes as a cache, with whose checks the rest is shared.
+int check_packed(const smallkv_packed_t *p, smallkv_cache_t *codes) {
+  if (!p || !p->k_scale || !p->v_scale) return SMALLKV_EINVAL;
+  if (p->format != SMALLKV_MXFP8 && p->format != SMALLKV_MXFP4) return SMALLKV_EINVAL;
+  const int64_t strides[] = {p->page_stride, p->head_stride, p->row_stride};
+  for (const int64_t s : strides)
+    if (s < 0 || s % 16) return SMALLKV_EINVAL;
+  if (p->head_dim != 64 && p->head_dim != 128) return SMALLKV_EUNSUPPORTED;
+  const int64_t w = p->head_dim / kBlock;
+  if (reinterpret_cast<uintptr_t>(p->k_scale) % w || reinterpret_cast<uintptr_t>(p->v_scale) % w)
+    return SMALLKV_EINVAL;
+  const int64_t scales[] = {p->scale_page_stride, p->scale_head_stride, p->scale_row_stride};
+  for (const int64_t s : scales) {
+    if (s < 0 || s % w) return SMALLKV_EINVAL;
+    if (s / w > UINT32_MAX) return SMALLKV_EUNSUPPORTED;
+  }
+  *codes = codes_of(*p);
+  return SMALLKV_OK;
+}
+
+// Rows that are written: no broadcast strides, of codes or scales.
+bool writable(const smallkv_packed_t &p) {
+  const int64_t row = p.head_dim * format_bits(p) / 8, w = p.head_dim / kBlock;
+  return (p.page_rows == 1 || (p.row_stride >= row && p.scale_row_stride >= w)) &&
+         (p.n_heads == 1 || (p.head_stride >= row && p.scale_head_stride >= w)) &&
+         (p.n_pages == 1 || (p.page_stride >= row && p.scale_page_stride >= w));
+}
+
+int check_append_packed(const smallkv_chunk_t *c, const smallkv_packed_t *kv, const smallkv_append_t *a) {
+  smallkv_cache_t codes;
+  int rc = check_packed(kv, &codes);
+  if (rc) return rc;
+  if ((rc = check_append(c, &codes, a, true))) return rc;
+  return writable(*kv) ? SMALLKV_OK : SMALLKV_EINVAL;
+}
+
+int check_attn_packed(const smallkv_chunk_t *c, const smallkv_packed_t *kv, const smallkv_queries_t *q) {
+  smallkv_cache_t codes;
+  const int rc = check_packed(kv, &codes);
+  return rc ? rc : check_attn(c, &codes, q, kv);
+}
+
+// *e: the eviction with the codes of `from` and `to` in their places.
+int check_evict_packed(const smallkv_evict_t *evict, const smallkv_packed_t *from, const smallkv_packed_t *to,
+                       smallkv_evict_t *e) {
+  if (!evict) return SMALLKV_EINVAL;
+  *e = *evict;
+  int rc = check_packed(from, &e->from);
+  if (rc) return rc;
+  if ((rc = check_packed(to, &e->to))) return rc;
+  if ((rc = check_evict(e, true))) return rc;
+  if (from->format != to->format || !writable(*to)) return SMALLKV_EINVAL;
+  if (from->k_scale == to->k_scale || from->v_scale == to->v_scale) return SMALLKV_EINVAL;
+  return SMALLKV_OK;
+}
+
+int check_read_packed(const smallkv_packed_t *from, const smallkv_cache_t *to, int batch, int max_len,
+                      const int32_t *len) {
+  if (batch < 1 || max_len < 1 || !len) return SMALLKV_EINVAL;
+  smallkv_cache_t codes;
+  int rc = check_packed(from, &codes);
+  if (rc) return rc;
+  if ((rc = check_cache(&codes, batch))) return rc;
+  if ((rc = check_cache(to, batch))) return rc;
+  if (codes.head_dim != to->head_dim || codes.n_heads != to->n_heads || !writable(*to)) return SMALLKV_EINVAL;
+  if (from->k == to->k || from->v == to->v) return SMALLKV_EINVAL;
+  // (32 workgroups a pair of a sequence and a head, for K and V)
+  if (max_len > (1 << 30) || (int64_t)batch * to->n_heads > kMaxGroups / 4) return SMALLKV_EUNSUPPORTED;
+  return SMALLKV_OK;
+}
+
+// The scores call's own arguments.
+int check_scores(const smallkv_chunk_t *chunk, const smallkv_cache_t *cache, const smallkv_queries_t *queries,
+                 int32_t n_score_heads, const float *out, int64_t score_rows, int64_t seq_stride,
+                 const smallkv_packed_t *packed = nullptr) {
+  const int rc = check_queries(chunk, cache, queries, packed);
+  if (rc) return rc;
+  if ((!queries->lse && chunk->n_tokens > 0) || !out || score_rows < chunk->max_len) return SMALLKV_EINVAL;
+  if (n_score_heads != queries->n_heads && n_score_heads != cache->n_heads) return SMALLKV_EINVAL;
+  if (score_rows > INT32_MAX || seq_stride < n_score_heads * score_rows) return SMALLKV_EINVAL;
+  // (a decode step's keys are cut into as many pieces as run at once)
+  if ((int64_t)chunk->max_new * (queries->n_heads / cache->n_heads) > 32 &&
+      ((int64_t)chunk->max_len + 127) / 128 * chunk->batch * n_score_heads > kMaxGroups)
     return SMALLKV_EUNSUPPORTED;
   return SMALLKV_OK;
 }
@@ -632,15 +725,8 @@ int smallkv_chunk_attn(const smallkv_chunk_t *chunk, const smallkv_cache_t *cach
 int smallkv_chunk_scores(const smallkv_chunk_t *chunk, const smallkv_cache_t *cache,
                          const smallkv_queries_t *queries, int32_t n_score_heads, const float *before,
                          float *out, int64_t score_rows, int64_t seq_stride, void *stream) {
-  const int rc = check_queries(chunk, cache, queries);
+  const int rc = check_scores(chunk, cache, queries, n_score_heads, out, score_rows, seq_stride);
   if (rc) return rc;
-  if ((!queries->lse && chunk->n_tokens > 0) || !out || score_rows < chunk->max_len) return SMALLKV_EINVAL;
-  if (n_score_heads != queries->n_heads && n_score_heads != cache->n_heads) return SMALLKV_EINVAL;
-  if (score_rows > INT32_MAX || seq_stride < n_score_heads * score_rows) return SMALLKV_EINVAL;
-  // (a decode step's keys are cut into as many pieces as run at once)
-  if ((int64_t)chunk->max_new * (queries->n_heads / cache->n_heads) > 32 &&
-      ((int64_t)chunk->max_len + 127) / 128 * chunk->batch * n_score_heads > kMaxGroups)
-    return SMALLKV_EUNSUPPORTED;
   return status_of(launch_chunk_scores(*chunk, *cache, *queries, n_score_heads, before, out, score_rows,
                                        seq_stride, static_cast<hipStream_t>(stream)));
 }
@@ -659,6 +745,70 @@ int smallkv_evict(const smallkv_evict_t *evict, void *ws, size_t ws_bytes, void 
   if (!ws || ws_bytes < evict_workspace(*evict)) return SMALLKV_EWORKSPACE;
   if (!aligned16(ws)) return SMALLKV_EINVAL;
   return status_of(launch_evict(*evict, ws, static_cast<hipStream_t>(stream)));
+}
+
+int smallkv_append_packed(const smallkv_chunk_t *chunk, const smallkv_packed_t *cache, const smallkv_append_t *append,
+                          void *stream) {
+  const int rc = check_append_packed(chunk, cache, append);
+  if (rc) return rc;
+  return status_of(launch_append_packed(*chunk, *cache, *append, static_cast<hipStream_t>(stream)));
+}
+
+int smallkv_read_packed(const smallkv_packed_t *from, const smallkv_cache_t *to, int32_t batch, int32_t max_len,
+                        const int32_t *begin, const int32_t *len, void *stream) {
+  const int rc = check_read_packed(from, to, batch, max_len, len);
+  if (rc) return rc;
+  return status_of(launch_read_packed(*from, *to, batch, max_len, begin, len, static_cast<hipStream_t>(stream)));
+}
+
+int smallkv_chunk_attn_packed_workspace_size(const smallkv_chunk_t *chunk, const smallkv_packed_t *cache,
+                                             const smallkv_queries_t *queries, size_t *bytes) {
+  if (!bytes) return SMALLKV_EINVAL;
+  const int rc = check_attn_packed(chunk, cache, queries);
+  if (rc) return rc;
+  *bytes = plan_packed_attn(*chunk, *cache, *queries).ws_bytes;
+  return SMALLKV_OK;
+}
+
+int smallkv_chunk_attn_packed(const smallkv_chunk_t *chunk, const smallkv_packed_t *cache,
+                              const smallkv_queries_t *queries, void *ws, size_t ws_bytes, void *stream) {
+  const int rc = check_attn_packed(chunk, cache, queries);
+  if (rc) return rc;
+  const AttnPlan p = plan_packed_attn(*chunk, *cache, *queries);
+  if (p.ws_bytes && (!ws || ws_bytes < p.ws_bytes)) return SMALLKV_EWORKSPACE;
+  if (p.ws_bytes && !aligned16(ws)) return SMALLKV_EINVAL;
+  return status_of(launch_packed_attn(*chunk, *cache, *queries, p, ws, static_cast<hipStream_t>(stream)));
+}
+
+int smallkv_chunk_scores_packed(const smallkv_chunk_t *chunk, const smallkv_packed_t *cache,
+                                const smallkv_queries_t *queries, int32_t n_score_heads, const float *before,
+                                float *out, int64_t score_rows, int64_t seq_stride, void *stream) {
+  smallkv_cache_t codes;
+  int rc = check_packed(cache, &codes);
+  if (rc) return rc;
+  if ((rc = check_scores(chunk, &codes, queries, n_score_heads, out, score_rows, seq_stride, cache))) return rc;
+  return status_of(launch_packed_scores(*chunk, *cache, *queries, n_score_heads, before, out, score_rows, seq_stride,
+                                        static_cast<hipStream_t>(stream)));
+}
+
+int smallkv_evict_packed_workspace_size(const smallkv_evict_t *evict, const smallkv_packed_t *from,
+                                        const smallkv_packed_t *to, size_t *bytes) {
+  if (!bytes) return SMALLKV_EINVAL;
+  smallkv_evict_t e;
+  const int rc = check_evict_packed(evict, from, to, &e);
+  if (rc) return rc;
+  *bytes = evict_workspace(e);
+  return SMALLKV_OK;
+}
+
+int smallkv_evict_packed(const smallkv_evict_t *evict, const smallkv_packed_t *from, const smallkv_packed_t *to,
+                         void *ws, size_t ws_bytes, void *stream) {
+  smallkv_evict_t e;
+  const int rc = check_evict_packed(evict, from, to, &e);
+  if (rc) return rc;
+  if (!ws || ws_bytes < evict_workspace(e)) return SMALLKV_EWORKSPACE;
+  if (!aligned16(ws)) return SMALLKV_EINVAL;
+  return status_of(launch_evict_packed(e, *from, *to, ws, static_cast<hipStream_t>(stream)));
 }
 
 int smallkv_step(const smallkv_step_t *s, void *ws, size_t ws_bytes, void *stream) {

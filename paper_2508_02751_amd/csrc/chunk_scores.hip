@@ -32,8 +32,8 @@
 #include <algorithm>
 #include <type_traits>
 
-#include "cache.h"
 #include "launch.h"
+#include "packed.h"
 
 namespace smallkv {
 namespace {
@@ -42,7 +42,8 @@ __device__ __align__(16) unsigned char zero_row[512];
 
 struct ScoreArgs {
   ChunkView c;
-  CacheView kv;
+  CacheView kv;  // a packed cache's codes
+  ScaleView sc;  // and their scales
   int hq, hkv, g, per_kv;
   const unsigned char *q;
   int64_t q_token, q_head;  // in bytes
@@ -71,6 +72,47 @@ template <typename T> __device__ __forceinline__ float weight_of(const ScoreArgs
   return __builtin_amdgcn_exp2f(sizeof(T) == 4 ? t * kLog2e : t);
 }
 
+// A lane's half of the key row of its column, as operands of the products: pieces of 16 bytes
+// of T.  Which half: of a plain row every other piece (bf16) or half of the dimensions
+// (fp32); of a packed one half of the dimensions.
+template <typename T, int D, int F> struct KeyHalf {
+  static constexpr int kPieces = sizeof(T) == 2 ? D / 16 : D / 8;
+  static constexpr int kWords = F ? D * F / 64 : 1;  // of codes
+  // piece i of half h
+  __device__ __forceinline__ static int piece(int i, int h) {
+    return sizeof(T) == 2 && F == 0 ? 2 * i + h : h * kPieces + i;
+  }
+  uint4 k[F ? 1 : kPieces];
+  uint32_t w[kWords], scales;  // F: its codes, and its blocks' scales from the low byte on
+  // off: of the row, or -1; page: its page
+  __device__ __forceinline__ void load(const ScoreArgs &a, int64_t off, int page, int key, int kvh, int half) {
+    const unsigned char *row = off >= 0 ? a.kv.k + off + (((uint64_t)kvh * a.kv.head_stride) << 4) : zero_row;
+    if constexpr (F == 0) {
+#pragma unroll
+      for (int i = 0; i < kPieces; ++i) k[i] = reinterpret_cast<const uint4 *>(row)[piece(i, half)];
+    } else {
+      const uint8_t *s = off >= 0 ? a.sc.k + scale_offset<D>(a.sc, a.kv, page, key, kvh) : zero_row;
+#pragma unroll
+      for (int i = 0; i < kWords; i += 4) {
+        const uint4 x = reinterpret_cast<const uint4 *>(row)[half * kWords / 4 + i / 4];
+        w[i] = x.x;
+        w[i + 1] = x.y;
+        w[i + 2] = x.z;
+        w[i + 3] = x.w;
+      }
+      if (D == 128)
+        scales = reinterpret_cast<const uint16_t *>(s)[half];
+      else
+        scales = s[half];
+    }
+  }
+  __device__ __forceinline__ uint4 get(int i) const {
+    if constexpr (F == 0) return k[i];
+    constexpr int per = kBlock * (int)sizeof(T) / 16;  // pieces of a block
+    return unpack16<T, F>(w, i, scale_of(scales >> (i / per * 8) & 255u));
+  }
+};
+
 // Sums over ROWS (16 or 32) neighbouring lanes' query rows: each exchange halves the keys
 // that a lane holds.  The lane ends with key register (lane % ROWS) * 16 / ROWS.
 template <int ROWS> __device__ __forceinline__ float sum_rows(float (&acc)[16]) {
@@ -90,7 +132,7 @@ template <int ROWS> __device__ __forceinline__ float sum_rows(float (&acc)[16]) 
   return ROWS == 32 ? acc[0] + __shfl_xor(acc[0], 1, kWave) : acc[0];
 }
 
-template <typename T, int D, bool PER_KV, bool SPLIT>
+template <typename T, int D, int F, bool PER_KV, bool SPLIT>
 __global__ __launch_bounds__(kNW * kWave, SPLIT && sizeof(T) * D == 512 ? 1 : 2) void chunk_scores(ScoreArgs a) {
   using L = TileLayout<T, D>;
   constexpr bool kBf16 = sizeof(T) == 2;
@@ -113,15 +155,17 @@ __global__ __launch_bounds__(kNW * kWave, SPLIT && sizeof(T) * D == 512 ? 1 : 2)
   const int first = max(0, block0 - pos0);  // the first token that sees a key of the workgroup
   const int n_tokens = s.n_new - first, n_rows = n_tokens * g;
 
+  using Key = KeyHalf<T, D, F>;
   uint4 kf[kFrag];
   uint32_t exists;
   {
     const int key = key0 + (lane & 31);
-    const int64_t off = key < s.len ? row_offset(a.kv, b, key) : -1;
-    const unsigned char *row = off >= 0 ? a.kv.k + off + (((uint64_t)kvh * a.kv.head_stride) << 4) : zero_row;
+    const int page = key < s.len ? row_page(a.kv, b, key) : -1;
+    const int64_t off = page_offset(a.kv, page, key);
+    Key k;
+    k.load(a, off, page, key, kvh, half);
 #pragma unroll
-    for (int i = 0; i < kFrag; ++i)
-      kf[i] = reinterpret_cast<const uint4 *>(row)[kBf16 ? 2 * i + half : half * kFrag + i];
+    for (int i = 0; i < kFrag; ++i) kf[i] = k.get(i);
     exists = (uint32_t)__ballot(off >= 0);
   }
 
@@ -193,7 +237,7 @@ __global__ __launch_bounds__(kNW * kWave, SPLIT && sizeof(T) * D == 512 ? 1 : 2)
       f32x16_t x = {};
 #pragma unroll
       for (int i = 0; i < kFrag; ++i) {
-        const int c = kBf16 ? 2 * i + half : half * kFrag + i;
+        const int c = Key::piece(i, half);
         const uint4 w = *reinterpret_cast<const uint4 *>(sq + (row * L::bytes + ((c ^ z) << 4)));
         if constexpr (kBf16) {
           x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, kf[i]),
@@ -249,7 +293,7 @@ __global__ __launch_bounds__(kNW * kWave, SPLIT && sizeof(T) * D == 512 ? 1 : 2)
 // between tiles would be waited for with the next tile's copies).
 constexpr int kWalk = 4;
 
-template <typename T, int D, int P>
+template <typename T, int D, int F, int P>
 __global__ __launch_bounds__(kNW * kWave, 2) void head_scores(ScoreArgs a) {
   using L = TileLayout<T, D>;
   constexpr bool kBf16 = sizeof(T) == 2;
@@ -272,15 +316,17 @@ __global__ __launch_bounds__(kNW * kWave, 2) void head_scores(ScoreArgs a) {
   const int first = max(0, block0 - pos0);  // the first token that sees a key of the workgroup
   const int n_tokens = s.n_new - first;
 
+  using Key = KeyHalf<T, D, F>;
   uint4 kf[kFrag];
   uint32_t exists;
   {
     const int key = key0 + (lane & 31);
-    const int64_t off = key < s.len ? row_offset(a.kv, b, key) : -1;
-    const unsigned char *row = off >= 0 ? a.kv.k + off + (((uint64_t)kvh * a.kv.head_stride) << 4) : zero_row;
+    const int page = key < s.len ? row_page(a.kv, b, key) : -1;
+    const int64_t off = page_offset(a.kv, page, key);
+    Key k;
+    k.load(a, off, page, key, kvh, half);
 #pragma unroll
-    for (int i = 0; i < kFrag; ++i)
-      kf[i] = reinterpret_cast<const uint4 *>(row)[kBf16 ? 2 * i + half : half * kFrag + i];
+    for (int i = 0; i < kFrag; ++i) kf[i] = k.get(i);
     exists = (uint32_t)__ballot(off >= 0);
   }
   // Row r of tile t of head group h: token 64 t + r % P of head h * kHeads + r / P; past
@@ -329,7 +375,7 @@ __global__ __launch_bounds__(kNW * kWave, 2) void head_scores(ScoreArgs a) {
         f32x16_t x = {};
 #pragma unroll
         for (int i = 0; i < kFrag; ++i) {
-          const int c = kBf16 ? 2 * i + half : half * kFrag + i;
+          const int c = Key::piece(i, half);
           const uint4 w = *reinterpret_cast<const uint4 *>(sq + (row * L::bytes + ((c ^ z) << 4)));
           if constexpr (kBf16) {
             x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, kf[i]),
@@ -392,7 +438,7 @@ __global__ __launch_bounds__(kNW * kWave, 2) void head_scores(ScoreArgs a) {
       a.out[at(n)] = old[n] + (n_tokens > 0 && exists >> in & 1u ? sums[n][threadIdx.x] : 0.0f);
 }
 
-template <typename T, int D>
+template <typename T, int D, int F>
 __global__ __launch_bounds__(kNW * kWave, 2) void few_scores(ScoreArgs a) {
   constexpr bool kBf16 = sizeof(T) == 2;
   constexpr int kFrag = kBf16 ? D / 16 : D / 8;  // 16-byte pieces of a row per lane
@@ -409,7 +455,7 @@ __global__ __launch_bounds__(kNW * kWave, 2) void few_scores(ScoreArgs a) {
   if (from >= s.len) return;
   const int begin = (int)from, end = min(begin + share, s.len);
   const int pos0 = s.len - s.n_new, rows = s.n_new * a.g;
-  const unsigned char *k = a.kv.k + (((uint64_t)kvh * a.kv.head_stride) << 4);
+  using Key = KeyHalf<T, D, F>;
   // keys are looked up two blocks ahead and their rows requested one ahead
   const int32_t *pages = a.kv.table ? a.kv.table + (int64_t)b * a.kv.width : a.c.len;
   auto page_of = [&](int key) { return pages[min(key, s.len - 1) >> a.kv.shift]; };  // (dense: any word)
@@ -432,7 +478,7 @@ __global__ __launch_bounds__(kNW * kWave, 2) void few_scores(ScoreArgs a) {
     const unsigned char *row = rows > 0 ? a.q + t * a.q_token + h * a.q_head : zero_row;
 #pragma unroll
     for (int i = 0; i < kFrag; ++i)
-      qf[i] = reinterpret_cast<const uint4 *>(row)[kBf16 ? 2 * i + half : half * kFrag + i];
+      qf[i] = reinterpret_cast<const uint4 *>(row)[Key::piece(i, half)];
   }
   float lse_x[16];
   int own[16];
@@ -450,23 +496,18 @@ __global__ __launch_bounds__(kNW * kWave, 2) void few_scores(ScoreArgs a) {
     }
   }
   int64_t off = offset_of(key, page);
-  uint4 kf[kFrag];
-  auto load = [&]() {
-    const unsigned char *row = off >= 0 ? k + off : zero_row;
-#pragma unroll
-    for (int i = 0; i < kFrag; ++i)
-      kf[i] = reinterpret_cast<const uint4 *>(row)[kBf16 ? 2 * i + half : half * kFrag + i];
-  };
-  load();
+  Key k;
+  auto load = [&](int at) { k.load(a, off, a.kv.table ? page : b, at, kvh, half); };
+  load(key);
   for (int base = begin + wave * 32; base < end; base += step, key += step) {
     f32x16_t x = {};
 #pragma unroll
     for (int i = 0; i < kFrag; ++i) {
       if constexpr (kBf16) {
         x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, qf[i]),
-                                                    __builtin_bit_cast(bf16x8_t, kf[i]), x, 0, 0, 0);
+                                                    __builtin_bit_cast(bf16x8_t, k.get(i)), x, 0, 0, 0);
       } else {
-        const f32x4_t qa = __builtin_bit_cast(f32x4_t, qf[i]), ka = __builtin_bit_cast(f32x4_t, kf[i]);
+        const f32x4_t qa = __builtin_bit_cast(f32x4_t, qf[i]), ka = __builtin_bit_cast(f32x4_t, k.get(i));
 #pragma unroll
         for (int e = 0; e < 4; ++e) x = __builtin_amdgcn_mfma_f32_32x32x2f32(qa[e], ka[e], x, 0, 0, 0);
       }
@@ -474,7 +515,7 @@ __global__ __launch_bounds__(kNW * kWave, 2) void few_scores(ScoreArgs a) {
     const bool exists = off >= 0, inside = key < end;
     page = page_next;
     off = offset_of(key + step, page);
-    load();
+    load(key + step);
     page_next = page_of(key + 2 * step);
     float p[16];
 #pragma unroll
@@ -513,11 +554,11 @@ __global__ __launch_bounds__(kNW * kWave, 2) void few_scores(ScoreArgs a) {
   }
 }
 
-template <typename T, int D, bool PER_KV, bool SPLIT> void launch_chunk(const ScoreArgs &a, dim3 grid, hipStream_t st) {
-  hipLaunchKernelGGL((chunk_scores<T, D, PER_KV, SPLIT>), grid, dim3(kNW * kWave), 0, st, a);
+template <typename T, int D, int F, bool PER_KV, bool SPLIT> void launch_chunk(const ScoreArgs &a, dim3 grid, hipStream_t st) {
+  hipLaunchKernelGGL((chunk_scores<T, D, F, PER_KV, SPLIT>), grid, dim3(kNW * kWave), 0, st, a);
 }
 
-template <typename T, int D>
+template <typename T, int D, int F>
 void launch_typed(ScoreArgs a, int max_new, int max_len, hipStream_t st) {
   const int64_t units = (int64_t)a.c.batch * a.hkv;
   const dim3 block(kNW * kWave);
@@ -528,7 +569,7 @@ void launch_typed(ScoreArgs a, int max_new, int max_len, hipStream_t st) {
     const int64_t rounds = ((int64_t)max_len + 127) / 128;
     const int64_t each = std::max<int64_t>(1, std::min<int64_t>(rounds, rounds * units / 512));
     a.pieces = (int)((rounds + each - 1) / each);
-    hipLaunchKernelGGL((few_scores<T, D>), dim3((unsigned)(a.pieces * units)), block, 0, st, a);
+    hipLaunchKernelGGL((few_scores<T, D, F>), dim3((unsigned)(a.pieces * units)), block, 0, st, a);
     return;
   }
   const unsigned heads = a.per_kv ? 1 : a.g;
@@ -542,7 +583,7 @@ void launch_typed(ScoreArgs a, int max_new, int max_len, hipStream_t st) {
     a.walk = std::min(tiles, kWalk);
     while (a.walk > 1 && pieces * ((tiles + a.walk - 1) / a.walk) < 1024) --a.walk;
     const dim3 grid((unsigned)(pieces * ((tiles + a.walk - 1) / a.walk)));
-    auto *kernel = packed == 4 ? head_scores<T, D, 16> : packed == 2 ? head_scores<T, D, 32> : head_scores<T, D, 64>;
+    auto *kernel = packed == 4 ? head_scores<T, D, F, 16> : packed == 2 ? head_scores<T, D, F, 32> : head_scores<T, D, F, 64>;
     hipLaunchKernelGGL(kernel, grid, block, 0, st, a);
     return;
   }
@@ -550,15 +591,20 @@ void launch_typed(ScoreArgs a, int max_new, int max_len, hipStream_t st) {
   // workgroups: 175 us, split 84; 512 tokens, four, 256 workgroups: 68, split 72)
   const bool split = blocks(32 * kNW) * (int64_t)heads < 256;
   const dim3 grid(blocks(split ? 32 : 32 * kNW) * heads);
-  (split ? a.per_kv ? launch_chunk<T, D, true, true> : launch_chunk<T, D, false, true>
-   : a.per_kv ? launch_chunk<T, D, true, false> : launch_chunk<T, D, false, false>)(a, grid, st);
+  (split ? a.per_kv ? launch_chunk<T, D, F, true, true> : launch_chunk<T, D, F, false, true>
+   : a.per_kv ? launch_chunk<T, D, F, true, false> : launch_chunk<T, D, F, false, false>)(a, grid, st);
 }
 
-}  // namespace
+template <int F> hipError_t launch_all(const ScoreArgs &a, bool f32, int d, int max_new, int max_len, hipStream_t st) {
+  if (f32)
+    (d == 64 ? launch_typed<float, 64, F> : launch_typed<float, 128, F>)(a, max_new, max_len, st);
+  else
+    (d == 64 ? launch_typed<bf16_t, 64, F> : launch_typed<bf16_t, 128, F>)(a, max_new, max_len, st);
+  return hipGetLastError();
+}
 
-hipError_t launch_chunk_scores(const smallkv_chunk_t &c, const smallkv_cache_t &kv, const smallkv_queries_t &q,
-                               int n_score_heads, const float *before, float *out, int64_t score_rows,
-                               int64_t seq_stride, hipStream_t st) {
+ScoreArgs score_args(const smallkv_chunk_t &c, const smallkv_cache_t &kv, const smallkv_queries_t &q,
+                     int n_score_heads, const float *before, float *out, int64_t score_rows, int64_t seq_stride) {
   const int e = kv.dtype == SMALLKV_F32 ? 4 : 2;
   ScoreArgs a{};
   a.c = chunk_view(c);
@@ -576,11 +622,25 @@ hipError_t launch_chunk_scores(const smallkv_chunk_t &c, const smallkv_cache_t &
   a.rows = score_rows;
   a.seq_stride = seq_stride;
   a.scale = e == 4 ? q.scale : q.scale * kLog2e;
-  if (kv.dtype == SMALLKV_F32)
-    (kv.head_dim == 64 ? launch_typed<float, 64> : launch_typed<float, 128>)(a, c.max_new, c.max_len, st);
-  else
-    (kv.head_dim == 64 ? launch_typed<bf16_t, 64> : launch_typed<bf16_t, 128>)(a, c.max_new, c.max_len, st);
-  return hipGetLastError();
+  return a;
+}
+
+}  // namespace
+
+hipError_t launch_chunk_scores(const smallkv_chunk_t &c, const smallkv_cache_t &kv, const smallkv_queries_t &q,
+                               int n_score_heads, const float *before, float *out, int64_t score_rows,
+                               int64_t seq_stride, hipStream_t st) {
+  const ScoreArgs a = score_args(c, kv, q, n_score_heads, before, out, score_rows, seq_stride);
+  return launch_all<0>(a, kv.dtype == SMALLKV_F32, kv.head_dim, c.max_new, c.max_len, st);
+}
+
+hipError_t launch_packed_scores(const smallkv_chunk_t &c, const smallkv_packed_t &kv, const smallkv_queries_t &q,
+                                int n_score_heads, const float *before, float *out, int64_t score_rows,
+                                int64_t seq_stride, hipStream_t st) {
+  ScoreArgs a = score_args(c, codes_of(kv), q, n_score_heads, before, out, score_rows, seq_stride);
+  a.sc = scale_view(kv);
+  return (format_bits(kv) == 8 ? launch_all<8> : launch_all<4>)(a, kv.dtype == SMALLKV_F32, kv.head_dim, c.max_new,
+                                                                 c.max_len, st);
 }
 
 }  // namespace smallkv

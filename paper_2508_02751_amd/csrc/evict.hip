@@ -7,7 +7,7 @@
 //                   passes, then the kept rows' numbers in ascending order, ties to
 //                   the lowest rows;
 //   evict_copy   -- the kept rows as a flat array of 16-byte pieces, K and V, and
-//                   their positions and scores.
+//                   their positions and scores (of a packed cache: and scales).
 //
 // Measured (MI355X): 4 sequences of 20000 - 32768 rows, 16 layers of 8 kv heads of 64,
 // 20% kept (1.4 GB read and written): 57 + 299 us, the copy at the rate of a large copy,
@@ -15,9 +15,10 @@
 // scores of 7 query heads added up: 12 + 17 us; one layer of 1237 rows: 6.4 + 2.8 us, two
 // launches and the selection's barriers.
 #include <algorithm>
+#include <type_traits>
 
-#include "cache.h"
 #include "launch.h"
+#include "packed.h"
 
 namespace smallkv {
 namespace {
@@ -29,6 +30,8 @@ struct EvictArgs {
   const int32_t *len, *keep, *recent;
   CacheView from, to;
   unsigned char *to_k, *to_v;
+  ScaleView from_s, to_s;  // of packed caches, else null
+  uint8_t *to_ks, *to_vs;
   int row_bytes;
   const float *scores;
   int64_t score_rows;
@@ -227,9 +230,21 @@ __global__ __launch_bounds__(NT, KPT <= 16 ? 8 : 4) void evict_select(EvictArgs 
   });
 }
 
+// The scales of a row, W bytes.
+template <int W> __device__ __forceinline__ void copy_scales(const EvictArgs &a, int b, int h, int row, int to) {
+  using S = std::conditional_t<W == 4, uint32_t, uint16_t>;
+  const int page = row_page(a.from, b, row), page_to = row_page(a.to, b, to);
+  if (page_offset(a.from, page, row) < 0 || page_offset(a.to, page_to, to) < 0) return;
+  const int64_t s = scale_offset<W * kBlock>(a.from_s, a.from, page, row, h);
+  const int64_t d = scale_offset<W * kBlock>(a.to_s, a.to, page_to, to, h);
+  *reinterpret_cast<S *>(a.to_ks + d) = *reinterpret_cast<const S *>(a.from_s.k + s);
+  *reinterpret_cast<S *>(a.to_vs + d) = *reinterpret_cast<const S *>(a.from_s.v + s);
+}
+
 // blockIdx.x: (sequence, kv head); blockIdx.y: interleaved shares of the pieces, as many
 // as a piece per thread asks for, up to 32; blockIdx.z: K (0), V (1), or positions and
-// scores (2).
+// scores (2), and the scales, W bytes a row, of packed caches (W 0: of a plain one).
+template <int W>
 __global__ __launch_bounds__(kCT) void evict_copy(EvictArgs a) {
   const int unit = blockIdx.x, b = unit / a.heads, h = unit % a.heads;
   const Budget x = budget(a, b);
@@ -242,6 +257,7 @@ __global__ __launch_bounds__(kCT) void evict_copy(EvictArgs a) {
         for (int i = 0; i < a.gs; ++i)
           a.out_scores[((int64_t)unit * a.gs + i) * a.out_rows + r] =
               a.scores[((int64_t)unit * a.gs + i) * a.score_rows + row];
+      if constexpr (W > 0) copy_scales<W>(a, b, h, row, r);
     }
     return;
   }
@@ -272,8 +288,10 @@ size_t evict_workspace(const smallkv_evict_t &e) {
   return (size_t)e.batch * e.from.n_heads * kept_cap(e) * sizeof(int32_t);
 }
 
-hipError_t launch_evict(const smallkv_evict_t &e, void *ws, hipStream_t st) {
-  EvictArgs a{};
+namespace {
+
+// scale_bytes: of a row's scales, 0 for plain caches.
+hipError_t launch_all(const smallkv_evict_t &e, EvictArgs a, int scale_bytes, void *ws, hipStream_t st) {
   a.batch = e.batch;
   a.max_len = e.max_len;
   a.heads = e.from.n_heads;
@@ -286,7 +304,6 @@ hipError_t launch_evict(const smallkv_evict_t &e, void *ws, hipStream_t st) {
   a.to = cache_view(e.to);
   a.to_k = static_cast<unsigned char *>(e.to.k);
   a.to_v = static_cast<unsigned char *>(e.to.v);
-  a.row_bytes = e.from.head_dim * (e.from.dtype == SMALLKV_F32 ? 4 : 2);
   a.scores = e.scores;
   a.score_rows = e.score_rows;
   a.row_pos = e.row_pos;
@@ -306,8 +323,28 @@ hipError_t launch_evict(const smallkv_evict_t &e, void *ws, hipStream_t st) {
   const hipError_t err = hipGetLastError();
   if (err != hipSuccess) return err;
   const unsigned shares = (unsigned)std::min<int64_t>((a.cap * (a.row_bytes / 16) + kCT - 1) / kCT, 32);
-  hipLaunchKernelGGL(evict_copy, dim3(units, shares, 3), dim3(kCT), 0, st, a);
+  const auto copy = scale_bytes == 4 ? evict_copy<4> : scale_bytes == 2 ? evict_copy<2> : evict_copy<0>;
+  hipLaunchKernelGGL(copy, dim3(units, shares, 3), dim3(kCT), 0, st, a);
   return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_evict(const smallkv_evict_t &e, void *ws, hipStream_t st) {
+  EvictArgs a{};
+  a.row_bytes = e.from.head_dim * (e.from.dtype == SMALLKV_F32 ? 4 : 2);
+  return launch_all(e, a, 0, ws, st);
+}
+
+hipError_t launch_evict_packed(const smallkv_evict_t &e, const smallkv_packed_t &from, const smallkv_packed_t &to,
+                               void *ws, hipStream_t st) {
+  EvictArgs a{};
+  a.row_bytes = from.head_dim * format_bits(from) / 8;
+  a.from_s = scale_view(from);
+  a.to_s = scale_view(to);
+  a.to_ks = to.k_scale;
+  a.to_vs = to.v_scale;
+  return launch_all(e, a, from.head_dim / kBlock, ws, st);
 }
 
 }  // namespace smallkv

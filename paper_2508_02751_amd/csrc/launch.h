@@ -152,4 +152,19 @@ hipError_t launch_append(const smallkv_chunk_t &c, const smallkv_cache_t &kv,
 size_t evict_workspace(const smallkv_evict_t &e);
 hipError_t launch_evict(const smallkv_evict_t &e, void *ws, hipStream_t st);
 
+// The same over packed caches.  An eviction's `from` and `to` hold the codes.
+AttnPlan plan_packed_attn(const smallkv_chunk_t &c, const smallkv_packed_t &kv,
+                          const smallkv_queries_t &q);
+hipError_t launch_packed_attn(const smallkv_chunk_t &c, const smallkv_packed_t &kv,
+                              const smallkv_queries_t &q, const AttnPlan &p, void *ws, hipStream_t st);
+hipError_t launch_packed_scores(const smallkv_chunk_t &c, const smallkv_packed_t &kv,
+                                const smallkv_queries_t &q, int n_score_heads, const float *before,
+                                float *out, int64_t score_rows, int64_t seq_stride, hipStream_t st);
+hipError_t launch_append_packed(const smallkv_chunk_t &c, const smallkv_packed_t &kv,
+                                const smallkv_append_t &a, hipStream_t st);
+hipError_t launch_read_packed(const smallkv_packed_t &from, const smallkv_cache_t &to, int batch,
+                              int max_len, const int32_t *begin, const int32_t *len, hipStream_t st);
+hipError_t launch_evict_packed(const smallkv_evict_t &e, const smallkv_packed_t &from,
+                               const smallkv_packed_t &to, void *ws, hipStream_t st);
+
 }  // namespace smallkv

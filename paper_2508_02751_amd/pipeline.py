@@ -122,17 +122,26 @@ class ModelCache:
     whose first layer() raised is not part of the cache, and the next begin() replaces
     it.  With keep_scores, scores [B][layers * Hkv][n_rows] sum the
     attention each row has received, over queries and the query heads of a kv head.
+    packed (smallkv.MXFP8 or MXFP4): k and v hold the rows' codes, k_scale and v_scale their
+    blocks' scales (see smallkv.PackedSpec); everything else is the same, and read_back gives
+    the rows as the step takes them.
     Everything runs on the current stream.
     """
 
     def __init__(self, batch: int, layers: int, q_heads: int, kv_heads: int, head_dim: int,
                  n_rows: int, rope: S.RopeSpec, dtype=torch.bfloat16, device="cuda",
-                 keep_scores: bool = False, positions: bool = False):
+                 keep_scores: bool = False, positions: bool = False, packed: Optional[int] = None):
         def new(*shape, dt=dtype):
             return torch.zeros(shape, dtype=dt, device=device)
         self.layers, self.q_heads, self.kv_heads, self.rope = layers, q_heads, kv_heads, rope
-        self.k = new(batch, layers, kv_heads, n_rows, head_dim)
-        self.v = torch.zeros_like(self.k)
+        self.head_dim, self.dtype, self.packed = head_dim, dtype, packed
+        rows = (batch, layers, kv_heads, n_rows)
+        if packed is None:
+            self.k, self.v = new(*rows, head_dim), new(*rows, head_dim)
+        else:
+            empty = S.PackedSpec.empty(batch, layers * kv_heads, n_rows, head_dim, packed, device=device)
+            self.k, self.v, self.k_scale, self.v_scale = (
+                t.view(*rows, -1) for t in (empty.k, empty.v, empty.k_scale, empty.v_scale))
         self.scores = new(batch, layers * kv_heads, n_rows, dt=torch.float32) if keep_scores else None
         self.row_pos = new(batch, layers, kv_heads, n_rows, dt=torch.int32) if positions else None
         self.rows, self.tokens = [0] * batch, [0] * batch
@@ -141,6 +150,14 @@ class ModelCache:
     @property
     def n_rows(self) -> int:
         return self.k.shape[3]
+
+    def _rows(self, at):
+        """The layers' rows as a cache: `at` takes [B][layers][Hkv][rows][...] to
+        [B][heads][rows][...]."""
+        if self.packed is None:
+            return S.CacheSpec(at(self.k), at(self.v))
+        return S.PackedSpec(*(at(t) for t in (self.k, self.v, self.k_scale, self.v_scale)),
+                            self.packed)
 
     def _ints(self, v) -> torch.Tensor:
         return torch.tensor(v, dtype=torch.int32, device=self.k.device)
@@ -176,8 +193,10 @@ class ModelCache:
         if not -self.layers <= layer < self.layers:
             raise IndexError(f"layer {layer} of {self.layers}")
         layer %= self.layers
-        cache = S.CacheSpec(self.k[:, layer], self.v[:, layer])
-        scale = softmax_scale(self.k.shape[-1])
+        if self.packed is not None and q.dtype != self.dtype:
+            raise ValueError(f"queries of {q.dtype} for a cache of {self.dtype}")
+        cache = self._rows(lambda t: t[:, layer])
+        scale = softmax_scale(self.head_dim)
         pos = None if self.row_pos is None else self.row_pos[:, layer]
         add = S.prepare_append(self._chunk, cache, self.rope, q, k, v, positions=self._positions,
                                row_pos=pos)
@@ -202,12 +221,14 @@ class ModelCache:
         received most attention.  Needs keep_scores."""
         if self.scores is None:
             raise ValueError("compress() needs a cache with keep_scores")
-        B, L, H, _, d = self.k.shape
-        to = ModelCache(B, L, self.q_heads, H, d, n_rows or max(max(keep), 1), self.rope,
-                        self.k.dtype, self.k.device, keep_scores=True, positions=True)
+        B, L, H = self.k.shape[:3]
+        to = ModelCache(B, L, self.q_heads, H, self.head_dim, n_rows or max(max(keep), 1), self.rope,
+                        self.dtype, self.k.device, keep_scores=True, positions=True,
+                        packed=self.packed)
         pos = None if self.row_pos is None else self.row_pos.view(B, L * H, -1)
-        S.prepare_evict(S.CacheSpec(self.k.flatten(1, 2), self.v.flatten(1, 2)),
-                        S.CacheSpec(to.k.flatten(1, 2), to.v.flatten(1, 2)), self._ints(self.rows),
+        def all_layers(t):
+            return t.flatten(1, 2)
+        S.prepare_evict(self._rows(all_layers), to._rows(all_layers), self._ints(self.rows),
                         self._ints(keep), self.scores,
                         recent=None if recent is None else self._ints(recent), sinks=sinks,
                         row_pos=pos, out_pos=to.row_pos.view(B, L * H, -1), out_scores=to.scores,
@@ -216,9 +237,29 @@ class ModelCache:
         to.tokens = list(self.tokens)
         return to
 
+    def read_back(self, out: Optional[tuple] = None, begin: Optional[Sequence[int]] = None):
+        """A packed cache's rows as plain keys and values (k, v) [B][layers][Hkv][n_rows][d]; out:
+        such a pair to write into (None: a new one, 0 where there are no rows), begin[b]: the
+        first row of each sequence to read (the others of `out` stay as they are)."""
+        if self.packed is None:
+            raise ValueError("read_back() is for packed caches")
+        if out is None:
+            out = tuple(torch.zeros((*self.k.shape[:4], self.head_dim), dtype=self.dtype,
+                                    device=self.k.device) for _ in range(2))
+        k, v = out
+        if not tuple(k.shape) == tuple(v.shape) == (*self.k.shape[:4], self.head_dim):
+            raise ValueError("out must be two tensors [B][layers][Hkv][n_rows][d]")
+        S.prepare_read(self._rows(lambda t: t.flatten(1, 2)),
+                       S.CacheSpec(k.view(k.shape[0], -1, *k.shape[3:]), v.view(v.shape[0], -1, *v.shape[3:])),
+                       self._ints(self.rows), None if begin is None else self._ints(begin),
+                       max_len=max(max(self.rows), 1)).run()
+        return k, v
+
     def small_inputs(self) -> dict:
-        """The small model's entries of a step's inputs (see prepare_step)."""
-        x = {"s_k": self.k, "s_v": self.v}
+        """The small model's entries of a step's inputs (see prepare_step); a packed cache's
+        rows are read back."""
+        k, v = (self.k, self.v) if self.packed is None else self.read_back()
+        x = {"s_k": k, "s_v": v}
         if self.row_pos is not None:
             x.update(s_held=self._ints(self.rows), s_row_pos=self.row_pos)
         return x

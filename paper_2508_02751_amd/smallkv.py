@@ -9,7 +9,9 @@ raises.
 Entry points mirror the C names: smallkv_small_attn, smallkv_partition,
 smallkv_hybrid_attn, smallkv_step, smallkv_workspace_size, the prefill
 matching smallkv_match, smallkv_match_workspace_size, and the cache operators
-(prepare_append, prepare_chunk_attn, prepare_chunk_scores, prepare_evict).
+(prepare_append, prepare_chunk_attn, prepare_chunk_scores, prepare_evict), over
+plain caches (CacheSpec) and packed ones (PackedSpec, which prepare_read reads
+back).
 """
 from __future__ import annotations
 
@@ -82,6 +84,16 @@ class Cache(C.Structure):
                 ("head_stride", C.c_int64), ("row_stride", C.c_int64), ("page_table", C.c_void_p)]
 
 
+class Packed(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p),
+                ("v_scale", C.c_void_p), ("format", C.c_int32), ("dtype", C.c_int32),
+                ("head_dim", C.c_int32), ("n_heads", C.c_int32), ("page_rows", C.c_int32),
+                ("n_pages", C.c_int32), ("table_width", C.c_int32), ("page_stride", C.c_int64),
+                ("head_stride", C.c_int64), ("row_stride", C.c_int64),
+                ("scale_page_stride", C.c_int64), ("scale_head_stride", C.c_int64),
+                ("scale_row_stride", C.c_int64), ("page_table", C.c_void_p)]
+
+
 class Chunk(C.Structure):
     _fields_ = [("batch", C.c_int32), ("n_tokens", C.c_int32), ("max_new", C.c_int32),
                 ("max_len", C.c_int32), ("start", C.c_void_p), ("len", C.c_void_p)]
@@ -123,7 +135,10 @@ EXPORTS = ("smallkv_small_attn", "smallkv_partition", "smallkv_hybrid_attn", "sm
            "smallkv_store_update", "smallkv_store_workspace_size",
            "smallkv_append", "smallkv_rope_freqs", "smallkv_chunk_attn",
            "smallkv_chunk_attn_workspace_size", "smallkv_chunk_scores", "smallkv_evict",
-           "smallkv_evict_workspace_size", "smallkv_status_string", "smallkv_abi_version")
+           "smallkv_evict_workspace_size", "smallkv_append_packed", "smallkv_read_packed",
+           "smallkv_chunk_attn_packed", "smallkv_chunk_attn_packed_workspace_size",
+           "smallkv_chunk_scores_packed", "smallkv_evict_packed",
+           "smallkv_evict_packed_workspace_size", "smallkv_status_string", "smallkv_abi_version")
 
 _lib = None
 
@@ -181,6 +196,20 @@ def lib():
                                            C.c_void_p, C.c_int64, C.c_int64, C.c_void_p]
         L.smallkv_evict.argtypes = [P(Evict), C.c_void_p, C.c_size_t, C.c_void_p]
         L.smallkv_evict_workspace_size.argtypes = [P(Evict), P(C.c_size_t)]
+        L.smallkv_append_packed.argtypes = [P(Chunk), P(Packed), P(Append), C.c_void_p]
+        L.smallkv_read_packed.argtypes = [P(Packed), P(Cache), C.c_int32, C.c_int32, C.c_void_p,
+                                          C.c_void_p, C.c_void_p]
+        L.smallkv_chunk_attn_packed.argtypes = [P(Chunk), P(Packed), P(Queries), C.c_void_p,
+                                                C.c_size_t, C.c_void_p]
+        L.smallkv_chunk_attn_packed_workspace_size.argtypes = [P(Chunk), P(Packed), P(Queries),
+                                                               P(C.c_size_t)]
+        L.smallkv_chunk_scores_packed.argtypes = [P(Chunk), P(Packed), P(Queries), C.c_int32,
+                                                  C.c_void_p, C.c_void_p, C.c_int64, C.c_int64,
+                                                  C.c_void_p]
+        L.smallkv_evict_packed.argtypes = [P(Evict), P(Packed), P(Packed), C.c_void_p, C.c_size_t,
+                                           C.c_void_p]
+        L.smallkv_evict_packed_workspace_size.argtypes = [P(Evict), P(Packed), P(Packed),
+                                                          P(C.c_size_t)]
         L.smallkv_status_string.argtypes = [C.c_int]
         L.smallkv_status_string.restype = C.c_char_p
         L.smallkv_abi_version.argtypes = []
@@ -193,7 +222,10 @@ def lib():
                   "smallkv_accum_select_workspace_size", "smallkv_store_update",
                   "smallkv_store_workspace_size", "smallkv_append", "smallkv_rope_freqs",
                   "smallkv_chunk_attn", "smallkv_chunk_attn_workspace_size",
-                  "smallkv_chunk_scores", "smallkv_evict", "smallkv_evict_workspace_size"):
+                  "smallkv_chunk_scores", "smallkv_evict", "smallkv_evict_workspace_size",
+                  "smallkv_append_packed", "smallkv_read_packed", "smallkv_chunk_attn_packed",
+                  "smallkv_chunk_attn_packed_workspace_size", "smallkv_chunk_scores_packed",
+                  "smallkv_evict_packed", "smallkv_evict_packed_workspace_size"):
             getattr(L, f).restype = C.c_int
         _lib = L
     return _lib
@@ -652,6 +684,87 @@ class CacheSpec:
         """Rows a sequence can have."""
         return self.k.shape[2] * (self.page_table.shape[1] if self.page_table is not None else 1)
 
+    @property
+    def head_dim(self) -> int:
+        return self.k.shape[3]
+
+    @property
+    def tensors(self) -> tuple:
+        return self.k, self.v, self.page_table
+
+
+MXFP8, MXFP4 = 0, 1
+
+
+@dataclasses.dataclass
+class PackedSpec:
+    """One layer's keys and values in 8 (MXFP8) or 4 bits (MXFP4), uint8 views of any strides
+    with contiguous rows: codes k and v [pages][Hkv][rows per page][d, or d / 2], the blocks'
+    scales k_scale and v_scale [pages][Hkv][rows per page][d / 32] (k and v alike).  page_table
+    as in CacheSpec.  Whatever takes a CacheSpec of the queries' dtype takes one of these."""
+    k: torch.Tensor
+    v: torch.Tensor
+    k_scale: torch.Tensor
+    v_scale: torch.Tensor
+    format: int = MXFP8
+    page_table: Optional[torch.Tensor] = None
+
+    @staticmethod
+    def empty(pages: int, heads: int, rows: int, head_dim: int, format: int = MXFP8, page_table=None,
+              device="cuda") -> "PackedSpec":
+        """A cache whose rows are all 0."""
+        if format not in (MXFP8, MXFP4) or head_dim % 32:
+            raise ValueError("format must be MXFP8 or MXFP4, head_dim a multiple of 32")
+
+        def new(n):
+            return torch.zeros((pages, heads, rows, n), dtype=torch.uint8, device=device)
+        codes = head_dim if format == MXFP8 else head_dim // 2
+        return PackedSpec(new(codes), new(codes), new(head_dim // 32), new(head_dim // 32), format,
+                          page_table)
+
+    @property
+    def head_dim(self) -> int:
+        return self.k.shape[3] * (2 if self.format == MXFP4 else 1)
+
+    @property
+    def capacity(self) -> int:
+        """Rows a sequence can have."""
+        return self.k.shape[2] * (self.page_table.shape[1] if self.page_table is not None else 1)
+
+    @property
+    def tensors(self) -> tuple:
+        return self.k, self.v, self.k_scale, self.v_scale, self.page_table
+
+    def c(self, batch: Optional[int] = None, dtype: int = BF16) -> Packed:
+        codes, scales, t = (self.k, self.v), (self.k_scale, self.v_scale), self.page_table
+        if self.format not in (MXFP8, MXFP4):
+            raise ValueError("format must be MXFP8 or MXFP4")
+        if any(x.dtype != torch.uint8 or x.dim() != 4 for x in codes + scales):
+            raise ValueError("packed codes and scales must be 4-d uint8 tensors")
+        shape = tuple(self.k.shape)
+        if tuple(self.v.shape) != shape or any(
+                tuple(x.shape) != (*shape[:3], self.head_dim // 32) for x in scales):
+            raise ValueError("packed k and v must have one shape, and d / 32 scales a row")
+        st, ss = _strides(self.k, "packed k"), _strides(self.k_scale, "k_scale")
+        if st != _strides(self.v, "packed v") or ss != _strides(self.v_scale, "v_scale"):
+            raise ValueError("packed k and v must have the same strides")
+        if t is not None:
+            if t.dim() != 2 or (batch is not None and t.shape[0] != batch):
+                raise ValueError("page_table must be [B][pages per sequence]")
+            _need(t, torch.int32, t.shape, "page_table")
+        elif batch is not None and shape[0] < batch:
+            raise ValueError("a dense cache has a page per sequence")
+        return Packed(*(x.data_ptr() for x in codes + scales), int(self.format), int(dtype),
+                      self.head_dim, shape[1], shape[2], shape[0], t.shape[1] if t is not None else 0,
+                      *st, *ss, t.data_ptr() if t is not None else None)
+
+
+def _rows_of(cache, batch: int, like: torch.Tensor):
+    """(descriptor, name suffix, rows' dtype) of a plain or packed cache for tokens like these."""
+    if isinstance(cache, PackedSpec):
+        return cache.c(batch, _dtype_code(like)), "_packed", like.dtype
+    return cache.c(batch), "", cache.k.dtype
+
 
 @dataclasses.dataclass
 class ChunkSpec:
@@ -683,10 +796,10 @@ class RopeSpec:
     amplitude: float = 1.0
 
 
-def _rows(t: torch.Tensor, n_tokens: int, heads: Optional[int], like: torch.Tensor, what: str):
-    """(token stride, head stride) of packed rows [T][heads][d]."""
-    if t.dim() != 3 or t.shape[0] != n_tokens or t.shape[2] != like.shape[3] or \
-            t.dtype != like.dtype or (heads is not None and t.shape[1] != heads):
+def _rows(t: torch.Tensor, n_tokens: int, heads: Optional[int], like: tuple, what: str):
+    """(token stride, head stride) of packed rows [T][heads][d]; like: (d, dtype)."""
+    if t.dim() != 3 or t.shape[0] != n_tokens or t.shape[2] != like[0] or \
+            t.dtype != like[1] or (heads is not None and t.shape[1] != heads):
         raise ValueError(f"{what} must be [n_tokens][heads][head_dim] in the cache's dtype")
     return _strides(t, what)
 
@@ -723,8 +836,9 @@ class AppendCall(_Call):
     """smallkv_append: q_out = turned q, the cache's new rows = turned k, and v."""
 
     def __init__(self, chunk, cache, rope, q, k, v, positions, q_out, row_pos):
-        ch, ca = chunk.c(), cache.c(chunk.length.numel())
-        T, like = chunk.n_tokens, cache.k
+        ch = chunk.c()
+        ca, form, dtype = _rows_of(cache, chunk.length.numel(), q)
+        T, like = chunk.n_tokens, (cache.head_dim, dtype)
         own = []
         if q_out is None:
             q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
@@ -735,14 +849,14 @@ class AppendCall(_Call):
         _need(positions, torch.int32, (T,), "positions", optional=True)
         planes = (0, 0) if row_pos is None else _planes(row_pos, torch.int32,
                                                         (ch.batch, ca.n_heads), "row_pos")
-        dev = _on_gpu(q, k, v, q_out, positions, row_pos, rope.freq, cache.k, cache.v,
-                      cache.page_table, chunk.start, chunk.length)
+        dev = _on_gpu(q, k, v, q_out, positions, row_pos, rope.freq, *cache.tensors, chunk.start,
+                      chunk.length)
         self.q_out = q_out
         self.desc = Append(q.data_ptr(), k.data_ptr(), v.data_ptr(), *qs, *ks, *vs, q.shape[1],
                            q_out.data_ptr(), *os, _ptr(positions), _ptr(rope.freq),
                            2 * rope.freq.numel(), int(rope.layout), float(rope.amplitude),
                            None if row_pos is None else row_pos.data_ptr(), *planes)
-        self._prepare("smallkv_append", dev, (chunk, cache, rope, q, k, v, positions, row_pos),
+        self._prepare("smallkv_append" + form, dev, (chunk, cache, rope, q, k, v, positions, row_pos),
                       own, ch, ca, self.desc)
 
 
@@ -760,32 +874,33 @@ class ChunkAttnCall(_Call):
     """smallkv_chunk_attn: out [T][Hq][d] and lse [T][Hq]."""
 
     def __init__(self, chunk, cache, q, scale, out, lse, ws):
-        ch, ca = chunk.c(), cache.c(chunk.length.numel())
-        T = chunk.n_tokens
-        qs = _rows(q, T, None, cache.k, "q")
+        ch = chunk.c()
+        ca, form, dtype = _rows_of(cache, chunk.length.numel(), q)
+        T, like = chunk.n_tokens, (cache.head_dim, dtype)
+        qs = _rows(q, T, None, like, "q")
         hq = q.shape[1]
         own = []
         if out is None:
             out = torch.empty((T, hq, q.shape[2]), dtype=q.dtype, device=q.device)
             own.append(out)
-        os = _rows(out, T, hq, cache.k, "out")
+        os = _rows(out, T, hq, like, "out")
         if lse is True:
             lse = torch.empty((T, hq), dtype=torch.float32, device=q.device)
             own.append(lse)
         lse = lse if lse is not False else None
         _need(lse, torch.float32, (T, hq), "lse", optional=True)
-        dev = _on_gpu(q, out, lse, ws, cache.k, cache.v, cache.page_table, chunk.start,
-                      chunk.length)
+        dev = _on_gpu(q, out, lse, ws, *cache.tensors, chunk.start, chunk.length)
         self.out, self.lse = out, lse
         self.desc = Queries(hq, float(scale), q.data_ptr(), *qs, out.data_ptr(), *os, _ptr(lse))
         n = C.c_size_t()
-        _check("smallkv_chunk_attn_workspace_size", lib().smallkv_chunk_attn_workspace_size(
+        name = "smallkv_chunk_attn" + form
+        _check(name + "_workspace_size", getattr(lib(), name + "_workspace_size")(
             C.byref(ch), C.byref(ca), C.byref(self.desc), C.byref(n)))
         if ws is None:
             ws = torch.empty(n.value, dtype=torch.uint8, device=dev)
             own.append(ws)
         self.ws = ws
-        self._prepare("smallkv_chunk_attn", dev, (chunk, cache, q), own, ch, ca, self.desc,
+        self._prepare(name, dev, (chunk, cache, q), own, ch, ca, self.desc,
                       *_ws(self.ws))
 
 
@@ -800,20 +915,20 @@ class ChunkScoresCall(_Call):
     """smallkv_chunk_scores: out [B][Hq or Hkv][rows]."""
 
     def __init__(self, chunk, cache, q, lse, scale, out, before):
-        ch, ca = chunk.c(), cache.c(chunk.length.numel())
+        ch = chunk.c()
+        ca, form, dtype = _rows_of(cache, chunk.length.numel(), q)
         T = chunk.n_tokens
-        qs = _rows(q, T, None, cache.k, "q")
+        qs = _rows(q, T, None, (cache.head_dim, dtype), "q")
         _need(lse, torch.float32, (T, q.shape[1]), "lse")
         if out.dim() != 3:
             raise ValueError("out must be [B][Hq or Hkv][rows]")
         planes = _planes(out, torch.float32, (ch.batch, out.shape[1]), "out")
         if before is not None and _planes(before, torch.float32, out.shape, "before") != planes:
             raise ValueError("before must have out's strides")
-        dev = _on_gpu(q, lse, out, before, cache.k, cache.v, cache.page_table, chunk.start,
-                      chunk.length)
+        dev = _on_gpu(q, lse, out, before, *cache.tensors, chunk.start, chunk.length)
         self.out = out
         self.desc = Queries(q.shape[1], float(scale), q.data_ptr(), *qs, None, 0, 0, _ptr(lse))
-        self._prepare("smallkv_chunk_scores", dev, (chunk, cache, q, lse, out, before), [], ch,
+        self._prepare("smallkv_chunk_scores" + form, dev, (chunk, cache, q, lse, out, before), [], ch,
                       ca, self.desc, out.shape[1], None if before is None else before.data_ptr(),
                       out.data_ptr(), *planes)
 
@@ -834,7 +949,10 @@ class EvictCall(_Call):
                  out_scores, held, max_len):
         if length.dim() != 1:
             raise ValueError("length must be int32 [B]")
+        if isinstance(cache, PackedSpec) != isinstance(to, PackedSpec):
+            raise ValueError("rows are kept as they are: both caches plain, or both packed")
         B = length.numel()
+        packed = isinstance(cache, PackedSpec)
         ca, ct = cache.c(B), to.c(B)
         H = ca.n_heads
         for t, what in ((length, "length"), (keep, "keep"), (recent, "recent"), (held, "held")):
@@ -847,8 +965,8 @@ class EvictCall(_Call):
                 raise ValueError("row_pos must be [B][Hkv][rows]")
             _need(row_pos, torch.int32, (B, H, row_pos.shape[2]), "row_pos")
         rows = to.capacity if out_pos is None else out_pos.shape[-1]
-        dev = _on_gpu(length, keep, recent, scores, row_pos, out_pos, out_scores, held, cache.k,
-                      cache.v, cache.page_table, to.k, to.v, to.page_table)
+        dev = _on_gpu(length, keep, recent, scores, row_pos, out_pos, out_scores, held,
+                      *cache.tensors, *to.tensors)
         own = []
         if out_pos is None:
             out_pos = torch.zeros((B, H, rows), dtype=torch.int32, device=dev)
@@ -862,16 +980,18 @@ class EvictCall(_Call):
             max_len = min(cache.capacity, scores.shape[2],
                           row_pos.shape[2] if row_pos is not None else 1 << 30)
         self.out_pos, self.out_scores, self.held = out_pos, out_scores, held
-        self.desc = Evict(B, int(max_len), _ptr(length), _ptr(keep), _ptr(recent), int(sinks), ca,
-                          ct, scores.shape[1], _ptr(scores), scores.shape[2], _ptr(row_pos),
+        plain = (Cache(), Cache()) if packed else (ca, ct)
+        self.desc = Evict(B, int(max_len), _ptr(length), _ptr(keep), _ptr(recent), int(sinks),
+                          *plain, scores.shape[1], _ptr(scores), scores.shape[2], _ptr(row_pos),
                           row_pos.shape[2] if row_pos is not None else 0, rows, _ptr(out_scores),
                           _ptr(out_pos), _ptr(held))
         n = C.c_size_t()
-        _check("smallkv_evict_workspace_size", lib().smallkv_evict_workspace_size(
-            C.byref(self.desc), C.byref(n)))
+        name, caches = ("smallkv_evict_packed", (ca, ct)) if packed else ("smallkv_evict", ())
+        _check(name + "_workspace_size", getattr(lib(), name + "_workspace_size")(
+            C.byref(self.desc), *map(C.byref, caches), C.byref(n)))
         self.ws = torch.empty(n.value, dtype=torch.uint8, device=dev)
-        self._prepare("smallkv_evict", dev, (cache, to, length, keep, recent, scores, row_pos),
-                      own + [self.ws], self.desc, *_ws(self.ws))
+        self._prepare(name, dev, (cache, to, length, keep, recent, scores, row_pos),
+                      own + [self.ws], self.desc, *caches, *_ws(self.ws))
 
 
 def prepare_evict(cache: CacheSpec, to: CacheSpec, length, keep, scores, recent=None,
@@ -881,6 +1001,34 @@ def prepare_evict(cache: CacheSpec, to: CacheSpec, length, keep, scores, recent=
     sum over a kv head's m) of each sequence's length[b], the first `sinks` and the
     last recent[b] among them, moved to the cache `to`.  row_pos int32
     [B][Hkv][rows]: the rows' positions (None: the rows).  out_pos, held: allocated
-    if None; out_scores float32 [B][m * Hkv][rows of out_pos] or None."""
+    if None; out_scores float32 [B][m * Hkv][rows of out_pos] or None.  Both caches are
+    plain, or both packed in one format."""
     return EvictCall(cache, to, length, keep, scores, recent, sinks, row_pos, out_pos, out_scores,
                      held, max_len)
+
+
+class ReadCall(_Call):
+    """smallkv_read_packed: rows of the plain cache `to`."""
+
+    def __init__(self, cache, to, length, begin, max_len):
+        if not isinstance(cache, PackedSpec) or not isinstance(to, CacheSpec):
+            raise ValueError("rows are read from a PackedSpec into a CacheSpec")
+        if length.dim() != 1:
+            raise ValueError("length must be int32 [B]")
+        B = length.numel()
+        _need(length, torch.int32, (B,), "length")
+        _need(begin, torch.int32, (B,), "begin", optional=True)
+        ca, ct = cache.c(B, _dtype_code(to.k)), to.c(B)
+        dev = _on_gpu(length, begin, *cache.tensors, *to.tensors)
+        if max_len is None:
+            max_len = min(cache.capacity, to.capacity)
+        self._prepare("smallkv_read_packed", dev, (cache, to, length, begin), [], ca, ct, B,
+                      int(max_len), _ptr(begin), _ptr(length))
+
+
+def prepare_read(cache: PackedSpec, to: CacheSpec, length, begin=None,
+                 max_len: Optional[int] = None) -> ReadCall:
+    """Read the packed rows begin[b] (None: 0) .. length[b] - 1 of each sequence back into the
+    same rows of the plain cache `to` (bf16 or fp32, which both hold them exactly).  max_len:
+    no sequence has more rows (None: what both caches can hold)."""
+    return ReadCall(cache, to, length, begin, max_len)
