@@ -264,9 +264,8 @@ template <typename T, int D> struct State {
 
 // O^T += V^T P^T over 32 keys.  TWO: a bf16 model's P in two parts, a product each;
 // without, one rounded part, whose sum is kept too.
-template <typename T, int D, bool TWO>
+template <typename T, int D, bool TWO, typename L = TileLayout<T, D>>
 __device__ __forceinline__ void values32(const unsigned char *sv, int key0, const f32x16_t &p, State<T, D> &st) {
-  using L = TileLayout<T, D>;
   const int lane = threadIdx.x & (kWave - 1), half = lane >> 5;
   if constexpr (sizeof(T) == 2) {
     const bf16x2_t ones = {(__bf16)1.0f, (__bf16)1.0f};
@@ -592,6 +591,40 @@ __device__ __forceinline__ void wait_lds() {
 }
 
 constexpr int kFewWaves = 4;
+
+// Joins the states of NW waves in wave 0: the upper half hands over to the lower one.
+// x: NW / 2 * (D / 2) * 64 floats, ml: the waves' maxima and sums.
+template <typename T, int D, int NW>
+__device__ __forceinline__ void join_waves(State<T, D> &st, float *x, float (&ml)[2][NW / 2][kWave]) {
+  const int lane = threadIdx.x & (kWave - 1);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+#pragma unroll
+  for (int h = NW / 2; h >= 1; h >>= 1) {
+    __syncthreads();
+    if (wave >= h && wave < 2 * h) {
+      float *y = x + (wave - h) * (D / 2) * kWave;
+      ml[0][wave - h][lane] = st.m;
+      ml[1][wave - h][lane] = st.l;
+#pragma unroll
+      for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) y[(d * 16 + i) * kWave + lane] = st.o[d][i];
+    }
+    __syncthreads();
+    if (wave < h) {
+      const float *y = x + wave * (D / 2) * kWave;
+      const float om = ml[0][wave][lane], ol = ml[1][wave][lane];
+      const float m = fmaxf(st.m, om), base = m == -INFINITY ? 0.0f : m;
+      const float f = __builtin_amdgcn_exp2f(st.m - base), fo = __builtin_amdgcn_exp2f(om - base);
+      st.m = m;
+      st.l = st.l * f + ol * fo;
+#pragma unroll
+      for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) st.o[d][i] = st.o[d][i] * f + y[(d * 16 + i) * kWave + lane] * fo;
+    }
+  }
+}
 
 // Joins the records of a tile's spans: four elements of a row per lane, and a row's
 // spans dealt to `parts` groups of such lanes, which each take theirs in one pass with

@@ -189,34 +189,7 @@ template <int D> __global__ __launch_bounds__(kFewWaves * kWave, D == 64 ? 3 : 2
     masked();
   }
   taken = __syncthreads_or(taken);
-  // join the waves' results: the upper half hands over to the lower one
-  float *x = reinterpret_cast<float *>(k0);
-#pragma unroll
-  for (int h = NW / 2; h >= 1; h >>= 1) {
-    __syncthreads();
-    if (wave >= h && wave < 2 * h) {
-      float *y = x + (wave - h) * (D / 2) * kWave;
-      ml[0][wave - h][lane] = st.m;
-      ml[1][wave - h][lane] = st.l;
-#pragma unroll
-      for (int d = 0; d < D / 32; ++d)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) y[(d * 16 + i) * kWave + lane] = st.o[d][i];
-    }
-    __syncthreads();
-    if (wave < h) {
-      const float *y = x + wave * (D / 2) * kWave;
-      const float om = ml[0][wave][lane], ol = ml[1][wave][lane];
-      const float m = fmaxf(st.m, om), base = m == -INFINITY ? 0.0f : m;
-      const float f = __builtin_amdgcn_exp2f(st.m - base), fo = __builtin_amdgcn_exp2f(om - base);
-      st.m = m;
-      st.l = st.l * f + ol * fo;
-#pragma unroll
-      for (int d = 0; d < D / 32; ++d)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) st.o[d][i] = st.o[d][i] * f + y[(d * 16 + i) * kWave + lane] * fo;
-    }
-  }
+  join_waves<T, D, NW>(st, reinterpret_cast<float *>(k0), ml);
   if (wave == 0) write_row<T, D, 32, BN, true>(a, w, st, taken);
 }
 

@@ -77,13 +77,11 @@ template <typename T> __device__ __forceinline__ float weight_of(const ScoreArgs
 // (fp32); of a packed one half of the dimensions.
 template <typename T, int D, int F> struct KeyHalf {
   static constexpr int kPieces = sizeof(T) == 2 ? D / 16 : D / 8;
-  static constexpr int kWords = F ? D * F / 64 : 1;  // of codes
   // piece i of half h
   __device__ __forceinline__ static int piece(int i, int h) {
     return sizeof(T) == 2 && F == 0 ? 2 * i + h : h * kPieces + i;
   }
-  uint4 k[F ? 1 : kPieces];
-  uint32_t w[kWords], scales;  // F: its codes, and its blocks' scales from the low byte on
+  std::conditional_t<F == 0, uint4[kPieces], HalfRow<D, F ? F : 8>> k;
   // off: of the row, or -1; page: its page
   __device__ __forceinline__ void load(const ScoreArgs &a, int64_t off, int page, int key, int kvh, int half) {
     const unsigned char *row = off >= 0 ? a.kv.k + off + (((uint64_t)kvh * a.kv.head_stride) << 4) : zero_row;
@@ -91,25 +89,14 @@ template <typename T, int D, int F> struct KeyHalf {
 #pragma unroll
       for (int i = 0; i < kPieces; ++i) k[i] = reinterpret_cast<const uint4 *>(row)[piece(i, half)];
     } else {
-      const uint8_t *s = off >= 0 ? a.sc.k + scale_offset<D>(a.sc, a.kv, page, key, kvh) : zero_row;
-#pragma unroll
-      for (int i = 0; i < kWords; i += 4) {
-        const uint4 x = reinterpret_cast<const uint4 *>(row)[half * kWords / 4 + i / 4];
-        w[i] = x.x;
-        w[i + 1] = x.y;
-        w[i + 2] = x.z;
-        w[i + 3] = x.w;
-      }
-      if (D == 128)
-        scales = reinterpret_cast<const uint16_t *>(s)[half];
-      else
-        scales = s[half];
+      k.load(row, off >= 0 ? a.sc.k + scale_offset<D>(a.sc, a.kv, page, key, kvh) : zero_row, half);
     }
   }
   __device__ __forceinline__ uint4 get(int i) const {
-    if constexpr (F == 0) return k[i];
-    constexpr int per = kBlock * (int)sizeof(T) / 16;  // pieces of a block
-    return unpack16<T, F>(w, i, scale_of(scales >> (i / per * 8) & 255u));
+    if constexpr (F == 0)
+      return k[i];
+    else
+      return k.template get<T>(i);
   }
 };
 

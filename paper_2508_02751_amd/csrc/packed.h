@@ -84,6 +84,31 @@ template <typename T, int F> __device__ __forceinline__ uint4 unpack16(const uin
   }
 }
 
+// Half of a packed row, its first or last head_dim / 2 elements: codes and scales as they
+// are in memory, and as pieces of 16 bytes of T.
+template <int D, int F> struct HalfRow {
+  static constexpr int kWords = D * F / 64;
+  uint32_t w[kWords], scales;  // (the first block's scale in the low byte)
+  __device__ __forceinline__ void load(const unsigned char *row, const uint8_t *s, int half) {
+#pragma unroll
+    for (int i = 0; i < kWords; i += 4) {
+      const uint4 x = reinterpret_cast<const uint4 *>(row)[half * (kWords / 4) + i / 4];
+      w[i] = x.x;
+      w[i + 1] = x.y;
+      w[i + 2] = x.z;
+      w[i + 3] = x.w;
+    }
+    if constexpr (D == 128)
+      scales = reinterpret_cast<const uint16_t *>(s)[half];
+    else
+      scales = s[half];
+  }
+  template <typename T> __device__ __forceinline__ uint4 get(int i) const {
+    constexpr int per = kBlock * (int)sizeof(T) / 16;  // pieces of a block
+    return unpack16<T, F>(w, i, scale_of(D == 128 ? scales >> (i / per * 8) & 255u : scales));
+  }
+};
+
 // Element e of a row: of T, or of codes of F bits and their scales.
 template <typename T, int F> __device__ __forceinline__ float cached(const unsigned char *row, const uint8_t *scales, int e) {
   if constexpr (F == 0) {

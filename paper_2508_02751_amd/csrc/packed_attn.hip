@@ -1,7 +1,7 @@
 // Attention of the new tokens over a packed cache: the sums of smallkv_chunk_attn with rows
 // of 8- or 4-bit codes, which become bf16 or fp32 (exactly) on their way into LDS.
 //
-// A workgroup's threads hold the codes of the tile after next in registers; a tile's are
+// Many rows: a workgroup's threads hold the codes of the tile after next in registers; a tile's are
 // converted and written to LDS while the tile before it is multiplied.
 #include "attn.h"
 
@@ -137,14 +137,142 @@ __global__ __launch_bounds__(NW * kWave, sizeof(T) * D == 512 ? 1 : 2) void pack
   write_row<T, D, BM, BN, false, F>(a, w, st, taken);
 }
 
+// Values of a wave's 32 keys in LDS, in bf16: written 16 rows of one piece at a time, read 4
+// rows of 4 pieces at a time, both without a conflict of banks.
+template <int D> struct ValueTile : TileLayout<bf16_t, D> {
+  __device__ __forceinline__ static int swz_v(int r) {
+    return D == 128 ? (r & 3) << 2 | (r >> 2 & 3) : (r >> 1 & 1) << 2 | (r >> 2 & 3);
+  }
+};
+
+// Few rows (a decode step), bf16: a column of 32, each wave walks tiles of its own.  A lane
+// takes half of a key's and of a value's row, as they are, a tile ahead: the keys are
+// converted into the operands of their product (whose order of dimensions is free: a
+// half-wave holds a half), the values by way of LDS, which turns them.
+template <int D, int F> __global__ __launch_bounds__(kFewWaves * kWave, 2) void packed_few(AttnArgs a) {
+  using T = bf16_t;
+  using L = ValueTile<D>;
+  constexpr int NW = kFewWaves, NB = F == 4 || D == 64 ? 2 : 1, BN = 32 * NB, P = D / 16;
+  constexpr int kTile = 32 * L::bytes;
+  __shared__ __align__(16) unsigned char v0[NW * kTile];
+  __shared__ float ml[2][NW / 2][kWave];
+  const int lane = threadIdx.x & (kWave - 1), half = lane >> 5, in = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  Share<32> w;
+  if (!w.find(a, blockIdx.x, NW * 32, 1, 0)) return;
+  unsigned char *sv = v0 + wave * kTile;
+  constexpr int step = NW * BN;
+  const int32_t *pages = a.kv.table ? a.kv.table + (int64_t)w.t.b * a.kv.width : a.c.len;
+  HalfRow<D, F> k[NB], v[NB];
+  int page[NB];     // of the tile that is requested next
+  int64_t off[NB];  // of the tile whose values are requested next, or -1, and of its scales
+  int64_t so[NB];
+  auto lookup = [&](int row) {
+#pragma unroll
+    for (int n = 0; n < NB; ++n) page[n] = pages[max(min(row + 32 * n + in, w.end - 1), 0) >> a.kv.shift];
+  };
+  // whether all rows of the tile exist
+  auto place = [&](int row) {
+#pragma unroll
+    for (int n = 0; n < NB; ++n) {
+      const int r = row + 32 * n + in, pg = a.kv.table ? page[n] : w.t.b;
+      off[n] = page_offset(a.kv, pg, r);
+      if (r >= w.end) off[n] = -1;
+      so[n] = scale_offset<D>(a.sc, a.kv, pg, r, w.kvh);
+    }
+  };
+  auto request_keys = [&](int n) {
+    k[n].load(off[n] < 0 ? zero_row : w.k + off[n], off[n] < 0 ? zero_row : a.sc.k + so[n], half);
+  };
+  auto request_values = [&](int n) {
+    v[n].load(off[n] < 0 ? zero_row : w.v + off[n], off[n] < 0 ? zero_row : a.sc.v + so[n], half);
+  };
+  int row = w.begin + wave * BN;
+  lookup(row);
+  bf16x8_t q[P];
+  {
+    const unsigned char *x = a.q + (w.token * a.q_token + w.head * a.q_head) * 2 + half * D;
+#pragma unroll
+    for (int i = 0; i < P; ++i) q[i] = reinterpret_cast<const bf16x8_t *>(x)[i];
+  }
+  State<T, D> st;
+  st.clear();
+  bool taken = false;
+  if (row < w.end) {
+    place(row);
+#pragma unroll
+    for (int n = 0; n < NB; ++n) request_keys(n);
+    lookup(row + step);
+#pragma unroll
+    for (int n = 0; n < NB; ++n) request_values(n);
+    for (; row < w.end; row += step) {
+      f32x16_t s[NB];
+      uint32_t valid[NB];
+      bool full = row + BN - 1 <= w.first_own;
+#pragma unroll
+      for (int n = 0; n < NB; ++n) {
+        const uint64_t there = __ballot(off[n] >= 0);
+        valid[n] = (uint32_t)there;
+        full &= there == ~0ull;
+      }
+#pragma unroll
+      for (int n = 0; n < NB; ++n) {
+        s[n] = f32x16_t{};
+#pragma unroll
+        for (int i = 0; i < P; ++i)
+          s[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, k[n].template get<T>(i)), q[i],
+                                                         s[n], 0, 0, 0);
+      }
+      place(row + step);
+#pragma unroll
+      for (int n = 0; n < NB; ++n) request_keys(n);
+      lookup(row + 2 * step);
+      if (!full) {
+#pragma unroll
+        for (int n = 0; n < NB; ++n) {
+          const uint32_t bits = valid[n] >> (4 * half);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const bool ok = (bits >> reg_key(i) & 1u) && row + 32 * n + reg_key(i) + 4 * half <= w.own;
+            s[n][i] = ok ? s[n][i] : -INFINITY;
+          }
+        }
+      }
+      softmax_step<T, D, NB>(st, s, a.scale2, a.scale2_lo);
+      const bool mixed = min(row + BN, w.end) - 1 > w.first_own;  // rows that some see and some do not
+#pragma unroll
+      for (int n = 0; n < NB; ++n) {
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+          uint4 x = v[n].template get<T>(i);
+          if (mixed) taken |= drop_not_finite<T>(x);
+          *reinterpret_cast<uint4 *>(sv + in * L::bytes + (((half * P + i) ^ L::swz_v(in)) << 4)) = x;
+        }
+        request_values(n);
+        values32<T, D, true, L>(sv, 0, s[n], st);
+      }
+    }
+  }
+  taken = __syncthreads_or(taken);
+  join_waves<T, D, NW>(st, reinterpret_cast<float *>(v0), ml);
+  if (wave == 0) write_row<T, D, 32, BN, true, F>(a, w, st, taken);
+}
+
 template <typename T, int D, int F> hipError_t launch_typed(AttnArgs a, const AttnPlan &p, hipStream_t st) {
   constexpr bool h = sizeof(T) == 2;
   const MergeShape m = merge_shape<D>(a, p);
-  hipLaunchKernelGGL((packed_many<T, D, F, kAttnWaves, h ? 64 : 32>), dim3(p.units * a.hkv),
-                     dim3(kAttnWaves * kWave), 0, st, a);
+  const dim3 grid(p.units * a.hkv);
+  if constexpr (h) {
+    if (p.few) hipLaunchKernelGGL((packed_few<D, F>), grid, dim3(kFewWaves * kWave), 0, st, a);
+  }
+  if (!p.few)
+    hipLaunchKernelGGL((packed_many<T, D, F, kAttnWaves, h ? 64 : 32>), grid, dim3(kAttnWaves * kWave), 0, st, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || !p.splits) return e;
-  launch_merge<T, D, kAttnWaves * 32>(a, p, m, st);
+  if (p.few)
+    launch_merge<T, D, 32>(a, p, m, st);
+  else
+    launch_merge<T, D, kAttnWaves * 32>(a, p, m, st);
   return hipGetLastError();
 }
 
@@ -159,12 +287,13 @@ AttnPlan plan_packed_attn(const smallkv_chunk_t &c, const smallkv_packed_t &kv, 
   AttnPlan p{};
   const int g = q.n_heads / kv.n_heads;
   const int64_t rows = (int64_t)c.max_new * g;
-  p.rows = kAttnWaves * 32;
+  p.few = rows <= 32 && kv.dtype == SMALLKV_BF16;
+  p.rows = p.few ? 32 : kAttnWaves * 32;
   // no more tiles than this, whatever the sequences' lengths
   p.tiles = (int)std::min<int64_t>(c.batch * ceil_div(rows, p.rows), (int64_t)c.n_tokens * g / p.rows + c.batch);
   // the workgroups that run at once on 256 CUs
-  const int slots = std::max(512 / kv.n_heads, 1);
-  const int round = kManyRound * kManyLeast;
+  const int slots = std::max((p.few ? 512 : 512) / kv.n_heads, 1);
+  const int round = p.few ? 32 * kFewWaves : kManyRound * kManyLeast;
   if (p.tiles < slots && c.max_len > round)
     p.splits = (int)std::min<int64_t>(slots, (int64_t)p.tiles * ceil_div(c.max_len, round));
   p.units = std::max(p.tiles, p.splits);
