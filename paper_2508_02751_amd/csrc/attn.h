@@ -418,12 +418,24 @@ template <int BM> struct Share {
   bool live;
   const unsigned char *k, *v; // of the kv head
 
-  __device__ __forceinline__ bool find(const AttnArgs &a, int block, int round, int least, int wave_row) {
-    kvh = block % a.hkv;
+  // Row `at` of the sequence as the lane's own.
+  __device__ __forceinline__ void row(const AttnArgs &a, int at) {
+    r = at;
+    live = r < t.rows;
+    const int rc = live ? r : t.rows - 1;
+    token = t.s.first + rc / a.g;
+    head = kvh * a.g + rc % a.g;
+    own = live ? t.s.len - t.s.n_new + rc / a.g : -1;
+  }
+
+  // The share of unit `flat` and a kv head.
+  __device__ __forceinline__ bool find(const AttnArgs &a, int flat, int kv_head, int round, int least, int wave_row) {
+    kvh = kv_head;
     int span = kWhole;
     if (BM <= 32 && a.single) {
       // no spans and a tile per sequence: many sequences, not searched one by one
-      t.b = block / a.hkv;
+      t.b = flat;
+      if (flat >= a.c.batch) return false;
       t.s = sequence(a.c, t.b, a.kv.cap);
       t.rows = t.s.n_new * a.g;
       t.row0 = t.split = t.unit0 = 0;
@@ -432,22 +444,17 @@ template <int BM> struct Share {
     } else {
       const Lanes<BM> lanes(a);
       span = find_span<BM>(a, lanes, round, least);
-      if (a.splits && block == 0 && threadIdx.x == 0) *a.span = span;
-      if (!locate<BM, true>(a, lanes, span, block / a.hkv, t)) return false;
+      if (a.splits && flat == 0 && kvh == 0 && threadIdx.x == 0) *a.span = span;
+      if (!locate<BM, true>(a, lanes, span, flat, t)) return false;
     }
-    unit = block;
+    unit = flat * a.hkv + kvh;
     const int pos0 = t.s.len - t.s.n_new;  // cached row of the first new token
     const int last = min(t.row0 + BM, t.rows) - 1;
     const int limit = max(pos0 + last / a.g + 1, 0);  // keys the tile's rows see (<= len)
     begin = t.split * span;  // (one span: 0)
     end = min(limit, begin + span);
     if (begin >= limit && t.split > 0) return false;  // (attn_merge reads no record of it)
-    r = t.row0 + wave_row + (int)(threadIdx.x & (BM < 32 ? BM - 1 : 31));
-    live = r < t.rows;
-    const int rc = live ? r : t.rows - 1;
-    token = t.s.first + rc / a.g;
-    head = kvh * a.g + rc % a.g;
-    own = live ? pos0 + rc / a.g : -1;
+    row(a, t.row0 + wave_row + (int)(threadIdx.x & (BM < 32 ? BM - 1 : 31)));
     first_own = pos0 + t.row0 / a.g;
     k = a.kv.k + (((uint64_t)kvh * a.kv.head_stride) << 4);
     v = a.kv.v + (((uint64_t)kvh * a.kv.head_stride) << 4);

@@ -62,7 +62,7 @@ __global__ __launch_bounds__(NW * kWave, 2) void attn_many(AttnArgs a) {
   __shared__ __align__(16) unsigned char k0[kBuf], v0[kBuf], k1[kBuf], v1[kBuf];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   Share<BM> w;
-  if (!w.find(a, blockIdx.x, kManyRound, kManyLeast, wave * 32)) return;
+  if (!w.find(a, blockIdx.x / a.hkv, blockIdx.x % a.hkv, kManyRound, kManyLeast, wave * 32)) return;
   const int w0 = w.t.row0 + wave * 32;
   const bool idle = w0 >= w.t.rows;
   const int highest = w.t.s.len - w.t.s.n_new + min(w0 + 31, w.t.rows - 1) / a.g;  // of the wave's rows
@@ -136,7 +136,7 @@ template <int D> __global__ __launch_bounds__(kFewWaves * kWave, D == 64 ? 3 : 2
   const int lane = threadIdx.x & (kWave - 1);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   Share<32> w;
-  if (!w.find(a, blockIdx.x, NW * 32, 1, 0)) return;
+  if (!w.find(a, blockIdx.x / a.hkv, blockIdx.x % a.hkv, NW * 32, 1, 0)) return;
   unsigned char *sk = k0 + wave * kTile, *sv = v0 + wave * kTile;
   constexpr int step = NW * BN;
   int row = w.begin + wave * BN;
@@ -209,7 +209,7 @@ template <int D> __global__ __launch_bounds__(kFewWaves * kWave, 2) void attn_fe
   const int lane = threadIdx.x & (kWave - 1), quarter = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   Share<16> w;
-  if (!w.find(a, blockIdx.x, NW * BN, 1, 0)) return;
+  if (!w.find(a, blockIdx.x / a.hkv, blockIdx.x % a.hkv, NW * BN, 1, 0)) return;
   unsigned char *sk = k0 + wave * kTile, *sv = v0 + wave * kTile;
   constexpr int step = NW * BN;
   int row = w.begin + wave * BN;

@@ -138,6 +138,7 @@ constexpr int kAttnWaves = 4;
 struct AttnPlan {
   bool few;
   int rows, tiles, splits, units;
+  int waves;  // of a workgroup (packed caches, few rows)
   size_t ws_bytes;
 };
 AttnPlan plan_chunk_attn(const smallkv_chunk_t &c, const smallkv_cache_t &kv,

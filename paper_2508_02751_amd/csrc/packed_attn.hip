@@ -3,6 +3,8 @@
 //
 // Many rows: a workgroup's threads hold the codes of the tile after next in registers; a tile's are
 // converted and written to LDS while the tile before it is multiplied.
+#include <type_traits>
+
 #include "attn.h"
 
 namespace smallkv {
@@ -73,7 +75,7 @@ __global__ __launch_bounds__(NW * kWave, sizeof(T) * D == 512 ? 1 : 2) void pack
   __shared__ __align__(16) unsigned char k0[kBuf], v0[kBuf], k1[kBuf], v1[kBuf];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   Share<BM> w;
-  if (!w.find(a, blockIdx.x, kManyRound, kManyLeast, wave * 32)) return;
+  if (!w.find(a, blockIdx.x / a.hkv, blockIdx.x % a.hkv, kManyRound, kManyLeast, wave * 32)) return;
   const int w0 = w.t.row0 + wave * 32;
   const bool idle = w0 >= w.t.rows;
   const int highest = w.t.s.len - w.t.s.n_new + min(w0 + 31, w.t.rows - 1) / a.g;  // of the wave's rows
@@ -137,142 +139,405 @@ __global__ __launch_bounds__(NW * kWave, sizeof(T) * D == 512 ? 1 : 2) void pack
   write_row<T, D, BM, BN, false, F>(a, w, st, taken);
 }
 
-// Values of a wave's 32 keys in LDS, in bf16: written 16 rows of one piece at a time, read 4
-// rows of 4 pieces at a time, both without a conflict of banks.
-template <int D> struct ValueTile : TileLayout<bf16_t, D> {
-  __device__ __forceinline__ static int swz_v(int r) {
-    return D == 128 ? (r & 3) << 2 | (r >> 2 & 3) : (r >> 1 & 1) << 2 | (r >> 2 & 3);
+// 32 packed rows on their way to LDS: neighbouring lanes take neighbouring pieces of a row, so
+// that an instruction touches whole lines (a row per lane, as the products want it: 16 lines
+// for every 256 bytes, and a third less of the memory's rate).  N pieces a lane.
+template <int D, int F> struct RowTile {
+  static constexpr int P = D * F / 128, R = kWave / P, N = 32 / R, bytes = D * F / 8;
+  u32x4_t w[N];
+  uint32_t s[N];
+  __device__ __forceinline__ static int row(int j) { return j * R + (int)(threadIdx.x & (kWave - 1)) / P; }
+  __device__ __forceinline__ static int piece() { return threadIdx.x & (P - 1); }
+  __device__ __forceinline__ void request(const unsigned char *rows, const uint8_t *scales, const int64_t (&off)[N],
+                                          const int64_t (&so)[N]) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      w[j] = *reinterpret_cast<const u32x4_t *>(rows + off[j]);
+      s[j] = scales[so[j]];
+    }
   }
 };
 
-// Few rows (a decode step), bf16: a column of 32, each wave walks tiles of its own.  A lane
-// takes half of a key's and of a value's row, as they are, a tile ahead: the keys are
-// converted into the operands of their product (whose order of dimensions is free: a
-// half-wave holds a half), the values by way of LDS, which turns them.
-template <int D, int F> __global__ __launch_bounds__(kFewWaves * kWave, 2) void packed_few(AttnArgs a) {
-  using T = bf16_t;
-  using L = ValueTile<D>;
-  constexpr int NW = kFewWaves, NB = F == 4 || D == 64 ? 2 : 1, BN = 32 * NB, P = D / 16;
-  constexpr int kTile = 32 * L::bytes;
-  __shared__ __align__(16) unsigned char v0[NW * kTile];
-  __shared__ float ml[2][NW / 2][kWave];
-  const int lane = threadIdx.x & (kWave - 1), half = lane >> 5, in = lane & 31;
+// Keys of a wave in LDS, as they are: written whole rows at a time, read a piece of 16 rows at a
+// time, both without a conflict of banks.
+template <int D, int F> struct KeyTile {
+  using X = RowTile<D, F>;
+  __device__ __forceinline__ static int swz(int r) { return r / (16 / X::P) & (X::P - 1); }
+  __device__ __forceinline__ static void store(unsigned char *lds, const X &x) {
+#pragma unroll
+    for (int j = 0; j < X::N; ++j)
+      *reinterpret_cast<u32x4_t *>(lds + X::row(j) * X::bytes + ((X::piece() ^ swz(X::row(j))) << 4)) = x.w[j];
+  }
+  // A quarter of row r.
+  __device__ __forceinline__ static void load(const unsigned char *lds, int r, int quarter, uint32_t (&w)[D * F / 128]) {
+    constexpr int kBytes = X::bytes / 4;
+    const unsigned char *row = lds + r * X::bytes;
+    if constexpr (kBytes == 8) {
+      const uint2 x = *reinterpret_cast<const uint2 *>(row + ((quarter / 2 ^ swz(r)) << 4) + quarter % 2 * 8);
+      w[0] = x.x;
+      w[1] = x.y;
+    } else {
+#pragma unroll
+      for (int i = 0; i < kBytes / 16; ++i) {
+        const u32x4_t x = *reinterpret_cast<const u32x4_t *>(row + (((quarter * (kBytes / 16) + i) ^ swz(r)) << 4));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[4 * i + e] = x[e];
+      }
+    }
+  }
+};
+
+// Values of a wave's 32 keys in LDS, in bf16: written as they come, read 32 bytes of 8 rows at a
+// time, both without a conflict of banks.
+template <int D, int F> struct ValueTile {
+  using X = RowTile<D, F>;
+  static constexpr int bytes = 2 * D, kLow = X::R == 8 ? 0 : X::R == 16 ? 1 : 2;
+  __device__ __forceinline__ static int swz(int r) { return (D == 128 ? r & 7 : r >> 1 & 3) << 1 | (r >> kLow & 1); }
+};
+
+// fp32 as a sum of three bf16 numbers (exactly, but for what lies below 2^-133), or as two
+// with an error of 2^-17 of it; infinities and NaN in the first.
+template <int PARTS> __device__ __forceinline__ void split(float x, float (&y)[PARTS]) {
+  y[0] = bf16_hi(__float_as_uint(x));
+  float rest = fabsf(x) <= 3.402823466e38f ? x - y[0] : 0.0f;
+#pragma unroll
+  for (int i = 1; i + 1 < PARTS; ++i) {
+    y[i] = bf16_hi(__float_as_uint(rest));
+    rest -= y[i];
+  }
+  if (PARTS > 1) y[PARTS - 1] = rest;
+}
+
+// Workgroups go to the XCDs, each with an L2 of its own, in turn: the kv heads of a unit, whose
+// rows share lines of memory where a page holds [row][head], follow each other on one.
+constexpr int kXcds = 8;
+
+// Few rows (a decode step): CB columns of 16, on 16 x 16 tiles; each wave walks tiles of 32
+// keys of its own, whose rows it requests a tile ahead.  Keys go through LDS as they are, and
+// become operands as they leave it (a quarter-wave holds a quarter of the dimensions: their
+// order in the product is free); values become bf16 on their way into it, and the read that
+// turns them leaves them as operands.  An fp32 model's queries and probabilities go through
+// the products in three bf16 parts, so that they lose nothing that fp32 holds.
+template <typename T, int D, int F, int CB, int NW>
+__global__ __launch_bounds__(NW * kWave, 2) void packed_few(AttnArgs a) {
+  using X = RowTile<D, F>;
+  using K = KeyTile<D, F>;
+  using L = ValueTile<D, F>;
+  constexpr int BN = 32, BM = 16 * CB, QP = sizeof(T) == 4 ? 3 : 1, PP = sizeof(T) == 4 ? 3 : 2;
+  constexpr int kKeys = BN * X::bytes, kTile = BN * L::bytes, kSteps = D / 32, kBlocks = D / 16;
+  __shared__ __align__(16) unsigned char v0[NW * kTile], k0[NW * kKeys];
+  __shared__ float ml[2][NW / 2][CB][kWave];
+  const int lane = threadIdx.x & (kWave - 1), quarter = lane >> 4, in = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  Share<32> w;
-  if (!w.find(a, blockIdx.x, NW * 32, 1, 0)) return;
-  unsigned char *sv = v0 + wave * kTile;
+  const int flat = blockIdx.x / kXcds / a.hkv * kXcds + blockIdx.x % kXcds;
+  int page = 0;  // of row lane % 32 of the tile that is requested next
+  if (a.single && a.kv.table && flat < a.c.batch)  // (the first does not wait for the lengths)
+    page = a.kv.table[(int64_t)flat * a.kv.width + (min(wave * BN + (lane & 31), a.kv.cap - 1) >> a.kv.shift)];
+  Share<BM> w;
+  if (!w.find(a, flat, blockIdx.x / kXcds % a.hkv, NW * BN, 1, 0)) return;
+  unsigned char *sv = v0 + wave * kTile, *sk = k0 + wave * kKeys;
   constexpr int step = NW * BN;
   const int32_t *pages = a.kv.table ? a.kv.table + (int64_t)w.t.b * a.kv.width : a.c.len;
-  HalfRow<D, F> k[NB], v[NB];
-  int page[NB];     // of the tile that is requested next
-  int64_t off[NB];  // of the tile whose values are requested next, or -1, and of its scales
-  int64_t so[NB];
-  auto lookup = [&](int row) {
-#pragma unroll
-    for (int n = 0; n < NB; ++n) page[n] = pages[max(min(row + 32 * n + in, w.end - 1), 0) >> a.kv.shift];
-  };
-  // whether all rows of the tile exist
+  X k, v;                        // of the next tile
+  int64_t off[X::N], so[X::N];   // of the rows that are requested next, and their blocks' scales
+  uint32_t scale[2];             // of the lane's quarters of two keys
+  auto lookup = [&](int row) { page = pages[max(min(row + (lane & 31), w.end - 1), 0) >> a.kv.shift]; };
+  // Rows that do not exist are read from rows that do, and masked.
   auto place = [&](int row) {
+    const int pg = a.kv.table ? page : w.t.b;
+    const bool there = (uint32_t)pg < (uint32_t)a.kv.n_pages;
+    const uint32_t exist = (uint32_t)__ballot(there && row + (lane & 31) < w.end);
+    const int at = there ? pg : 0;
 #pragma unroll
-    for (int n = 0; n < NB; ++n) {
-      const int r = row + 32 * n + in, pg = a.kv.table ? page[n] : w.t.b;
-      off[n] = page_offset(a.kv, pg, r);
-      if (r >= w.end) off[n] = -1;
-      so[n] = scale_offset<D>(a.sc, a.kv, pg, r, w.kvh);
+    for (int j = 0; j < X::N; ++j) {
+      const int r = min(row + X::row(j), w.end - 1), from = __shfl(at, X::row(j), kWave);
+      off[j] = page_offset(a.kv, from, r) + X::piece() * 16;
+      so[j] = scale_offset<D>(a.sc, a.kv, from, r, w.kvh) + X::piece() * 128 / F / kBlock;
     }
-  };
-  auto request_keys = [&](int n) {
-    k[n].load(off[n] < 0 ? zero_row : w.k + off[n], off[n] < 0 ? zero_row : a.sc.k + so[n], half);
-  };
-  auto request_values = [&](int n) {
-    v[n].load(off[n] < 0 ? zero_row : w.v + off[n], off[n] < 0 ? zero_row : a.sc.v + so[n], half);
+    return exist;
   };
   int row = w.begin + wave * BN;
-  lookup(row);
-  bf16x8_t q[P];
-  {
-    const unsigned char *x = a.q + (w.token * a.q_token + w.head * a.q_head) * 2 + half * D;
+  if (!a.single) lookup(row);
+  bf16x8_t q[CB][QP][kSteps];
+  int own[CB];
 #pragma unroll
-    for (int i = 0; i < P; ++i) q[i] = reinterpret_cast<const bf16x8_t *>(x)[i];
+  for (int c = 0; c < CB; ++c) {
+    w.row(a, w.t.row0 + 16 * c + in);
+    own[c] = w.own;
+    const unsigned char *x = a.q + (w.token * a.q_token + w.head * a.q_head + quarter * (D / 4)) * (int64_t)sizeof(T);
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) {
+      if constexpr (sizeof(T) == 2) {
+        q[c][0][i] = reinterpret_cast<const bf16x8_t *>(x)[i];
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          float y[QP];
+          split<QP>(reinterpret_cast<const float *>(x)[8 * i + e], y);
+#pragma unroll
+          for (int p = 0; p < QP; ++p) q[c][p][i][e] = (__bf16)y[p];
+        }
+      }
+    }
   }
-  State<T, D> st;
-  st.clear();
+  float m[CB], l[CB];  // running maximum (log2 units), this quarter-wave's part of the sum
+  f32x4_t o[CB][kBlocks];
+#pragma unroll
+  for (int c = 0; c < CB; ++c) {
+    m[c] = -INFINITY;
+    l[c] = 0.0f;
+#pragma unroll
+    for (int d = 0; d < kBlocks; ++d) o[c][d] = f32x4_t{};
+  }
   bool taken = false;
   if (row < w.end) {
-    place(row);
-#pragma unroll
-    for (int n = 0; n < NB; ++n) request_keys(n);
+    uint32_t next = place(row);  // rows of the next tile that exist
+    k.request(w.k, a.sc.k, off, so);
     lookup(row + step);
-#pragma unroll
-    for (int n = 0; n < NB; ++n) request_values(n);
+    v.request(w.v, a.sc.v, off, so);
     for (; row < w.end; row += step) {
-      f32x16_t s[NB];
-      uint32_t valid[NB];
-      bool full = row + BN - 1 <= w.first_own;
-#pragma unroll
-      for (int n = 0; n < NB; ++n) {
-        const uint64_t there = __ballot(off[n] >= 0);
-        valid[n] = (uint32_t)there;
-        full &= there == ~0ull;
+      const uint32_t rows = next;
+      const bool full = row + BN - 1 <= w.first_own && rows == ~0u;
+      K::store(sk, k);
+      // a quarter's scale: of the lane that brought its (first) piece
+      const int from = in % X::R * X::P + quarter * X::P / 4;
+      if constexpr (X::R == 8) {
+        const int s0 = __shfl((int)k.s[0], from, kWave), s1 = __shfl((int)k.s[1], from, kWave);
+        const int s2 = __shfl((int)k.s[2], from, kWave), s3 = __shfl((int)k.s[3], from, kWave);
+        scale[0] = in < 8 ? s0 : s1;
+        scale[1] = in < 8 ? s2 : s3;
+      } else {
+        scale[0] = __shfl((int)k.s[0], from, kWave);
+        scale[1] = __shfl((int)k.s[X::N - 1], X::R == 32 ? from + 16 * X::P : from, kWave);
       }
+      f32x4_t s[CB][2] = {};
 #pragma unroll
-      for (int n = 0; n < NB; ++n) {
-        s[n] = f32x16_t{};
+      for (int n = 0; n < 2; ++n) {
+        uint32_t codes[D * F / 128];
+        K::load(sk, 16 * n + in, quarter, codes);
 #pragma unroll
-        for (int i = 0; i < P; ++i)
-          s[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, k[n].template get<T>(i)), q[i],
-                                                         s[n], 0, 0, 0);
+        for (int i = 0; i < kSteps; ++i) {
+          const bf16x8_t x = __builtin_bit_cast(bf16x8_t, (unpack16<bf16_t, F>(codes, i, scale_of(scale[n]))));
+#pragma unroll
+          for (int c = 0; c < CB; ++c)
+#pragma unroll
+            for (int p = QP - 1; p >= 0; --p) s[c][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, q[c][p][i], s[c][n], 0, 0, 0);
+        }
       }
-      place(row + step);
-#pragma unroll
-      for (int n = 0; n < NB; ++n) request_keys(n);
+      next = place(row + step);
+      k.request(w.k, a.sc.k, off, so);
       lookup(row + 2 * step);
       if (!full) {
 #pragma unroll
-        for (int n = 0; n < NB; ++n) {
-          const uint32_t bits = valid[n] >> (4 * half);
+        for (int n = 0; n < 2; ++n)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const bool ok = (bits >> reg_key(i) & 1u) && row + 32 * n + reg_key(i) + 4 * half <= w.own;
-            s[n][i] = ok ? s[n][i] : -INFINITY;
+          for (int i = 0; i < 4; ++i) {
+            const bool there = rows >> (16 * n + 4 * quarter + i) & 1u;
+#pragma unroll
+            for (int c = 0; c < CB; ++c)
+              if (!there || row + 16 * n + 4 * quarter + i > own[c]) s[c][n][i] = -INFINITY;
+          }
+      }
+      // the running maximum and sum; the reference point moves only when the maximum has
+      // grown by more than 2^8 since it was set
+      bf16x8_t pf[CB][PP];
+#pragma unroll
+      for (int c = 0; c < CB; ++c) {
+        float mx = s[c][0][0];
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) mx = fmaxf(mx, s[c][n][i]);
+        mx = swap_halves_max(swap_rows_max(mx)) * a.scale2;
+        if (__any(mx > m[c] + 8.0f)) {
+          const float top = fmaxf(m[c], mx), f = __builtin_amdgcn_exp2f(m[c] - (top == -INFINITY ? 0.0f : top));
+          m[c] = top;
+          l[c] *= f;
+#pragma unroll
+          for (int d = 0; d < kBlocks; ++d) o[c][d] *= f;
+        }
+        const float base = m[c] == -INFINITY ? 0.0f : m[c];
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float x = s[c][n][i];
+            const float y = sizeof(T) == 4 ? __builtin_fmaf(fmaxf(x, -3.402823466e38f), a.scale2_lo, -base) : -base;
+            const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x, a.scale2, y));
+            l[c] += p;
+            float parts[PP];
+            split<PP>(p, parts);
+#pragma unroll
+            for (int e = 0; e < PP; ++e) pf[c][e][4 * n + i] = (__bf16)parts[e];
+          }
+      }
+      const bool mixed = min(row + BN, w.end) - 1 > w.first_own;  // rows that some see and some do not
+      auto put = [&](auto whole) {
+#pragma unroll
+        for (int j = 0; j < X::N; ++j) {
+          const int r = X::row(j);
+          const uint32_t codes[4] = {v.w[j][0], v.w[j][1], v.w[j][2], v.w[j][3]};
+#pragma unroll
+          for (int i = 0; i < 16 / F; ++i) {
+            uint4 x = unpack16<bf16_t, F>(codes, i, scale_of(v.s[j]));
+            if (!whole) {
+              if (!(rows >> r & 1u)) x = make_uint4(0, 0, 0, 0);
+              if (mixed) taken |= drop_not_finite<bf16_t>(x);
+            }
+            *reinterpret_cast<uint4 *>(sv + r * L::bytes + (((X::piece() * (16 / F) + i) ^ L::swz(r)) << 4)) = x;
           }
         }
-      }
-      softmax_step<T, D, NB>(st, s, a.scale2, a.scale2_lo);
-      const bool mixed = min(row + BN, w.end) - 1 > w.first_own;  // rows that some see and some do not
+      };
+      if (full)
+        put(std::true_type());
+      else
+        put(std::false_type());
+      v.request(w.v, a.sc.v, off, so);
+      // the transposing read: 16 lanes take 4 rows of 16 elements, lane i of them ends with
+      // the 4 rows' element i
 #pragma unroll
-      for (int n = 0; n < NB; ++n) {
+      for (int d = 0; d < kBlocks; ++d) {
+        union { s16x4_t h[2]; bf16x8_t v; } x;
 #pragma unroll
-        for (int i = 0; i < P; ++i) {
-          uint4 x = v[n].template get<T>(i);
-          if (mixed) taken |= drop_not_finite<T>(x);
-          *reinterpret_cast<uint4 *>(sv + in * L::bytes + (((half * P + i) ^ L::swz_v(in)) << 4)) = x;
+        for (int n = 0; n < 2; ++n) {
+          const int r = 16 * n + 4 * quarter + (in >> 2), c = 2 * d + ((lane & 3) >> 1);
+          x.h[n] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+              (SMALLKV_LDS s16x4_t *)(sv + (r * L::bytes + ((c ^ L::swz(r)) << 4) + (lane & 1) * 8)));
         }
-        request_values(n);
-        values32<T, D, true, L>(sv, 0, s[n], st);
+#pragma unroll
+        for (int c = 0; c < CB; ++c)
+#pragma unroll
+          for (int e = PP - 1; e >= 0; --e) o[c][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x.v, pf[c][e], o[c][d], 0, 0, 0);
       }
     }
   }
   taken = __syncthreads_or(taken);
-  join_waves<T, D, NW>(st, reinterpret_cast<float *>(v0), ml);
-  if (wave == 0) write_row<T, D, 32, BN, true, F>(a, w, st, taken);
+  // join the waves' results: the upper half hands over to the lower one
+  float *x = reinterpret_cast<float *>(v0);
+#pragma unroll
+  for (int h = NW / 2; h >= 1; h >>= 1) {
+    __syncthreads();
+    float *y = x + (wave & (h - 1)) * CB * (D / 4) * kWave;
+    if (wave >= h && wave < 2 * h) {
+#pragma unroll
+      for (int c = 0; c < CB; ++c) {
+        ml[0][wave - h][c][lane] = m[c];
+        ml[1][wave - h][c][lane] = l[c];
+#pragma unroll
+        for (int d = 0; d < kBlocks; ++d) reinterpret_cast<f32x4_t *>(y)[(c * kBlocks + d) * kWave + lane] = o[c][d];
+      }
+    }
+    __syncthreads();
+    if (wave < h) {
+#pragma unroll
+      for (int c = 0; c < CB; ++c) {
+        const float om = ml[0][wave][c][lane], ol = ml[1][wave][c][lane];
+        const float top = fmaxf(m[c], om), base = top == -INFINITY ? 0.0f : top;
+        const float f = __builtin_amdgcn_exp2f(m[c] - base), fo = __builtin_amdgcn_exp2f(om - base);
+        m[c] = top;
+        l[c] = l[c] * f + ol * fo;
+#pragma unroll
+        for (int d = 0; d < kBlocks; ++d)
+          o[c][d] = o[c][d] * f + reinterpret_cast<const f32x4_t *>(y)[(c * kBlocks + d) * kWave + lane] * fo;
+      }
+    }
+  }
+  if (wave > 0) return;
+#pragma unroll
+  for (int c = 0; c < CB; ++c) {
+    w.row(a, w.t.row0 + 16 * c + in);
+    const float sum = swap_halves_sum(swap_rows_sum(l[c]));
+    if (w.live) write_row<T, D, BM, BN, F>(a, w, o[c], m[c], sum, 4 * quarter, 16, quarter == 0, taken);
+  }
+}
+
+// Joins the records of a tile's spans: four elements of a row per lane, a row's spans dealt to
+// `parts` groups of such lanes, which each take theirs in one pass with the running maximum,
+// scale their sums to the row's maximum and add them up in LDS.
+template <typename T, int D, int BM> __global__ __launch_bounds__(kMaxParts * (D / 4)) void join_spans(AttnArgs a) {
+  constexpr int W = D / 4;  // lanes of a row
+  __shared__ f32x4_t so[kMaxParts * W];
+  __shared__ float2 sml[kMaxParts];
+  const int kvh = blockIdx.x % a.hkv, span = *a.span;
+  const Lanes<BM> lanes(a);
+  Tile t;
+  if (span == kWhole || !locate<BM, false>(a, lanes, span, blockIdx.x / a.hkv, t) || t.n_split == 1) return;
+  const int group = threadIdx.x / W, e = threadIdx.x % W * 4;
+  const int n_rows = blockDim.x / W / a.parts, part = group / n_rows;
+  const int in = blockIdx.y * n_rows + group % n_rows, r = t.row0 + in;
+  const int own = t.s.len - t.s.n_new + r / a.g;
+  const int token = t.s.first + r / a.g, head = kvh * a.g + r % a.g;
+  // spans that hold a row this one sees; the others wrote nothing it needs
+  const int n = r >= t.rows || own < 0 ? 0 : min(own / span + 1, t.n_split);
+  const int64_t stride = (int64_t)a.hkv * BM, at = ((int64_t)t.unit0 * a.hkv + kvh) * BM + in;
+  const int64_t step = stride * a.parts;
+  const float *ml = a.rec + a.rec_ml + 2 * (at + part * stride), *rec = a.rec + (at + part * stride) * D + e;
+  float m = -INFINITY, l = 0.0f;
+  f32x4_t o = {};
+  const int count = n > part ? (n - part - 1) / a.parts + 1 : 0;
+#pragma unroll 4
+  for (int s = 0; s < count; ++s) {
+    const float2 x = *reinterpret_cast<const float2 *>(ml + 2 * s * step);
+    const f32x4_t v = *reinterpret_cast<const f32x4_t *>(rec + s * step * D);
+    const float top = fmaxf(m, x.x), base = top == -INFINITY ? 0.0f : top;
+    const float f = __builtin_amdgcn_exp2f(m - base), w = __builtin_amdgcn_exp2f(x.x - base);
+    m = top;
+    l = l * f + x.y * w;
+    o = o * f + v * w;
+  }
+  if (a.parts > 1) {
+    if (e == 0) sml[group] = make_float2(m, l);
+    __syncthreads();
+    float top = -INFINITY;
+    for (int g = group % n_rows; g < n_rows * a.parts; g += n_rows) top = fmaxf(top, sml[g].x);
+    const float base = top == -INFINITY ? 0.0f : top, f = __builtin_amdgcn_exp2f(m - base);
+    so[threadIdx.x] = o * f;
+    l = 0.0f;
+    for (int g = group % n_rows; g < n_rows * a.parts; g += n_rows)
+      l += sml[g].y * __builtin_amdgcn_exp2f(sml[g].x - base);
+    m = top;
+    __syncthreads();
+    if (part > 0) return;
+    o = f32x4_t{};
+    for (int g = group; g < n_rows * a.parts; g += n_rows) o += so[g * W + threadIdx.x % W];
+  }
+  if (r >= t.rows) return;
+  const f32x4_t x = l == 0.0f ? f32x4_t{} : o * (1.0f / l);
+  unsigned char *out = a.out + (token * a.o_token + head * a.o_head) * (int64_t)sizeof(T);
+  if constexpr (sizeof(T) == 4)
+    *reinterpret_cast<f32x4_t *>(out + e * 4) = x;
+  else
+    *reinterpret_cast<bf16x4_t *>(out + e * 2) = __builtin_convertvector(x, bf16x4_t);
+  if (a.lse && e == 0)
+    a.lse[(int64_t)token * a.hq + head] = l == 0.0f ? -INFINITY : (m + __log2f(l)) * kLn2;
+}
+
+// rows: of a tile that there can be.
+template <typename T, int D, int BM>
+void launch_join(AttnArgs a, const AttnPlan &p, const MergeShape &m, int rows, hipStream_t st) {
+  hipLaunchKernelGGL((join_spans<T, D, BM>), dim3(p.tiles * a.hkv, ceil_div(rows, m.n_rows)), dim3(m.threads), 0, st,
+                     a);
 }
 
 template <typename T, int D, int F> hipError_t launch_typed(AttnArgs a, const AttnPlan &p, hipStream_t st) {
   constexpr bool h = sizeof(T) == 2;
   const MergeShape m = merge_shape<D>(a, p);
-  const dim3 grid(p.units * a.hkv);
-  if constexpr (h) {
-    if (p.few) hipLaunchKernelGGL((packed_few<D, F>), grid, dim3(kFewWaves * kWave), 0, st, a);
-  }
+  const dim3 grid((p.few ? (p.units + kXcds - 1) / kXcds * kXcds : p.units) * a.hkv), few(p.waves * kWave);
   if (!p.few)
     hipLaunchKernelGGL((packed_many<T, D, F, kAttnWaves, h ? 64 : 32>), grid, dim3(kAttnWaves * kWave), 0, st, a);
+  else if (p.rows == 16)
+    hipLaunchKernelGGL((p.waves == 8 ? packed_few<T, D, F, 1, 8> : packed_few<T, D, F, 1, 4>), grid, few, 0, st, a);
+  else if constexpr (h)
+    hipLaunchKernelGGL((p.waves == 8 ? packed_few<T, D, F, 2, 8> : packed_few<T, D, F, 2, 4>), grid, few, 0, st, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || !p.splits) return e;
-  if (p.few)
-    launch_merge<T, D, 32>(a, p, m, st);
+  const int rows = (int)std::min<int64_t>(p.rows, (int64_t)a.c.max_new * a.g);
+  if (!p.few)
+    launch_join<T, D, kAttnWaves * 32>(a, p, m, rows, st);
+  else if (p.rows == 16)
+    launch_join<T, D, 16>(a, p, m, rows, st);
   else
-    launch_merge<T, D, kAttnWaves * 32>(a, p, m, st);
+    launch_join<T, D, 32>(a, p, m, rows, st);
   return hipGetLastError();
 }
 
@@ -287,14 +552,28 @@ AttnPlan plan_packed_attn(const smallkv_chunk_t &c, const smallkv_packed_t &kv, 
   AttnPlan p{};
   const int g = q.n_heads / kv.n_heads;
   const int64_t rows = (int64_t)c.max_new * g;
-  p.few = rows <= 32 && kv.dtype == SMALLKV_BF16;
-  p.rows = p.few ? 32 : kAttnWaves * 32;
+  const bool f32 = kv.dtype == SMALLKV_F32;
+  p.few = rows <= (f32 ? 64 : 32);
+  p.rows = !p.few ? kAttnWaves * 32 : f32 || rows <= 16 ? 16 : 32;
   // no more tiles than this, whatever the sequences' lengths
   p.tiles = (int)std::min<int64_t>(c.batch * ceil_div(rows, p.rows), (int64_t)c.n_tokens * g / p.rows + c.batch);
-  // the workgroups that run at once on 256 CUs
-  const int slots = std::max((p.few ? 512 : 512) / kv.n_heads, 1);
+  // Few rows: whole sequences where they are short, or make a workgroup for enough CUs and are
+  // not long; else spans, and a join.  (28 query and 4 kv heads of 128 in 8 bits, us: one
+  // sequence of 512 rows 8.7, in spans 10.6; of 1024 13.0 and 11.1; 16 of 1024 rows 13.4 and
+  // 15.4, 64 16.0 and 21.6; 24 of 2048 20.8 and 19.8, 48 22.4 and 28.0; 32 of 4096 36.0 and
+  // 35.9, 48 41.8 and 48.9; 40 of 1024 - 4096 34.9 and 29.5, 64 42.2 and 45.9.)
+  const int64_t groups = (int64_t)p.tiles * kv.n_heads;
+  const bool whole = p.few && p.tiles <= c.batch &&
+                     (c.max_len <= 512 || (c.max_len <= 1024 && groups >= 32) || (c.max_len <= 4096 && groups >= 160));
+  // eight waves where that is one workgroup per CU (64 of 1024 - 4096 rows 41.8 us, with four
+  // 50.0; 90 of 2048 49.7 and 41.7)
+  p.waves = whole && c.max_len > 512 && groups <= 256 ? 8 : kFewWaves;
+  // the workgroups that run at once on 256 CUs, two on each; of 4 bits three (64 of 1024 - 4096
+  // rows 32.7 us with two, 28.6 with three; in 8 bits 45.4 and 50.8)
+  const bool three = p.rows == 16 && kv.dtype == SMALLKV_BF16 && kv.head_dim == 128 && kv.format == SMALLKV_MXFP4;
+  const int slots = std::max((three ? 768 : 512) / kv.n_heads, 1);
   const int round = p.few ? 32 * kFewWaves : kManyRound * kManyLeast;
-  if (p.tiles < slots && c.max_len > round)
+  if (p.tiles < slots && c.max_len > round && !whole)
     p.splits = (int)std::min<int64_t>(slots, (int64_t)p.tiles * ceil_div(c.max_len, round));
   p.units = std::max(p.tiles, p.splits);
   if (p.splits) p.ws_bytes = kSpanBytes + (size_t)p.units * kv.n_heads * p.rows * (kv.head_dim + 2) * sizeof(float);
