@@ -4,6 +4,7 @@
 #pragma once
 
 #include <algorithm>
+#include <type_traits>
 
 #include "launch.h"
 #include "packed.h"
@@ -200,6 +201,19 @@ template <typename L, int BN, int SHARE> struct Loader {
   }
 };
 
+// fp32 as a sum of three bf16 numbers (exactly, but for what lies below 2^-133), or as two
+// with an error of 2^-17 of it; infinities and NaN in the first.
+template <int PARTS> __device__ __forceinline__ void split(float x, float (&y)[PARTS]) {
+  y[0] = bf16_hi(__float_as_uint(x));
+  float rest = fabsf(x) <= 3.402823466e38f ? x - y[0] : 0.0f;
+#pragma unroll
+  for (int i = 1; i + 1 < PARTS; ++i) {
+    y[i] = bf16_hi(__float_as_uint(rest));
+    rest -= y[i];
+  }
+  if (PARTS > 1) y[PARTS - 1] = rest;
+}
+
 template <typename T, int D> struct QFrag;
 template <int D> struct QFrag<bf16_t, D> {
   bf16x8_t f[D / 16];
@@ -216,6 +230,37 @@ template <int D> struct QFrag<float, D> {
   }
 };
 
+template <int D> struct QFrag<wide_t, D> {
+  // (the last part of 128 elements waits in LDS: registers for two waves per SIMD)
+  static constexpr int kKept = D == 128 ? 2 : 3, kLds = (3 - kKept) * D / 16;
+  bf16x8_t f[kKept][D / 16];
+  const bf16x8_t *rest;
+  // lds: kLds * 64 pieces of the wave's own
+  __device__ __forceinline__ void load(const unsigned char *row, int half, bf16x8_t *lds) {
+    rest = lds + (threadIdx.x & (kWave - 1));
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s) {
+      bf16x8_t x[3];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        float y[3];
+        split<3>(reinterpret_cast<const float *>(row)[s * 16 + half * 8 + e], y);
+#pragma unroll
+        for (int p = 0; p < 3; ++p) x[p][e] = (__bf16)y[p];
+      }
+#pragma unroll
+      for (int p = 0; p < kKept; ++p) f[p][s] = x[p];
+      if (kKept < 3) lds[s * kWave + (threadIdx.x & (kWave - 1))] = x[2];
+    }
+  }
+  template <int P> __device__ __forceinline__ bf16x8_t part(int i) const {
+    if constexpr (P < kKept)
+      return f[P][i];
+    else
+      return rest[i * kWave];
+  }
+};
+
 // S^T of 32 keys (rows key0 .. of the tile) and the wave's 32 query rows.
 template <typename T, int D>
 __device__ __forceinline__ f32x16_t logits32(const unsigned char *sk, int key0, const QFrag<T, D> &q) {
@@ -223,7 +268,17 @@ __device__ __forceinline__ f32x16_t logits32(const unsigned char *sk, int key0, 
   const int lane = threadIdx.x & (kWave - 1), r = key0 + (lane & 31), half = lane >> 5;
   const unsigned char *row = sk + r * L::bytes;
   const int z = L::swz_k(r);
-  if constexpr (sizeof(T) == 2) {
+  if constexpr (std::is_same_v<T, wide_t>) {
+    f32x16_t s = {};
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) {
+      const bf16x8_t k = *reinterpret_cast<const bf16x8_t *>(row + (((2 * i + half) ^ z) << 4));
+      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q.template part<2>(i), s, 0, 0, 0);
+      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q.template part<1>(i), s, 0, 0, 0);
+      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q.template part<0>(i), s, 0, 0, 0);
+    }
+    return s;
+  } else if constexpr (sizeof(T) == 2) {
     f32x16_t s = {};
 #pragma unroll
     for (int i = 0; i < D / 16; ++i) {
@@ -267,7 +322,32 @@ template <typename T, int D> struct State {
 template <typename T, int D, bool TWO, typename L = TileLayout<T, D>>
 __device__ __forceinline__ void values32(const unsigned char *sv, int key0, const f32x16_t &p, State<T, D> &st) {
   const int lane = threadIdx.x & (kWave - 1), half = lane >> 5;
-  if constexpr (sizeof(T) == 2) {
+  if constexpr (std::is_same_v<T, wide_t>) {
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      bf16x8_t pf[3];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        float y[3];
+        split<3>(p[8 * s + e], y);
+#pragma unroll
+        for (int x = 0; x < 3; ++x) pf[x][e] = (__bf16)y[x];
+      }
+#pragma unroll
+      for (int d = 0; d < D / 32; ++d) {
+        union { s16x4_t h[2]; bf16x8_t v; } vf;
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {  // (as below)
+          const int r = key0 + 16 * s + 8 * x + 4 * half + ((lane & 15) >> 2);
+          const int c = d * 4 + ((lane & 31) >> 4) * 2 + ((lane & 3) >> 1);
+          const int at = r * L::bytes + ((c ^ L::swz_v(r)) << 4) + (lane & 1) * 8;
+          vf.h[x] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((SMALLKV_LDS s16x4_t *)(sv + at));
+        }
+#pragma unroll
+        for (int x = 2; x >= 0; --x) st.o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf.v, pf[x], st.o[d], 0, 0, 0);
+      }
+    }
+  } else if constexpr (sizeof(T) == 2) {
     const bf16x2_t ones = {(__bf16)1.0f, (__bf16)1.0f};
     float sum = 0.0f;
 #pragma unroll

@@ -11,6 +11,15 @@
 
 namespace smallkv {
 
+// fp32 queries over rows that bf16 holds exactly (a packed cache's): both products run on bf16
+// operands, the queries and the probabilities in three bf16 parts each, which together hold
+// what fp32 holds.
+struct wide_t {
+  float x;
+};
+template <> struct elem<wide_t> : elem<float> {};
+template <int D> struct TileLayout<wide_t, D> : TileLayout<bf16_t, D> {};
+
 constexpr int kBlock = 32;  // elements that share a scale
 
 // The scales of one layer: a row has head_dim / 32 bytes.  Strides in rows' scales.

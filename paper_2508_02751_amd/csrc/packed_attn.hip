@@ -11,12 +11,12 @@ namespace smallkv {
 namespace {
 
 // A thread's share of the pieces (16 bytes of codes) of tiles of BN rows of keys and
-// values.  The page of the lane's row is looked up a tile ahead, as in Loader.
-template <typename T, int D, int F, int BN, int NT> struct Unpacker {
-  using L = TileLayout<T, D>;
+// values, which go to LDS in bf16.  The page of the lane's row is looked up a tile ahead, as in Loader.
+template <int D, int F, int BN, int NT> struct Unpacker {
+  using L = TileLayout<bf16_t, D>;
   static constexpr int P = D * F / 128, E = 128 / F;        // pieces of a row, elements of a piece
   static constexpr int kAll = 2 * BN * P, N = (kAll + NT - 1) / NT;
-  static constexpr int O = E * (int)sizeof(T) / 16;         // 16-byte pieces that it becomes
+  static constexpr int O = E / 8;                           // 16-byte pieces that it becomes
   const int32_t *pages;
   int len, page;
   uint4 w[N];
@@ -63,13 +63,13 @@ template <typename T, int D, int F, int BN, int NT> struct Unpacker {
 #pragma unroll
       for (int o = 0; o < O; ++o)
         *reinterpret_cast<uint4 *>(row + (((p * O + o) ^ z) << 4)) =
-            unpack16<T, F>(reinterpret_cast<const uint32_t *>(&w[j]), o, scale_of(s[j]));
+            unpack16<bf16_t, F>(reinterpret_cast<const uint32_t *>(&w[j]), o, scale_of(s[j]));
     }
   }
 };
 
 template <typename T, int D, int F, int NW, int BN>
-__global__ __launch_bounds__(NW * kWave, sizeof(T) * D == 512 ? 1 : 2) void packed_many(AttnArgs a) {
+__global__ __launch_bounds__(NW * kWave, 2) void packed_many(AttnArgs a) {
   using L = TileLayout<T, D>;
   constexpr int BM = NW * 32, kBuf = BN * L::bytes;
   __shared__ __align__(16) unsigned char k0[kBuf], v0[kBuf], k1[kBuf], v1[kBuf];
@@ -80,12 +80,19 @@ __global__ __launch_bounds__(NW * kWave, sizeof(T) * D == 512 ? 1 : 2) void pack
   const bool idle = w0 >= w.t.rows;
   const int highest = w.t.s.len - w.t.s.n_new + min(w0 + 31, w.t.rows - 1) / a.g;  // of the wave's rows
   QFrag<T, D> q;
-  q.load(a.q + (w.token * a.q_token + w.head * a.q_head) * (int64_t)sizeof(T), (threadIdx.x & (kWave - 1)) >> 5);
+  const unsigned char *queries = a.q + (w.token * a.q_token + w.head * a.q_head) * (int64_t)sizeof(T);
+  const int half = (threadIdx.x & (kWave - 1)) >> 5;
+  if constexpr (sizeof(T) == 4) {
+    __shared__ bf16x8_t parts[NW][QFrag<T, D>::kLds ? QFrag<T, D>::kLds : 1][kWave];
+    q.load(queries, half, &parts[wave][0][0]);
+  } else {
+    q.load(queries, half);
+  }
   State<T, D> st;
   st.clear();
   constexpr uint64_t kAll = BN == 64 ? ~0ull : (1ull << (BN & 63)) - 1;
   int row = w.begin;
-  Unpacker<T, D, F, BN, NW * kWave> ld;
+  Unpacker<D, F, BN, NW * kWave> ld;
   ld.init(a, w.t.b, w.end);
   ld.lookup(a.kv, row);
   uint64_t valid = 0, next = 0;  // rows of the tile at `row`, and of the one after it
@@ -131,7 +138,7 @@ __global__ __launch_bounds__(NW * kWave, sizeof(T) * D == 512 ? 1 : 2) void pack
     if (full) now = advance(odd ? k0 : k1, odd ? v0 : v1);
     full = true;
     if (min(row + BN, w.end) - 1 > w.first_own)
-      taken |= __syncthreads_or(take_out<T, BN * L::C>(sv, threadIdx.x, NW * kWave));
+      taken |= __syncthreads_or(take_out<bf16_t, BN * L::C>(sv, threadIdx.x, NW * kWave));
     if (!idle) masked_tile<T, D, BN, false>(st, q, sk, sv, row, w.own, highest, now, a.scale2, a.scale2_lo);
     row += BN;
     odd = !odd;
@@ -194,19 +201,6 @@ template <int D, int F> struct ValueTile {
   static constexpr int bytes = 2 * D, kLow = X::R == 8 ? 0 : X::R == 16 ? 1 : 2;
   __device__ __forceinline__ static int swz(int r) { return (D == 128 ? r & 7 : r >> 1 & 3) << 1 | (r >> kLow & 1); }
 };
-
-// fp32 as a sum of three bf16 numbers (exactly, but for what lies below 2^-133), or as two
-// with an error of 2^-17 of it; infinities and NaN in the first.
-template <int PARTS> __device__ __forceinline__ void split(float x, float (&y)[PARTS]) {
-  y[0] = bf16_hi(__float_as_uint(x));
-  float rest = fabsf(x) <= 3.402823466e38f ? x - y[0] : 0.0f;
-#pragma unroll
-  for (int i = 1; i + 1 < PARTS; ++i) {
-    y[i] = bf16_hi(__float_as_uint(rest));
-    rest -= y[i];
-  }
-  if (PARTS > 1) y[PARTS - 1] = rest;
-}
 
 // Workgroups go to the XCDs, each with an L2 of its own, in turn: the kv heads of a unit, whose
 // rows share lines of memory where a page holds [row][head], follow each other on one.
@@ -524,7 +518,7 @@ template <typename T, int D, int F> hipError_t launch_typed(AttnArgs a, const At
   const MergeShape m = merge_shape<D>(a, p);
   const dim3 grid((p.few ? (p.units + kXcds - 1) / kXcds * kXcds : p.units) * a.hkv), few(p.waves * kWave);
   if (!p.few)
-    hipLaunchKernelGGL((packed_many<T, D, F, kAttnWaves, h ? 64 : 32>), grid, dim3(kAttnWaves * kWave), 0, st, a);
+    hipLaunchKernelGGL((packed_many<std::conditional_t<h, bf16_t, wide_t>, D, F, kAttnWaves, h || D == 64 ? 64 : 32>), grid, dim3(kAttnWaves * kWave), 0, st, a);
   else if (p.rows == 16)
     hipLaunchKernelGGL((p.waves == 8 ? packed_few<T, D, F, 1, 8> : packed_few<T, D, F, 1, 4>), grid, few, 0, st, a);
   else if constexpr (h)
