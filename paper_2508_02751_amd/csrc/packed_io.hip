@@ -111,33 +111,64 @@ template <int F> struct Codes {
   }
 };
 
-template <typename T> __device__ __forceinline__ void load8(const unsigned char *row, int e, float (&x)[8]) {
-  const uint4 *p = reinterpret_cast<const uint4 *>(row + e * (int)sizeof(T));
-  elem<T>::unpack(p[0], x);
-  if constexpr (sizeof(T) == 4) elem<T>::unpack(p[1], x + 4);
-}
+// 8 elements of a row as they are in memory.
+template <typename T> struct Raw8 {
+  u32x4_t w[sizeof(T) / 2];
+  __device__ __forceinline__ void load(const unsigned char *row, int e) {
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) w[i] = reinterpret_cast<const u32x4_t *>(row + e * (int)sizeof(T))[i];
+  }
+  __device__ __forceinline__ void get(float (&x)[8]) const {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if constexpr (sizeof(T) == 4)
+        x[i] = __uint_as_float(w[i / 4][i % 4]);
+      else
+        x[i] = i % 2 ? bf16_hi(w[0][i / 2]) : bf16_lo(w[0][i / 2]);
+    }
+  }
+};
 template <typename T> __device__ __forceinline__ void store8(unsigned char *row, int e, const float (&x)[8]) {
-  uint4 w[sizeof(T) / 2];
-  uint32_t *u = reinterpret_cast<uint32_t *>(w);
+  Raw8<T> r;
 #pragma unroll
   for (int i = 0; i < (int)sizeof(T) * 2; ++i) {
     if constexpr (sizeof(T) == 4)
-      u[i] = __float_as_uint(x[i]);
+      r.w[i / 4][i % 4] = __float_as_uint(x[i]);
     else
-      u[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t{x[2 * i], x[2 * i + 1]}), bf16x2_t));
+      r.w[0][i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t{x[2 * i], x[2 * i + 1]}), bf16x2_t));
   }
 #pragma unroll
-  for (int i = 0; i < (int)sizeof(T) / 2; ++i) reinterpret_cast<uint4 *>(row + e * (int)sizeof(T))[i] = w[i];
+  for (int i = 0; i < (int)sizeof(T) / 2; ++i) reinterpret_cast<u32x4_t *>(row + e * (int)sizeof(T))[i] = r.w[i];
 }
 
-// HALF pairs (j, j + rot/2) whose halves are whole groups of 8, the same at any rot/2, or
-// neighbours.
-enum { kHalf = 0, kHalfScalar = 1, kInterleaved = 2 };
+// HALF pairs (j, j + rot/2) of a head that turns whole, the same where halves are whole groups
+// of 8, at any rot/2, or neighbours.
+enum { kWhole = 0, kHalf = 1, kHalfScalar = 2, kInterleaved = 3 };
 
-// Elements e .. e + 7 of a head (x) turned: cs[j] are cosine and sine of pair j.
-template <typename T, int FORM, typename R, typename CS>
+// The elements half a head away: of the lane 8 (128 elements) or 4 (64) further in the head's.
+template <typename T, int D> __device__ __forceinline__ Raw8<T> other_half(const Raw8<T> &x) {
+  Raw8<T> y;
+#pragma unroll
+  for (int i = 0; i < (int)sizeof(T) / 2; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      int w = (int)x.w[i][j];
+      if (D == 128) {
+        w = __builtin_amdgcn_update_dpp(w, w, 0x128, 0xf, 0xf, false);  // rotated by 8 of 16 lanes
+      } else {
+        w = __builtin_amdgcn_update_dpp(w, w, 0x141, 0xf, 0xf, false);  // 8 lanes mirrored,
+        w = __builtin_amdgcn_update_dpp(w, w, 0x1b, 0xf, 0xf, false);   // then 4
+      }
+      y.w[i][j] = (uint32_t)w;
+    }
+  return y;
+}
+
+// Elements e .. e + 7 of a head (x) turned: cs[j] are cosine and sine of pair j, other the
+// pairs' other halves (kWhole; kHalf, e < rot).
+template <typename T, int D, int FORM, typename R, typename CS>
 __device__ __forceinline__ void turn8(const unsigned char *row, int e, int rot, const CS *cs, const float (&x)[8],
-                                      R (&y)[8]) {
+                                      const Raw8<T> &partner, R (&y)[8]) {
   const int half = rot / 2;
   if (FORM == kInterleaved) {
 #pragma unroll
@@ -151,8 +182,16 @@ __device__ __forceinline__ void turn8(const unsigned char *row, int e, int rot, 
     return;
   }
   float other[8];
-  if (FORM == kHalf) {
-    if (e < rot) load8<T>(row, e < half ? e + half : e - half, other);
+  if (FORM != kHalfScalar) partner.get(other);
+  if (FORM == kWhole) {
+    const bool low = e < D / 2;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const CS r = cs[(e & (D / 2 - 1)) + i];
+      const R u = x[i], v = other[i];
+      y[i] = u * r.x + (low ? -v : v) * r.y;
+    }
+    return;
   }
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
@@ -160,79 +199,109 @@ __device__ __forceinline__ void turn8(const unsigned char *row, int e, int rot, 
     const bool low = at < half, turns = at < rot;
     if (FORM == kHalfScalar) other[i] = turns ? elem<T>::load1(row, low ? at + half : at - half) : 0.0f;
     const CS r = cs[turns ? (low ? at : at - half) : half];
-    const R u = x[i], v = FORM == kHalf && e >= rot ? 0.0f : other[i];
+    const R u = x[i], v = other[i];
     // x' = x cos - y sin of the lower half, y' = y cos + x sin of the upper one
     y[i] = !turns ? u : low ? u * r.x - v * r.y : u * r.x + v * r.y;
   }
 }
 
-template <typename T, int D, int F, int FORM, int TOK>
-__global__ __launch_bounds__(256) void append_packed(PackArgs a) {
+// A token to a workgroup, NI items (8 elements of a head) to a thread; blockIdx.y: slices of the
+// token's items.  The rows are requested first, before anything is known of the token.  A wave's
+// items are whole heads, so that queries may be turned in place.
+template <typename T, int D, int F, int FORM, int NI> __global__ __launch_bounds__(256) void append_packed(PackArgs a) {
   constexpr int W = D / 8;  // lanes of a head
-  __shared__ double2 cs[TOK][D / 2 + 1];
-  __shared__ float2 csf[TOK][D / 2 + 1];
+  __shared__ double2 cs[D / 2 + 1];
+  __shared__ float2 csf[D / 2 + 1];
   struct Where {
     int64_t row, scale;  // the cache row's offsets for head 0 (row: or -1)
-    int token, pos, seq, cached;
+    int in, pos, seq, cached;
   };
-  __shared__ Where where[TOK];
-  const int lane = threadIdx.x & (kWave - 1);
+  __shared__ Where where;
+  const int lane = threadIdx.x & (kWave - 1), t = blockIdx.x;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  for (int i = wave; i < TOK; i += 4) {
-    const int t = blockIdx.x * TOK + i;
-    // the token's sequence: the one that it is in, if any
+  const int heads = a.hq + 2 * a.hk;
+  // The item's head and first element; four lanes, a block, stay or go together.
+  auto item = [&](int n, int &h, int &e) {
+    const int i = (blockIdx.y * NI + n) * (int)blockDim.x + (int)threadIdx.x;
+    h = i / W;
+    e = (i & (W - 1)) * 8;
+    return h < heads;
+  };
+  auto source = [&](int h) {
+    if (h < a.hq) return a.q + t * a.q_token + h * a.q_head;
+    h -= a.hq;
+    return h < a.hk ? a.k + t * a.k_token + h * a.k_head : a.v + t * a.v_token + (h - a.hk) * a.v_head;
+  };
+  Raw8<T> own[NI], partner[NI];
+#pragma unroll
+  for (int n = 0; n < NI; ++n) {
+    int h, e;
+    own[n] = partner[n] = Raw8<T>{};
+    if (item(n, h, e)) {
+      const unsigned char *src = source(h);
+      own[n].load(src, e);
+      if (FORM == kHalf && e < a.rot && h < a.hq + a.hk)
+        partner[n].load(src, e < a.rot / 2 ? e + a.rot / 2 : e - a.rot / 2);
+    }
+  }
+  // The first wave finds the token's sequence, row and place; a lane turns the angle of a pair, in
+  // another wave where positions are given.
+  const double freq = lane < a.rot / 2 ? a.freq[lane] : 0.0;
+  int pos = a.positions ? a.positions[t] : 0;
+  if (wave == 0) {
     int b = -1;
+    Seq s{0, 0, 0};
     for (int b0 = 0; b0 < a.c.batch; b0 += kWave) {
-      bool in = false;
-      if (b0 + lane < a.c.batch) {
-        const Seq s = sequence(a.c, b0 + lane, a.kv.cap);
-        in = t >= s.first && t < s.first + s.n_new;
-      }
-      const uint64_t m = __ballot(in);
+      Seq x{0, 0, 0};
+      if (b0 + lane < a.c.batch) x = sequence(a.c, b0 + lane, a.kv.cap);
+      const uint64_t m = __ballot(t >= x.first && t < x.first + x.n_new);
       if (m) {
-        b = b0 + __ffsll((long long)m) - 1;
+        const int l = __builtin_amdgcn_readfirstlane(__ffsll((long long)m) - 1);
+        b = b0 + l;
+        s = Seq{__builtin_amdgcn_readlane(x.first, l), __builtin_amdgcn_readlane(x.n_new, l),
+                __builtin_amdgcn_readlane(x.len, l)};
         break;
       }
     }
-    if (lane == 0) {
-      Where w{-1, 0, -1, 0, 0, 0};
-      if (b >= 0 && t < a.c.n_tokens) {
-        const Seq s = sequence(a.c, b, a.kv.cap);
-        const int row = s.len - s.n_new + (t - s.first);
-        w.token = t;
-        w.pos = a.positions ? a.positions[t] : row;
-        w.seq = b;
-        w.cached = row;
-        if (row >= 0) {
-          const int page = row_page(a.kv, b, row);
-          w.row = page_offset(a.kv, page, row);
-          if (w.row >= 0) w.scale = scale_offset<D>(a.sc, a.kv, page, row, 0);
-        }
+    Where w{-1, 0, 0, 0, 0, 0};
+    if (b >= 0) {
+      const int row = s.len - s.n_new + (t - s.first);
+      if (!a.positions) pos = row;
+      w.in = 1;
+      w.pos = pos;
+      w.seq = b;
+      w.cached = row;
+      if (row >= 0) {
+        const int page = row_page(a.kv, b, row);
+        w.row = page_offset(a.kv, page, row);
+        if (w.row >= 0) w.scale = scale_offset<D>(a.sc, a.kv, page, row, 0);
       }
-      where[i] = w;
     }
+    if (lane == 0) where = w;
   }
-  __syncthreads();
-  for (int i = threadIdx.x; i < TOK * (a.rot / 2); i += 256) {
-    const int tok = TOK == 1 ? 0 : i / (a.rot / 2), j = i - tok * (a.rot / 2);
+  if (wave == (a.positions ? 1 : 0) && lane < a.rot / 2) {
     double co, si;
-    cos_sin((double)where[tok].pos * a.freq[j], co, si);
-    cs[tok][j] = make_double2((double)a.amplitude * co, (double)a.amplitude * si);
-    csf[tok][j] = make_float2((float)cs[tok][j].x, (float)cs[tok][j].y);
+    cos_sin((double)pos * freq, co, si);
+    co *= (double)a.amplitude;
+    si *= (double)a.amplitude;
+    cs[lane] = make_double2(co, si);
+    csf[lane] = make_float2((float)co, (float)si);
   }
   __syncthreads();
-  const int heads = a.hq + 2 * a.hk, chunks = (heads * W + kWave - 1) / kWave;
-  for (int i = wave; i < TOK * chunks; i += 4) {
-    const int tok = TOK == 1 ? 0 : i / chunks, item = (i - tok * chunks) * kWave + lane;
-    const int h = item / W, e = (item & (W - 1)) * 8;
-    const Where at = where[tok];
-    if (at.token < 0 || h >= heads) continue;  // (whole heads: four lanes stay or go together)
+  const Where at = where;
+  if (!at.in) return;
+#pragma unroll
+  for (int n = 0; n < NI; ++n) {
+    int h, e;
+    if (!item(n, h, e)) continue;
+    const unsigned char *src = source(h);
+    float x[8];
+    own[n].get(x);
+    if (FORM == kWhole) partner[n] = other_half<T, D>(own[n]);
     if (h < a.hq) {
-      const unsigned char *src = a.q + at.token * a.q_token + h * a.q_head;
-      float x[8], y[8];
-      load8<T>(src, e, x);
-      turn8<T, FORM, float>(src, e, a.rot, csf[tok], x, y);
-      store8<T>(a.q_out + at.token * a.o_token + h * a.o_head, e, y);
+      float y[8];
+      turn8<T, D, FORM, float>(src, e, a.rot, csf, x, partner[n], y);
+      store8<T>(a.q_out + t * a.o_token + h * a.o_head, e, y);
       continue;
     }
     const bool value = h >= a.hq + a.hk;
@@ -240,14 +309,11 @@ __global__ __launch_bounds__(256) void append_packed(PackArgs a) {
     if (a.row_pos && !value && e == 0 && at.cached >= 0 && at.cached < a.pos_rows)
       a.row_pos[at.seq * a.pos_stride + kh * a.pos_rows + at.cached] = at.pos;
     if (at.row < 0) continue;
-    const unsigned char *src = value ? a.v + at.token * a.v_token + kh * a.v_head : a.k + at.token * a.k_token + kh * a.k_head;
-    float x[8];
-    load8<T>(src, e, x);
     if (!value && a.rot > 0) {
       double y[8];
-      turn8<T, FORM, double>(src, e, a.rot, cs[tok], x, y);
+      turn8<T, D, FORM, double>(src, e, a.rot, cs, x, partner[n], y);
 #pragma unroll
-      for (int n = 0; n < 8; ++n) x[n] = round_to_odd(y[n]);
+      for (int i = 0; i < 8; ++i) x[i] = round_to_odd(y[i]);
     }
     const Codes<F> c(x);
     unsigned char *dst = (value ? a.cv : a.ck) + at.row + (((uint64_t)kh * a.kv.head_stride) << 4);
@@ -298,15 +364,24 @@ template <typename T, int D, int F> __global__ __launch_bounds__(256) void read_
   }
 }
 
+template <typename T, int D, int F, int FORM, int NI> void launch_items(const PackArgs &a, hipStream_t st) {
+  const int items = (a.hq + 2 * a.hk) * (D / 8);
+  const int threads = std::max(std::min((items + 63) / 64 * 64, 256), 128);
+  const dim3 grid(a.c.n_tokens, (items + threads * NI - 1) / (threads * NI));
+  hipLaunchKernelGGL((append_packed<T, D, F, FORM, NI>), grid, dim3(threads), 0, st, a);
+}
 template <typename T, int D, int F, int FORM> void launch_tokens(const PackArgs &a, hipStream_t st) {
-  if (a.c.n_tokens < 2048)
-    hipLaunchKernelGGL((append_packed<T, D, F, FORM, 1>), dim3(a.c.n_tokens), dim3(256), 0, st, a);
+  // few tokens or few heads: an item per thread, the shortest chain; else three, for which the
+  // sines and cosines are found once (4000 tokens of 36 heads of 128 each of two sequences: 41 us
+  // with one, 35 with three; 3000 of 18 heads of 64: 8.2 and 8.9)
+  if (a.c.n_tokens < 512 || (a.hq + 2 * a.hk) * (D / 8) <= 256)
+    launch_items<T, D, F, FORM, 1>(a, st);
   else
-    hipLaunchKernelGGL((append_packed<T, D, F, FORM, 4>), dim3((a.c.n_tokens + 3) / 4), dim3(256), 0, st, a);
+    launch_items<T, D, F, FORM, 3>(a, st);
 }
 template <typename T, int D, int F> void launch_form(const PackArgs &a, int layout, hipStream_t st) {
   (layout == SMALLKV_ROPE_INTERLEAVED ? launch_tokens<T, D, F, kInterleaved>
-   : a.rot % 16 == 0 ? launch_tokens<T, D, F, kHalf> : launch_tokens<T, D, F, kHalfScalar>)(a, st);
+   : a.rot == D ? launch_tokens<T, D, F, kWhole> : a.rot % 16 == 0 ? launch_tokens<T, D, F, kHalf> : launch_tokens<T, D, F, kHalfScalar>)(a, st);
 }
 template <typename T, int D, int F> void launch_read(const ReadArgs &a, dim3 grid, hipStream_t st) {
   hipLaunchKernelGGL((read_packed<T, D, F>), grid, dim3(256), 0, st, a);
