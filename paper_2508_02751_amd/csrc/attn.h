@@ -457,7 +457,7 @@ __device__ __forceinline__ void softmax_step(State<T, D> &st, f32x16_t (&s)[NB],
 }
 
 // A tile that every row of the wave sees whole.
-template <typename T, int D, int BN>
+template <typename T, int D, int BN, typename L = TileLayout<T, D>>
 __device__ __forceinline__ void full_tile(State<T, D> &st, const QFrag<T, D> &q, const unsigned char *sk,
                                           const unsigned char *sv, float c, float c_lo) {
   f32x16_t s[BN / 32];
@@ -465,12 +465,12 @@ __device__ __forceinline__ void full_tile(State<T, D> &st, const QFrag<T, D> &q,
   for (int b = 0; b < BN / 32; ++b) s[b] = logits32<T, D>(sk, 32 * b, q);
   softmax_step<T, D>(st, s, c, c_lo);
 #pragma unroll
-  for (int b = 0; b < BN / 32; ++b) values32<T, D, false>(sv, 32 * b, s[b], st);
+  for (int b = 0; b < BN / 32; ++b) values32<T, D, false, L>(sv, 32 * b, s[b], st);
 }
 
 // Any other, 32 keys at a time.  own: the lane's own row; highest: of the wave's; valid:
 // bit t set iff key row0 + t exists.
-template <typename T, int D, int BN, bool TWO>
+template <typename T, int D, int BN, bool TWO, typename L = TileLayout<T, D>>
 __device__ __forceinline__ void masked_tile(State<T, D> &st, const QFrag<T, D> &q, const unsigned char *sk,
                                             const unsigned char *sv, int row0, int own, int highest,
                                             uint64_t valid, float c, float c_lo) {
@@ -485,7 +485,7 @@ __device__ __forceinline__ void masked_tile(State<T, D> &st, const QFrag<T, D> &
       s[0][i] = ok ? s[0][i] : -INFINITY;
     }
     softmax_step<T, D>(st, s, c, c_lo);
-    values32<T, D, TWO>(sv, k0, s[0], st);
+    values32<T, D, TWO, L>(sv, k0, s[0], st);
   }
 }
 

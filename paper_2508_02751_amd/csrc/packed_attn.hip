@@ -10,10 +10,18 @@
 namespace smallkv {
 namespace {
 
+// Values of a tile in LDS as TileLayout has them, and neighbouring pieces exchanged so that a
+// piece of codes, which becomes two or four, is written without a conflict of banks.
+template <int D> struct MixedTile : TileLayout<bf16_t, D> {
+  __device__ __forceinline__ static int swz_v(int r) {
+    return D == 128 ? (r & 3) << 2 | (r & 3) : (r >> 1 & 1) << 2 | (r >> 1 & 3);
+  }
+};
+
 // A thread's share of the pieces (16 bytes of codes) of tiles of BN rows of keys and
 // values, which go to LDS in bf16.  The page of the lane's row is looked up a tile ahead, as in Loader.
 template <int D, int F, int BN, int NT> struct Unpacker {
-  using L = TileLayout<bf16_t, D>;
+  using L = MixedTile<D>;
   static constexpr int P = D * F / 128, E = 128 / F;        // pieces of a row, elements of a piece
   static constexpr int kAll = 2 * BN * P, N = (kAll + NT - 1) / NT;
   static constexpr int O = E / 8;                           // 16-byte pieces that it becomes
@@ -123,13 +131,13 @@ __global__ __launch_bounds__(NW * kWave, 2) void packed_many(AttnArgs a) {
   while (row < w.end) {
     now = advance(k1, v1);
     if (!(full = row + BN - 1 <= w.first_own && (now & kAll) == kAll)) break;
-    if (!idle) full_tile<T, D, BN>(st, q, k0, v0, a.scale2, a.scale2_lo);
+    if (!idle) full_tile<T, D, BN, MixedTile<D>>(st, q, k0, v0, a.scale2, a.scale2_lo);
     row += BN;
     if (row >= w.end) break;
     odd = true;
     now = advance(k0, v0);
     if (!(full = row + BN - 1 <= w.first_own && (now & kAll) == kAll)) break;
-    if (!idle) full_tile<T, D, BN>(st, q, k1, v1, a.scale2, a.scale2_lo);
+    if (!idle) full_tile<T, D, BN, MixedTile<D>>(st, q, k1, v1, a.scale2, a.scale2_lo);
     row += BN;
     odd = false;
   }
@@ -139,7 +147,7 @@ __global__ __launch_bounds__(NW * kWave, 2) void packed_many(AttnArgs a) {
     full = true;
     if (min(row + BN, w.end) - 1 > w.first_own)
       taken |= __syncthreads_or(take_out<bf16_t, BN * L::C>(sv, threadIdx.x, NW * kWave));
-    if (!idle) masked_tile<T, D, BN, false>(st, q, sk, sv, row, w.own, highest, now, a.scale2, a.scale2_lo);
+    if (!idle) masked_tile<T, D, BN, false, MixedTile<D>>(st, q, sk, sv, row, w.own, highest, now, a.scale2, a.scale2_lo);
     row += BN;
     odd = !odd;
   }
@@ -517,8 +525,11 @@ template <typename T, int D, int F> hipError_t launch_typed(AttnArgs a, const At
   constexpr bool h = sizeof(T) == 2;
   const MergeShape m = merge_shape<D>(a, p);
   const dim3 grid((p.few ? (p.units + kXcds - 1) / kXcds * kXcds : p.units) * a.hkv), few(p.waves * kWave);
+  using M = std::conditional_t<h, bf16_t, wide_t>;
+  constexpr int BN = h || D == 64 ? 64 : 32;
   if (!p.few)
-    hipLaunchKernelGGL((packed_many<std::conditional_t<h, bf16_t, wide_t>, D, F, kAttnWaves, h || D == 64 ? 64 : 32>), grid, dim3(kAttnWaves * kWave), 0, st, a);
+    hipLaunchKernelGGL((h && p.rows == 256 ? packed_many<M, D, F, h ? 8 : 4, BN> : packed_many<M, D, F, 4, BN>), grid,
+                       dim3(p.rows * 2), 0, st, a);
   else if (p.rows == 16)
     hipLaunchKernelGGL((p.waves == 8 ? packed_few<T, D, F, 1, 8> : packed_few<T, D, F, 1, 4>), grid, few, 0, st, a);
   else if constexpr (h)
@@ -526,8 +537,10 @@ template <typename T, int D, int F> hipError_t launch_typed(AttnArgs a, const At
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || !p.splits) return e;
   const int rows = (int)std::min<int64_t>(p.rows, (int64_t)a.c.max_new * a.g);
-  if (!p.few)
-    launch_join<T, D, kAttnWaves * 32>(a, p, m, rows, st);
+  if (p.rows == 256)
+    launch_join<T, D, 256>(a, p, m, rows, st);
+  else if (!p.few)
+    launch_join<T, D, 128>(a, p, m, rows, st);
   else if (p.rows == 16)
     launch_join<T, D, 16>(a, p, m, rows, st);
   else
@@ -549,8 +562,11 @@ AttnPlan plan_packed_attn(const smallkv_chunk_t &c, const smallkv_packed_t &kv, 
   const bool f32 = kv.dtype == SMALLKV_F32;
   // (fp32, up to four tiles of 16: 54 rows over 8 x 4096 and 32 x 2048 cached rows 34 and 48 us,
   // as many rows 38 and 57; bf16, 28 rows: 25 and 27, 23 and 32)
+  // Many rows, bf16: tiles of 256 where that leaves little of the last one empty: half as much
+  // to unpack (2 x 2048 tokens over 16384 rows of 8 kv heads of 128: 1144 us, 1189 in tiles of
+  // 128, in 4 bits 999 and 1109; 1200 rows of 8 sequences 596 and 579).
   p.few = rows <= (f32 ? 64 : 32);
-  p.rows = !p.few ? kAttnWaves * 32 : f32 || rows <= 16 ? 16 : 32;
+  p.rows = !p.few ? (rows >= 1536 && !f32 ? 256 : 128) : f32 || rows <= 16 ? 16 : 32;
   // no more tiles than this, whatever the sequences' lengths
   p.tiles = (int)std::min<int64_t>(c.batch * ceil_div(rows, p.rows), (int64_t)c.n_tokens * g / p.rows + c.batch);
   // Few rows: whole sequences where they are short, or make a workgroup for enough CUs and are
@@ -567,7 +583,7 @@ AttnPlan plan_packed_attn(const smallkv_chunk_t &c, const smallkv_packed_t &kv, 
   // the workgroups that run at once on 256 CUs, two on each; of 4 bits three (64 of 1024 - 4096
   // rows 32.7 us with two, 28.6 with three; in 8 bits 45.4 and 50.8)
   const bool three = p.rows == 16 && kv.dtype == SMALLKV_BF16 && kv.head_dim == 128 && kv.format == SMALLKV_MXFP4;
-  const int slots = std::max((three ? 768 : 512) / kv.n_heads, 1);
+  const int slots = std::max((three ? 768 : p.rows == 256 ? 256 : 512) / kv.n_heads, 1);
   const int round = p.few ? 32 * kFewWaves : kManyRound * kManyLeast;
   if (p.tiles < slots && c.max_len > round && !whole)
     p.splits = (int)std::min<int64_t>(slots, (int64_t)p.tiles * ceil_div(c.max_len, round));
