@@ -524,7 +524,7 @@ void launch_join(AttnArgs a, const AttnPlan &p, const MergeShape &m, int rows, h
 template <typename T, int D, int F> hipError_t launch_typed(AttnArgs a, const AttnPlan &p, hipStream_t st) {
   constexpr bool h = sizeof(T) == 2;
   const MergeShape m = merge_shape<D>(a, p);
-  const dim3 grid((p.few ? (p.units + kXcds - 1) / kXcds * kXcds : p.units) * a.hkv), few(p.waves * kWave);
+  const dim3 grid(p.units * a.hkv), few(p.waves * kWave);
   using M = std::conditional_t<h, bf16_t, wide_t>;
   constexpr int BN = h || D == 64 ? 64 : 32;
   if (!p.few)
@@ -588,6 +588,7 @@ AttnPlan plan_packed_attn(const smallkv_chunk_t &c, const smallkv_packed_t &kv, 
   if (p.tiles < slots && c.max_len > round && !whole)
     p.splits = (int)std::min<int64_t>(slots, (int64_t)p.tiles * ceil_div(c.max_len, round));
   p.units = std::max(p.tiles, p.splits);
+  if (p.few) p.units = (p.units + kXcds - 1) / kXcds * kXcds;
   if (p.splits) p.ws_bytes = kSpanBytes + (size_t)p.units * kv.n_heads * p.rows * (kv.head_dim + 2) * sizeof(float);
   return p;
 }
