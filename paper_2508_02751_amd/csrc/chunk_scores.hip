@@ -20,6 +20,9 @@
 //              one key's logits, and each wave streams its keys' rows, bound by
 //              reading K once.
 //
+// Keys of a packed cache (F: bits of a code) become bf16 or fp32 operands, exactly, as they
+// arrive; the rest is the same.
+//
 // Measured (MI355X, after a hundred calls, when the clock has settled: the first tens of
 // calls, of which the pairs of figures at the rules below are, take up to 15% more): 2048
 // tokens of 32 query heads of 64 over 16384 rows, bf16 (1.0e9 exponentials, 129 GFLOP)
@@ -28,7 +31,9 @@
 // of 14 heads over 8192 rows of 2 kv heads of 64, 74 us (SPLIT): latency, the vector units
 // busy 42%, the matrix cores 13%.  A token each of 64 sequences of 1024 - 4096 rows of 4 kv
 // heads of 128 (168 MB) 41 us, 4.1 TB/s; of 16 sequences over 82552 rows of 2 kv heads of
-// 64 (23 MB) 9.0 us: latency.
+// 64 (23 MB) 9.0 us: latency.  Packed: the former in 4 bits per kv head (22 MB and as much of
+// scores) 19 us, in 8 bits per query head (43 and 36 MB) 38 us, the latter in 4 bits (6 MB) 7.1 us:
+// latency; 1024 tokens of 32 query heads of 64 over 16384 rows in 8 bits 101 us, the exponentials.
 #include <algorithm>
 #include <type_traits>
 
@@ -425,7 +430,8 @@ __global__ __launch_bounds__(kNW * kWave, 2) void head_scores(ScoreArgs a) {
       a.out[at(n)] = old[n] + (n_tokens > 0 && exists >> in & 1u ? sums[n][threadIdx.x] : 0.0f);
 }
 
-template <typename T, int D, int F>
+// HEADS: packed caches, per query head; else as a.per_kv says (packed: per kv head).
+template <typename T, int D, int F, bool HEADS>
 __global__ __launch_bounds__(kNW * kWave, 2) void few_scores(ScoreArgs a) {
   constexpr bool kBf16 = sizeof(T) == 2;
   constexpr int kFrag = kBf16 ? D / 16 : D / 8;  // 16-byte pieces of a row per lane
@@ -487,6 +493,22 @@ __global__ __launch_bounds__(kNW * kWave, 2) void few_scores(ScoreArgs a) {
   auto load = [&](int at) { k.load(a, off, a.kv.table ? page : b, at, kvh, half); };
   load(key);
   for (int base = begin + wave * 32; base < end; base += step, key += step) {
+    // packed caches: the old scores are requested before the next keys' rows (per query head of
+    // one token: a half-wave holds, and writes, half of the heads).  (A token each of 64 sequences
+    // of 1024 - 4096 rows and 28 heads of 128 in 8 bits: 38 us, 96 with the old scores requested
+    // where they are added; of plain caches in fp32 the registers do not last for it.)
+    const bool per_kv = F ? !HEADS : a.per_kv, one = HEADS && s.n_new == 1;
+    const int64_t at0 = b * a.seq_stride + (per_kv ? kvh : kvh * a.g) * a.rows + key;
+    float old[HEADS ? 16 : 1];
+    if constexpr (F != 0) {
+      const bool adds = a.before && key < pos0 && key < end;
+#pragma unroll
+      for (int i = 0; i < (HEADS ? 16 : 1); ++i) {
+        const int r = 8 * (i / 4) + i % 4 + 4 * half;
+        old[i] = 0.0f;
+        if (adds && (HEADS ? one && r < a.g : half == 0)) old[i] = a.before[at0 + (HEADS ? r * a.rows : 0)];
+      }
+    }
     f32x16_t x = {};
 #pragma unroll
     for (int i = 0; i < kFrag; ++i) {
@@ -511,20 +533,26 @@ __global__ __launch_bounds__(kNW * kWave, 2) void few_scores(ScoreArgs a) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) p[i] = exists && key <= own[i] ? p[i] : 0.0f;
     }
-    if (a.per_kv) {
+    if (per_kv) {
       float sum = 0.0f;
 #pragma unroll
       for (int i = 0; i < 16; ++i) sum += p[i];
       sum = swap_halves_sum(sum);
-      if (half == 0 && inside) {
-        const int64_t at = b * a.seq_stride + kvh * a.rows + key;
-        a.out[at] = (a.before && key < pos0 ? a.before[at] : 0.0f) + sum;
+      if constexpr (F == 0) old[0] = half == 0 && inside && a.before && key < pos0 ? a.before[at0] : 0.0f;
+      if (half == 0 && inside) a.out[at0] = old[0] + sum;
+    } else if (one) {
+      if constexpr (HEADS) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int r = 8 * (i / 4) + i % 4 + 4 * half;
+          if (r < a.g && inside) a.out[at0 + r * a.rows] = old[i] + p[i];
+        }
       }
     } else {
       // rows of head j: j, j + g, j + 2g, ...
       for (int j = 0; j < a.g; ++j) {
         float sum = 0.0f;
-        if (s.n_new == 1) {
+        if (!HEADS && s.n_new == 1) {
 #pragma unroll
           for (int i = 0; i < 16; ++i) sum = j == 8 * (i / 4) + i % 4 + 4 * half ? p[i] : sum;
         } else {
@@ -556,7 +584,7 @@ void launch_typed(ScoreArgs a, int max_new, int max_len, hipStream_t st) {
     const int64_t rounds = ((int64_t)max_len + 127) / 128;
     const int64_t each = std::max<int64_t>(1, std::min<int64_t>(rounds, rounds * units / 512));
     a.pieces = (int)((rounds + each - 1) / each);
-    hipLaunchKernelGGL((few_scores<T, D, F>), dim3((unsigned)(a.pieces * units)), block, 0, st, a);
+    hipLaunchKernelGGL((F && !a.per_kv ? few_scores<T, D, F, F != 0> : few_scores<T, D, F, false>), dim3((unsigned)(a.pieces * units)), block, 0, st, a);
     return;
   }
   const unsigned heads = a.per_kv ? 1 : a.g;

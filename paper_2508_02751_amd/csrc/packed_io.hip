@@ -8,6 +8,12 @@
 //           that: rounded to odd (the last bit set where anything was cut off), comparisons
 //           with values of fewer bits and the next rounding see what the 64 bits would show.
 // read   -- the reverse, without the turn: 16 bytes of output per lane.
+//
+// Bound by memory.  Measured (MI355X): 21000 tokens of 32 + 2 x 8 heads of 128 in bf16 (461 MB
+// read and written) 88 us, 5.3 TB/s; 8000 of 28 + 2 x 4 heads 33 us; one token each of 64
+// sequences 5.6 us, a launch and a chain of dependent loads (sequence, page) beside which the
+// rows and angles are on their way.  Read: 4 x 20000 - 32768 rows of 32 heads of 64 from 8 bits
+// to bf16 (1.26 GB) 266 us, the rate of a large copy.
 #include <algorithm>
 
 #include "launch.h"
@@ -366,16 +372,18 @@ template <typename T, int D, int F> __global__ __launch_bounds__(256) void read_
 
 template <typename T, int D, int F, int FORM, int NI> void launch_items(const PackArgs &a, hipStream_t st) {
   const int items = (a.hq + 2 * a.hk) * (D / 8);
-  const int threads = std::max(std::min((items + 63) / 64 * 64, 256), 128);
+  const int threads = std::max(std::min((items + NI - 1) / NI + 63, 256) / 64 * 64, 128);
   const dim3 grid(a.c.n_tokens, (items + threads * NI - 1) / (threads * NI));
   hipLaunchKernelGGL((append_packed<T, D, F, FORM, NI>), grid, dim3(threads), 0, st, a);
 }
 template <typename T, int D, int F, int FORM> void launch_tokens(const PackArgs &a, hipStream_t st) {
-  // few tokens or few heads: an item per thread, the shortest chain; else three, for which the
-  // sines and cosines are found once (4000 tokens of 36 heads of 128 each of two sequences: 41 us
-  // with one, 35 with three; 3000 of 18 heads of 64: 8.2 and 8.9)
-  if (a.c.n_tokens < 512 || (a.hq + 2 * a.hk) * (D / 8) <= 256)
+  // few tokens: an item per thread, the shortest chain; else two or three, for which the sines
+  // and cosines are found once (4000 tokens of 36 heads of 128 each of two sequences: 41 us with
+  // one, 33 with three; 3000 of 18 heads of 64: 8.1 with one, 7.0 with two)
+  if (a.c.n_tokens < 512)
     launch_items<T, D, F, FORM, 1>(a, st);
+  else if ((a.hq + 2 * a.hk) * (D / 8) <= 256)
+    launch_items<T, D, F, FORM, 2>(a, st);
   else
     launch_items<T, D, F, FORM, 3>(a, st);
 }
