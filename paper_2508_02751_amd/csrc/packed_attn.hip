@@ -476,11 +476,15 @@ __global__ __launch_bounds__(NW * kWave, 2) void packed_few(AttnArgs a) {
 
 // Joins the records of a tile's spans: four elements of a row per lane, a row's spans dealt to
 // `parts` groups of such lanes, which each take theirs in one pass with the running maximum,
-// scale their sums to the row's maximum and add them up in LDS.
-template <typename T, int D, int BM> __global__ __launch_bounds__(kMaxParts * (D / 4)) void join_spans(AttnArgs a) {
+// scale their sums to the row's maximum and add them up in LDS.  Eight parts at most: workgroups
+// of 256 threads start sooner than larger ones (128 spans of a token of 28 heads: 5.6 us, with 32
+// parts 9.2, with four 7.1; 24 spans of 16 sequences 4.6, 7.5 and 4.2).
+constexpr int kJoinParts = 8, kJoinThreads = 256;
+
+template <typename T, int D, int BM> __global__ __launch_bounds__(kJoinThreads) void join_spans(AttnArgs a) {
   constexpr int W = D / 4;  // lanes of a row
-  __shared__ f32x4_t so[kMaxParts * W];
-  __shared__ float2 sml[kMaxParts];
+  __shared__ f32x4_t so[kJoinThreads];
+  __shared__ float2 sml[kJoinThreads / W];
   const int kvh = blockIdx.x % a.hkv, span = *a.span;
   const Lanes<BM> lanes(a);
   Tile t;
@@ -536,15 +540,15 @@ template <typename T, int D, int BM> __global__ __launch_bounds__(kMaxParts * (D
 }
 
 // rows: of a tile that there can be.
-template <typename T, int D, int BM>
-void launch_join(AttnArgs a, const AttnPlan &p, const MergeShape &m, int rows, hipStream_t st) {
-  hipLaunchKernelGGL((join_spans<T, D, BM>), dim3(p.tiles * a.hkv, ceil_div(rows, m.n_rows)), dim3(m.threads), 0, st,
-                     a);
+template <typename T, int D, int BM> void launch_join(const AttnArgs &a, const AttnPlan &p, int rows, hipStream_t st) {
+  const dim3 grid(p.tiles * a.hkv, ceil_div(rows, kJoinThreads / (D / 4) / a.parts));
+  hipLaunchKernelGGL((join_spans<T, D, BM>), grid, dim3(kJoinThreads), 0, st, a);
 }
 
 template <typename T, int D, int F> hipError_t launch_typed(AttnArgs a, const AttnPlan &p, hipStream_t st) {
   constexpr bool h = sizeof(T) == 2;
-  const MergeShape m = merge_shape<D>(a, p);
+  merge_shape<D>(a, p);
+  a.parts = std::min(a.parts, kJoinParts);
   const dim3 grid(p.units * a.hkv), few(p.waves * kWave);
   using M = std::conditional_t<h, bf16_t, wide_t>;
   constexpr int BN = h || D == 64 ? 64 : 32;
@@ -559,13 +563,13 @@ template <typename T, int D, int F> hipError_t launch_typed(AttnArgs a, const At
   if (e != hipSuccess || !p.splits) return e;
   const int rows = (int)std::min<int64_t>(p.rows, (int64_t)a.c.max_new * a.g);
   if (p.rows == 256)
-    launch_join<T, D, 256>(a, p, m, rows, st);
+    launch_join<T, D, 256>(a, p, rows, st);
   else if (!p.few)
-    launch_join<T, D, 128>(a, p, m, rows, st);
+    launch_join<T, D, 128>(a, p, rows, st);
   else if (p.rows == 16)
-    launch_join<T, D, 16>(a, p, m, rows, st);
+    launch_join<T, D, 16>(a, p, rows, st);
   else
-    launch_join<T, D, 32>(a, p, m, rows, st);
+    launch_join<T, D, 32>(a, p, rows, st);
   return hipGetLastError();
 }
 
