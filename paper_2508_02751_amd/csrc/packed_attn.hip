@@ -596,12 +596,13 @@ AttnPlan plan_packed_attn(const smallkv_chunk_t &c, const smallkv_packed_t &kv, 
   p.tiles = (int)std::min<int64_t>(c.batch * ceil_div(rows, p.rows), (int64_t)c.n_tokens * g / p.rows + c.batch);
   // Few rows: whole sequences where they are short, or make a workgroup for enough CUs and are
   // not long; else spans, and a join.  (28 query and 4 kv heads of 128 in 8 bits, us: one
-  // sequence of 512 rows 8.7, in spans 10.6; of 1024 13.0 and 11.1; 16 of 1024 rows 13.4 and
-  // 15.4, 64 16.0 and 21.6; 24 of 2048 20.8 and 19.8, 48 22.4 and 28.0; 32 of 4096 36.0 and
-  // 35.9, 48 41.8 and 48.9; 40 of 1024 - 4096 34.9 and 29.5, 64 42.2 and 45.9.)
-  const int64_t groups = (int64_t)p.tiles * kv.n_heads;
+  // sequence of 512 rows 9.6, in spans 10.8; of 1024 12.6 and 11.3; 16 of 1024 rows 13.3 and
+  // 14.1, 48 13.9 and 19.5; 24 of 2048 20.6 and 19.9, 48 22.5 and 28.4; 32 of 4096 35.9 and
+  // 36.0, 48 41.9 and 49.9; 40 of 1024 - 4096 34.7 and 29.6, 48 36.5 and 36.7.  Heads of 64 in
+  // 4 bits: one sequence of 1024 rows 8.0 and 10.1, 32 of 2048 11.9 and 12.0.)
+  const int64_t groups = (int64_t)p.tiles * kv.n_heads, length = (int64_t)c.max_len * kv.head_dim / 128;
   const bool whole = p.few && p.tiles <= c.batch &&
-                     (c.max_len <= 512 || (c.max_len <= 1024 && groups >= 32) || (c.max_len <= 4096 && groups >= 160));
+                     (length <= 512 || (length <= 1024 && groups >= 64) || (c.max_len <= 4096 && groups >= 160));
   // eight waves where that is one workgroup per CU (64 of 1024 - 4096 rows 41.8 us, with four
   // 50.0; 90 of 2048 49.7 and 41.7)
   p.waves = whole && c.max_len > 512 && groups <= 256 ? 8 : kFewWaves;
