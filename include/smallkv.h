@@ -668,7 +668,9 @@ typedef enum {
  * blocks at k_scale + page * scale_page_stride + h * scale_head_stride + (r % page_rows) *
  * scale_row_stride (v alike).  Codes and their strides are multiples of 16 bytes, scales and
  * theirs of head_dim / 32.  The other fields as in smallkv_cache_t; dtype is that of the
- * queries, of the rows to append and of the outputs. */
+ * queries, of the rows to append and of the outputs.  smallkv_append_packed writes scales from
+ * 27 to 246 (MXFP4: 252), with which every element is a normal number of bf16 or 0, and 255;
+ * outputs that see rows with others are unspecified. */
 typedef struct {
   void *k, *v;
   uint8_t *k_scale, *v_scale;
@@ -698,7 +700,8 @@ int smallkv_append_packed(const smallkv_chunk_t *chunk, const smallkv_packed_t *
 int smallkv_read_packed(const smallkv_packed_t *from, const smallkv_cache_t *to, int32_t batch,
                         int32_t max_len, const int32_t *begin, const int32_t *len, void *stream);
 
-/* smallkv_chunk_attn over a packed cache.  bf16 models: the probabilities keep 16 bits in the
+/* smallkv_chunk_attn over a packed cache (with few rows its units, sequences or spans of them, are
+ * counted in eights towards what a launch can count).  bf16 models: the probabilities keep 16 bits in the
  * product with V with max_new tokens of at most 32 (token, query head) rows per kv head,
  * else 8, as there. */
 int smallkv_chunk_attn_packed(const smallkv_chunk_t *chunk, const smallkv_packed_t *cache,
