@@ -596,7 +596,7 @@ AttnPlan plan_packed_attn(const smallkv_chunk_t &c, const smallkv_packed_t &kv, 
   p.tiles = (int)std::min<int64_t>(c.batch * ceil_div(rows, p.rows), (int64_t)c.n_tokens * g / p.rows + c.batch);
   // Few rows: whole sequences where they are short, or make a workgroup for enough CUs and are
   // not long; else spans, and a join.  (28 query and 4 kv heads of 128 in 8 bits, us: one
-  // sequence of 512 rows 9.6, in spans 10.8; of 1024 12.6 and 11.3; 16 of 1024 rows 13.3 and
+  // sequence of 512 rows 9.0, in spans 10.8; of 1024 12.6 and 11.3; 16 of 1024 rows 13.3 and
   // 14.1, 48 13.9 and 19.5; 24 of 2048 20.6 and 19.9, 48 22.5 and 28.4; 32 of 4096 35.9 and
   // 36.0, 48 41.9 and 49.9; 40 of 1024 - 4096 34.7 and 29.6, 48 36.5 and 36.7.  Heads of 64 in
   // 4 bits: one sequence of 1024 rows 8.0 and 10.1, 32 of 2048 11.9 and 12.0.)
@@ -604,8 +604,10 @@ AttnPlan plan_packed_attn(const smallkv_chunk_t &c, const smallkv_packed_t &kv, 
   const bool whole = p.few && p.tiles <= c.batch &&
                      (length <= 512 || (length <= 1024 && groups >= 64) || (c.max_len <= 4096 && groups >= 160));
   // eight waves where that is one workgroup per CU (64 of 1024 - 4096 rows 41.8 us, with four
-  // 50.0; 90 of 2048 49.7 and 41.7)
-  p.waves = whole && c.max_len > 512 && groups <= 256 ? 8 : kFewWaves;
+  // 50.0; 90 of 2048 49.7 and 41.7), from 256 rows on where half the CUs have none (one sequence
+  // of 512 rows 9.0 us, with four 9.6; of 300 7.9 and 8.5; 16 of 512 9.5 and 10.0, but 64 of 512
+  // 10.9 and 10.6)
+  p.waves = whole && c.max_len > (groups <= 128 ? 256 : 512) && groups <= 256 ? 8 : kFewWaves;
   // the workgroups that run at once on 256 CUs, two on each; of 4 bits three (64 of 1024 - 4096
   // rows 32.7 us with two, 28.6 with three; in 8 bits 45.4 and 50.8)
   const bool three = p.rows == 16 && kv.dtype == SMALLKV_BF16 && kv.head_dim == 128 && kv.format == SMALLKV_MXFP4;
