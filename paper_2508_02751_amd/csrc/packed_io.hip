@@ -70,8 +70,10 @@ __device__ __forceinline__ void cos_sin(double angle, double &co, double &si) {
 }
 
 // fp32, cut off, the last bit set where the rest is not 0 (infinities and NaN as they are).
+// Cut off, a finite x past fp32's largest number is that number, whose last bit is set.
 __device__ __forceinline__ float round_to_odd(double x) {
-  const float f = (float)x;
+  float f = (float)x;
+  if (fabsf(f) == INFINITY && fabs(x) != (double)INFINITY) f = copysignf(3.402823466e38f, f);
   const double rest = x - (double)f;
   const uint32_t u = __float_as_uint(f);
   if (rest == 0.0 || (u & 1u) || !(fabsf(f) <= 3.402823466e38f)) return f;
