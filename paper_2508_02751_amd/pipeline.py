@@ -123,8 +123,9 @@ class ModelCache:
     it.  With keep_scores, scores [B][layers * Hkv][n_rows] sum the
     attention each row has received, over queries and the query heads of a kv head.
     packed (smallkv.MXFP8 or MXFP4): k and v hold the rows' codes, k_scale and v_scale their
-    blocks' scales (see smallkv.PackedSpec); everything else is the same, and read_back gives
-    the rows as the step takes them.
+    blocks' scales (see smallkv.PackedSpec); read_back gives the rows as the step takes them,
+    and small_inputs a copy of them, to be brought up to date after later chunks; everything
+    else is the same.
     Everything runs on the current stream.
     """
 
@@ -255,11 +256,25 @@ class ModelCache:
                        max_len=max(max(self.rows), 1)).run()
         return k, v
 
-    def small_inputs(self) -> dict:
-        """The small model's entries of a step's inputs (see prepare_step); a packed cache's
-        rows are read back."""
-        k, v = (self.k, self.v) if self.packed is None else self.read_back()
-        x = {"s_k": k, "s_v": v}
+    def small_inputs(self, into: Optional[dict] = None, begin: Optional[Sequence[int]] = None) -> dict:
+        """The small model's entries of a step's inputs (see prepare_step).  A plain cache's rows
+        and the positions are the cache's own tensors, which later chunks reach.  A packed
+        cache's rows are read back, and s_held is counted, as of this call.  into: what an
+        earlier call returned (other entries may be beside it), which is brought up to date in
+        place and returned, so that a step prepared from it finds the present rows; begin[b]: the
+        first row of each sequence that it does not hold yet (None: every row is read again)."""
+        if into is None:
+            k, v = (self.k, self.v) if self.packed is None else self.read_back()
+            x = {"s_k": k, "s_v": v}
+            if self.row_pos is not None:
+                x.update(s_held=self._ints(self.rows), s_row_pos=self.row_pos)
+            return x
+        own = self.packed is not None or (into.get("s_k") is self.k and into.get("s_v") is self.v)
+        if not own or "s_k" not in into or "s_v" not in into or \
+                into.get("s_row_pos") is not self.row_pos or ("s_held" in into) != (self.row_pos is not None):
+            raise ValueError("into must be what small_inputs() of this cache returned")
+        if self.packed is not None:
+            self.read_back((into["s_k"], into["s_v"]), begin)
         if self.row_pos is not None:
-            x.update(s_held=self._ints(self.rows), s_row_pos=self.row_pos)
-        return x
+            into["s_held"].copy_(self._ints(self.rows))
+        return into
