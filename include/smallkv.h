@@ -670,7 +670,8 @@ typedef enum {
  * theirs of head_dim / 32.  The other fields as in smallkv_cache_t; dtype is that of the
  * queries, of the rows to append and of the outputs.  smallkv_append_packed writes scales from
  * 27 to 246 (MXFP4: 252), with which every element is a normal number of bf16 or 0, and 255;
- * outputs that see rows with others are unspecified. */
+ * outputs that see rows with others are unspecified, but a block whose codes are all 0 or -0 is
+ * 0 under every scale below 255 (memory that was cleared holds rows of 0). */
 typedef struct {
   void *k, *v;
   uint8_t *k_scale, *v_scale;

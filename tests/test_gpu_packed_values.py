@@ -1,5 +1,5 @@
 """Values at the edges of packed caches and of the queries over them, against the plain forms in 64
-bits: NaN of every payload."""
+bits: NaN of every payload, rows of codes 0 under any scale."""
 from __future__ import annotations
 
 import pytest
@@ -45,3 +45,57 @@ def test_nan_queries_whatever_their_payload(lens, fmt, dtype):
         assert torch.isnan(out[hit]).all() and torch.isnan(lse[hit]).all(), (out[hit], lse[hit])
         within(out[~hit], clean[0][~hit], clean[2][~hit], "out")
         within(lse[~hit], clean[1][~hit], clean[3][~hit], "lse")
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("fmt", FORMATS, ids=NAMES.get)
+@pytest.mark.parametrize("lens", [[(70, 1), (9, 1)], [(300, 70), (40, 1)]], ids=["few", "many"])
+def test_codes_of_0_are_0_under_every_scale(lens, fmt, dtype):
+    """Rows of zeros (PackedSpec.empty's have scales 0): read, attended to and scored."""
+    S = lib()
+    log(f"[packed] codes 0 {lens} {NAMES[fmt]} {dtype}")
+    c = P.Case(lens, 14, 2, 64, dtype, fmt, 16, seed=42)
+    zeros = torch.tensor([0, 128] if fmt == P.MXFP8 else [0, 8, 128, 136], dtype=torch.uint8)
+    for i, t in enumerate(c.codes):
+        if i % 2:
+            t.copy_(torch.randint(0, 255, t.shape, generator=c.gen, dtype=torch.uint8))
+        else:
+            t.copy_(zeros[torch.randint(0, len(zeros), t.shape, generator=c.gen)])
+    c.codes[1][:, :, ::3] = 0
+    c.codes[3][:, :, 1::3] = 254
+    c.refresh()
+    chunk, cache, q = c.to(DEV)
+    call = S.prepare_chunk_attn(chunk, cache, q, c.scale)
+    call.run()
+    scores = torch.zeros(c.B, 14, c.rows, device=DEV)
+    S.prepare_chunk_scores(chunk, cache, q, call.lse, c.scale, scores).run()
+    to = S.CacheSpec(*(torch.full((c.B, 2, c.rows, 64), 5.0, dtype=dtype, device=DEV) for _ in range(2)))
+    S.prepare_read(cache, to, chunk.length).run()
+    torch.cuda.synchronize()
+    assert (call.out == 0).all()
+    _, lse, _, ltol = R.attention(c)
+    within(call.lse, lse, ltol, "lse")
+    want, tol = R.scores(c, call.lse.cpu(), torch.zeros(c.B, 14, c.rows), per_kv=False)
+    for b, (n, _) in enumerate(c.lens):
+        assert (to.k[b, :, :n] == 0).all() and (to.v[b, :, :n] == 0).all()
+        within(scores[b, :, :n], want[b, :, :n], tol[b, :, :n], f"scores of {b}")
+
+
+def test_an_empty_cache_holds_zeros():
+    S = lib()
+    log("[packed] empty")
+    for fmt in FORMATS:
+        cache = S.PackedSpec.empty(3, 2, 32, 128, fmt)
+        to = S.CacheSpec(*(torch.full((3, 2, 32, 128), 5.0, dtype=F32, device=DEV) for _ in range(2)))
+        length = torch.tensor([32, 1, 17], dtype=torch.int32, device=DEV)
+        S.prepare_read(cache, to, length).run()
+        chunk = S.ChunkSpec(torch.tensor([0, 1, 2, 3], dtype=torch.int32, device=DEV), length, 3, 1, 32)
+        q = torch.randn(3, 4, 128, device=DEV)
+        call = S.prepare_chunk_attn(chunk, cache, q, 0.1)
+        call.run()
+        torch.cuda.synchronize()
+        for b, n in enumerate((32, 1, 17)):
+            assert (to.k[b, :, :n] == 0).all() and (to.v[b, :, n:] == 5.0).all()
+        assert (call.out == 0).all()
+        want = length.cpu().double().log()[:, None].expand(3, 4)
+        within(call.lse, want, 8 * R.U * (1 + want), "lse")
