@@ -1,6 +1,9 @@
-"""Values at the edges of packed caches and of the queries over them, against the plain forms in 64
-bits: NaN of every payload, rows of codes 0 under any scale."""
+"""Values at the edges of packed caches and of the queries over them: NaN of every payload, rows
+of codes 0 under any scale, every code under every scale that an append writes, each read back
+and attended to, against the plain forms in 64 bits."""
 from __future__ import annotations
+
+import math
 
 import pytest
 import torch
@@ -8,7 +11,7 @@ import torch
 import cache_ref as R
 import packed_ref as P
 from parity import log
-from test_gpu_packed_ops import NAMES, lib, within
+from test_gpu_packed_ops import NAMES, lib, same, within
 
 pytestmark = pytest.mark.gpu
 
@@ -99,3 +102,54 @@ def test_an_empty_cache_holds_zeros():
         assert (call.out == 0).all()
         want = length.cpu().double().log()[:, None].expand(3, 4)
         within(call.lse, want, 8 * R.U * (1 + want), "lse")
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("fmt", FORMATS, ids=NAMES.get)
+def test_every_code_under_every_scale(fmt, dtype):
+    """Read back, under every scale that an append writes; and attended to by a token whose
+    weights are equal (keys 0): the mean of the values, under those that do not overflow in it."""
+    S = lib()
+    log(f"[packed] every code {NAMES[fmt]} {dtype}")
+    g = torch.Generator().manual_seed(43)
+    codes = torch.arange(256, dtype=torch.uint8)
+    if fmt == P.MXFP8:
+        codes[127], codes[255] = 0, 128  # (no NaN)
+    codes = codes[torch.randperm(256, generator=g)]
+    width = 64 if fmt == P.MXFP8 else 32
+    rows = codes.view(-1, width)
+    n = rows.shape[0]
+    cache = S.PackedSpec.empty(1, 1, n, 64, fmt)
+    cache.v.copy_(rows.view(1, 1, n, width).to(DEV))
+    to = S.CacheSpec(*(torch.zeros(1, 1, n, 64, dtype=dtype, device=DEV) for _ in range(2)))
+    length = torch.tensor([n], dtype=torch.int32, device=DEV)
+    chunk = S.ChunkSpec(torch.tensor([0, 1], dtype=torch.int32, device=DEV), length, 1, 1, n)
+    q = torch.randn(1, 2, 64, generator=g).to(DEV, dtype)
+    read = S.prepare_read(cache, to, length)
+    attn = S.prepare_chunk_attn(chunk, cache, q, 0.125)
+    for x in range(27, 247 if fmt == P.MXFP8 else 253):
+        cache.v_scale.fill_(x)
+        read.run()
+        attn.run()
+        torch.cuda.synchronize()
+        want = P.unpack(rows, torch.full((n, 2), x, dtype=torch.uint8), fmt)
+        same(to.v.view(n, 64), want.to(dtype), f"scale {x}")
+        if x > 240:  # (a sum of n values of up to 448 * 2^113, or 6 * 2^113, is below 2^128)
+            continue
+        # n sums, a division and its product, each off by a rounding of fp32 of at most the sum of
+        # magnitudes; the output's rounding
+        mean, size = want.mean(0), want.abs().mean(0)
+        tol = (n + 4) * R.U * size + 1.01 * R.HALF[dtype] * mean.abs()
+        within(attn.out.view(2, 64), mean.expand(2, 64), tol.expand(2, 64), f"mean under scale {x}")
+        within(attn.lse, torch.full((1, 2), math.log(n)), torch.full((1, 2), 8 * R.U * (1 + math.log(n))), "lse")
+    # what an append makes of a block with an infinity: codes 0, scale 255
+    cache.v.zero_()
+    cache.v_scale.zero_()
+    cache.v_scale[0, 0, 1, 1] = 255
+    read.run()
+    attn.run()
+    torch.cuda.synchronize()
+    hit = torch.zeros(64, dtype=torch.bool)
+    hit[32:] = True
+    assert torch.isnan(to.v[0, 0, 1, 32:]).all() and (to.v[0, 0, 1, :32] == 0).all() and (to.v[0, 0, 2:] == 0).all()
+    assert torch.isnan(attn.out[0, :, hit]).all() and (attn.out[0, :, ~hit] == 0).all()
