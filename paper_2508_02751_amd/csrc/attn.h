@@ -202,23 +202,17 @@ template <typename L, int BN, int SHARE> struct Loader {
 };
 
 // fp32 as a sum of three bf16 numbers (exactly, but for what lies below 2^-133), or as two
-// with an error of 2^-17 of it; infinities and NaN (as arithmetic leaves them) in the first.
+// with an error of 2^-17 of it; infinities in the first.  NaN in all (cut off, one that only
+// bits below bf16's tell from an infinity is that infinity).
 template <int PARTS> __device__ __forceinline__ void split(float x, float (&y)[PARTS]) {
   y[0] = bf16_hi(__float_as_uint(x));
-  float rest = fabsf(x) <= 3.402823466e38f ? x - y[0] : 0.0f;
+  float rest = fabsf(x) == INFINITY ? 0.0f : x - y[0];
 #pragma unroll
   for (int i = 1; i + 1 < PARTS; ++i) {
     y[i] = bf16_hi(__float_as_uint(rest));
     rest -= y[i];
   }
   if (PARTS > 1) y[PARTS - 1] = rest;
-}
-
-// An element from memory for `split`: of a NaN that only bits below bf16's tell from an
-// infinity the first part would be that infinity.
-__device__ __forceinline__ float quiet(float x) {
-  const uint32_t u = __float_as_uint(x);
-  return (u & 0x7fffffffu) > 0x7f800000u ? __uint_as_float(u | 0x400000u) : x;
 }
 
 template <typename T, int D> struct QFrag;
@@ -251,7 +245,7 @@ template <int D> struct QFrag<wide_t, D> {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         float y[3];
-        split<3>(quiet(reinterpret_cast<const float *>(row)[s * 16 + half * 8 + e]), y);
+        split<3>(reinterpret_cast<const float *>(row)[s * 16 + half * 8 + e], y);
 #pragma unroll
         for (int p = 0; p < 3; ++p) x[p][e] = (__bf16)y[p];
       }

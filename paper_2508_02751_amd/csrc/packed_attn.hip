@@ -296,7 +296,7 @@ __global__ __launch_bounds__(NW * kWave, 2) void packed_few(AttnArgs a) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           float y[QP];
-          split<QP>(quiet(reinterpret_cast<const float *>(x)[8 * i + e]), y);
+          split<QP>(reinterpret_cast<const float *>(x)[8 * i + e], y);
 #pragma unroll
           for (int p = 0; p < QP; ++p) q[c][p][i][e] = (__bf16)y[p];
         }
