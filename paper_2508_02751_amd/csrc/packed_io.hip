@@ -70,15 +70,15 @@ __device__ __forceinline__ void cos_sin(double angle, double &co, double &si) {
 }
 
 // fp32, cut off, the last bit set where the rest is not 0 (infinities and NaN as they are).
-// Cut off, a finite x past fp32's largest number is that number, whose last bit is set.
+// Cut off, a finite x past fp32's largest number is that number, whose last bit is set: one step
+// back from the infinity that it converts to.
 __device__ __forceinline__ float round_to_odd(double x) {
-  float f = (float)x;
-  if (fabsf(f) == INFINITY && fabs(x) != (double)INFINITY) f = copysignf(3.402823466e38f, f);
-  const double rest = x - (double)f;
+  const float f = (float)x;
+  const double rest = x - (double)f;  // NaN of infinities and NaN
   const uint32_t u = __float_as_uint(f);
-  if (rest == 0.0 || (u & 1u) || !(fabsf(f) <= 3.402823466e38f)) return f;
+  if (!(rest < 0.0 || rest > 0.0) || (u & 1u)) return f;
   // an even f that is not x: one step towards x is odd
-  const bool grow = (rest > 0.0) == (f > 0.0) || f == 0.0f;
+  const bool grow = (rest > 0.0) == (f > 0.0);
   if (f == 0.0f) return __uint_as_float((__double2hiint(x) & 0x80000000u) | 1u);
   return __uint_as_float(grow ? u + 1u : u - 1u);
 }
