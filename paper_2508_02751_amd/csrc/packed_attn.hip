@@ -21,9 +21,11 @@
 //   a token each of 4 sequences of 90001 - 131072 rows, 32 and 8 heads of 128, 8 bits (900 MB):
 //     170 us, 5.3 TB/s, memory; in 4 bits (468 MB) 100 us, 4.7 TB/s, 122 where a page holds
 //     [row][head], so that a head's 64 bytes lie 512 apart;
-//   one token over 512 rows in fp32: 10.7 us, a chain of four dependent loads, four tiles a wave;
+//   one token over 512 rows in fp32: 10.3 us, a chain of three dependent loads, two tiles a wave;
 //   2 x 2048 tokens over 16384 rows, 32 and 8 heads of 128: 1145 us, 900 TFLOP/s, in 4 bits 1010:
-//     products and softmax by turns, as over bf16 rows, and the unpacking.
+//     products and softmax by turns, as over bf16 rows, and the unpacking;
+//   4 x 4096 tokens over 16384 rows, 14 and 2 heads of 64: 1273 us, 660 TFLOP/s, in 4 bits 1285, more
+//     than over bf16 rows (1085, workgroups of four waves, three on a CU): a CU has one workgroup.
 #include <type_traits>
 
 #include "attn.h"
@@ -31,8 +33,9 @@
 namespace smallkv {
 namespace {
 
-// Values of a tile in LDS as TileLayout has them, and neighbouring pieces exchanged so that a
-// piece of codes, which becomes two or four, is written without a conflict of banks.
+// Values of a tile in LDS as TileLayout has them, and neighbouring pieces exchanged against the
+// conflicts of banks in which a piece of codes, which becomes two or four, would be written.  (Of
+// the LDS cycles of 2 x 2048 tokens over 16384 rows 16% are lost to conflicts.)
 template <int D> struct MixedTile : TileLayout<bf16_t, D> {
   __device__ __forceinline__ static int swz_v(int r) {
     return D == 128 ? (r & 3) << 2 | (r & 3) : (r >> 1 & 1) << 2 | (r >> 1 & 3);
@@ -195,7 +198,9 @@ template <int D, int F> struct RowTile {
 };
 
 // Keys of a wave in LDS, as they are: written whole rows at a time, read a piece of 16 rows at a
-// time, both without a conflict of banks.
+// time, the pieces of a row exchanged against conflicts of banks.  (Not free of them: of the LDS
+// cycles of a decode step, keys and values, 32% are lost to conflicts, of a long one in 4 bits 36%;
+// which accesses have them was not found.)
 template <int D, int F> struct KeyTile {
   using X = RowTile<D, F>;
   __device__ __forceinline__ static int swz(int r) { return r / (16 / X::P) & (X::P - 1); }
@@ -224,7 +229,7 @@ template <int D, int F> struct KeyTile {
 };
 
 // Values of a wave's 32 keys in LDS, in bf16: written as they come, read 32 bytes of 8 rows at a
-// time, both without a conflict of banks.
+// time, their pieces exchanged against conflicts of banks as those of the keys.
 template <int D, int F> struct ValueTile {
   using X = RowTile<D, F>;
   static constexpr int bytes = 2 * D, kLow = X::R == 8 ? 0 : X::R == 16 ? 1 : 2;
@@ -589,7 +594,8 @@ AttnPlan plan_packed_attn(const smallkv_chunk_t &c, const smallkv_packed_t &kv, 
   // as many rows 38 and 57; bf16, 28 rows: 25 and 27, 23 and 32)
   // Many rows, bf16: tiles of 256 where that leaves little of the last one empty: half as much
   // to unpack (2 x 2048 tokens over 16384 rows of 8 kv heads of 128: 1144 us, 1189 in tiles of
-  // 128, in 4 bits 999 and 1109; 1200 rows of 8 sequences 596 and 579).
+  // 128, in 4 bits 999 and 1109; 1200 rows of 8 sequences 596 and 579; heads of 64 were not
+  // compared).
   p.few = rows <= (f32 ? 64 : 32);
   p.rows = !p.few ? (rows >= 1536 && !f32 ? 256 : 128) : f32 || rows <= 16 ? 16 : 32;
   // no more tiles than this, whatever the sequences' lengths
@@ -598,8 +604,10 @@ AttnPlan plan_packed_attn(const smallkv_chunk_t &c, const smallkv_packed_t &kv, 
   // not long; else spans, and a join.  (28 query and 4 kv heads of 128 in 8 bits, us: one
   // sequence of 512 rows 9.0, in spans 10.8; of 1024 12.6 and 11.3; 16 of 1024 rows 13.3 and
   // 14.1, 48 13.9 and 19.5; 24 of 2048 20.6 and 19.9, 48 22.5 and 28.4; 32 of 4096 35.9 and
-  // 36.0, 48 41.9 and 49.9; 40 of 1024 - 4096 34.7 and 29.6, 48 36.5 and 36.7.  Heads of 64 in
-  // 4 bits: one sequence of 1024 rows 8.0 and 10.1, 32 of 2048 11.9 and 12.0.)
+  // 36.0, 48 41.9 and 49.9; 40 of 1024 - 4096 34.7 and 29.6, 48 36.5 and 36.7: with such mixed
+  // lengths whole sequences lose at 160 groups, where the rule begins to take them, and no longer
+  // at 192.  Heads of 64 in 4 bits: one sequence of 1024 rows 8.0 and 10.1, 32 of 2048 11.9 and
+  // 12.0.  Many groups past 4096 rows, and that limit with heads of 64, were not measured.)
   const int64_t groups = (int64_t)p.tiles * kv.n_heads, length = (int64_t)c.max_len * kv.head_dim / 128;
   const bool whole = p.few && p.tiles <= c.batch &&
                      (length <= 512 || (length <= 1024 && groups >= 64) || (c.max_len <= 4096 && groups >= 160));

@@ -13,7 +13,9 @@
 // read and written) 88 us, 5.3 TB/s; 8000 of 28 + 2 x 4 heads 33 us; one token each of 64
 // sequences 5.6 us, a launch and a chain of dependent loads (sequence, page) beside which the
 // rows and angles are on their way.  Read: 4 x 20000 - 32768 rows of 32 heads of 64 from 8 bits
-// to bf16 (1.26 GB) 266 us, the rate of a large copy.
+// to bf16 (1.26 GB) 266 us, the rate of a large copy.  Few (sequence, head) pairs make too few
+// workgroups for it, at most 32 a pair for K and as many for V: one sequence of 32768 rows of 8
+// heads of 128 from 8 bits to bf16 (203 MB) 84 us, 2.4 TB/s, of 2 heads of 64 (25 MB) 23 us, 1.1 TB/s.
 #include <algorithm>
 
 #include "launch.h"
